@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "common.h"
+#include "host.h"
 #include "mla_probe.h"
 #include "moe.h"
 #include "oproj.h"
@@ -24,11 +25,12 @@
 // life of the process); host code reaches it only through scratch_address().
 static __device__ __align__(256) unsigned char scratch[MLA_NOALLOC_SCRATCH_BYTES];
 
-namespace {
+static thread_local std::string g_detail;
 
-thread_local std::string g_detail;
+namespace mla {
 
-mla_status fail(mla_status s, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+void clear_detail() { g_detail.clear(); }
+
 mla_status fail(mla_status s, const char* fmt, ...) {
   char buf[512];
   va_list ap;
@@ -43,14 +45,9 @@ mla_status hip_fail(hipError_t e, const char* what) {
   return fail(MLA_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 // ---------------------------------------------------------------------------
 // validation
 // ---------------------------------------------------------------------------
-// width of one head output: the latent, plus the RoPE dims when the value is rotary
-int32_t head_dv(const mla_geom* g) { return g->d_latent + (g->value_rope ? g->d_rope : 0); }
-
 mla_status check_geom(const mla_geom* g, bool for_oproj) {
   if (g == nullptr) return fail(MLA_ERR_NULL, "geom is NULL");
   if (g->n_heads < 1 || g->n_groups < 1 || g->n_heads % g->n_groups != 0)
@@ -79,6 +76,24 @@ mla_status check_geom(const mla_geom* g, bool for_oproj) {
   }
   return MLA_OK;
 }
+
+void rope_theta_rev(const mla_geom* g, double* th) {
+  const double two_pi = 6.283185307179586476925286766559;
+  for (int j = 0; j < g->d_rope / 2; ++j) th[j] = std::pow(g->rope_base, -2.0 * j / g->d_rope) / two_pi;
+}
+
+}  // namespace mla
+
+namespace {
+
+using mla::aligned16;
+using mla::check_geom;
+using mla::fail;
+using mla::hip_fail;
+using mla::rope_theta_rev;
+
+// width of one head output: the latent, plus the RoPE dims when the value is rotary
+int32_t head_dv(const mla_geom* g) { return g->d_latent + (g->value_rope ? g->d_rope : 0); }
 
 // Segments: lengths >= 1; storage and request intervals both tile [0, N).
 mla_status check_segments(const mla_segment* segs, int32_t n, int64_t* n_rows) {
@@ -194,12 +209,6 @@ void segment_tables(const mla_geom* g, const mla_segment* segs, int32_t n_segs, 
     if (!offline) cum += (int64_t)G * T->info[i].length * T->info[i].n_chunks;
   }
   T->global_parts = cum;
-}
-
-// RoPE frequencies in revolutions: base^(-2j/d_r) / (2 pi)
-void rope_theta_rev(const mla_geom* g, double* th) {
-  const double two_pi = 6.283185307179586476925286766559;
-  for (int j = 0; j < g->d_rope / 2; ++j) th[j] = std::pow(g->rope_base, -2.0 * j / g->d_rope) / two_pi;
 }
 
 // offline: the producer's plan (Alg. 1) -- every segment sees only itself, and
