@@ -488,6 +488,143 @@ mla_status mla_moe_fanout(int64_t n_rows, int32_t n_experts, const float* router
 mla_status mla_shared_wb(int64_t n_rows, int32_t d_in, int32_t d_out, const void* z, const void* w_b,
                          int32_t out_dtype, void* y, void* stream);
 
+/* ----------------------------------------------------------------------------
+ * The 4-bit format "mx4" of cached latents and of W_b: groups of 32 consecutive
+ * values; a value is an e2m1 code (sign, and 0 0.5 1 1.5 2 3 4 6) times its
+ * group's scale.  Codes are two a byte, the even value in the low nibble; a scale
+ * is one byte e that stands for 2^(e - 127), and e = 255 makes its group NaN.
+ * What a code stands for is exact in bf16.
+ *
+ * mla_mx4_quantize: bf16 values to codes and scales.  The scale is
+ * 2^(floor(log2 max|x|) - 2), one power more where max|x| is 7 times it or more;
+ * codes round to nearest, ties to the even code.  A group of zeros has e = 0; a
+ * group with a NaN or an infinity has e = 255 and codes 0.  Every step is exact,
+ * so the result does not depend on the machine.
+ * mla_mx4_dequantize: back to bf16 (with mla_shared_wb, W_b for many rows).
+ *
+ *   n_rows, n_cols  N rows (>= 0) of n_cols values (a multiple of 32)
+ *   x               device bf16 [N, n_cols], rows x_stride elements apart (a
+ *                   multiple of 8, at least n_cols), 16-byte aligned
+ *   codes           device [N, n_cols/2] bytes, 16-byte aligned
+ *   scales          device [N, n_cols/32] bytes
+ * Errors: NULL, SHAPE, HIP.  Kernels only: may be captured.
+ * ------------------------------------------------------------------------- */
+mla_status mla_mx4_quantize(int64_t n_rows, int32_t n_cols, const void* x, int64_t x_stride, void* codes, void* scales,
+                            void* stream);
+
+mla_status mla_mx4_dequantize(int64_t n_rows, int32_t n_cols, const void* codes, const void* scales, void* x,
+                              int64_t x_stride, void* stream);
+
+/* y = W_b z as mla_shared_wb, with W_b in mx4, for the rows of a decode step or a
+ * chunk of new tokens: at most MLA_WB_MX4_MAX_ROWS (more rows are bound by the
+ * matrix cores, not by the weight: dequantize once and call mla_shared_wb).
+ * Products and sums as in mla_shared_wb (bf16 MFMA, fp32 sums), in an order that
+ * depends on d_in alone: a row of z gives the same bits in any call.
+ *   n_rows, d_in, d_out  as for mla_shared_wb (d_in up to MLA_WB_MAX_D_IN)
+ *   z              [N, d_in] bf16 device, 16-byte aligned
+ *   w_codes        [d_out, d_in/2] device, 16-byte aligned
+ *   w_scales       [d_out, d_in/32] device, 4-byte aligned
+ *   out_dtype, y   as for mla_shared_wb
+ * Errors: NULL, SHAPE, UNSUPPORTED, HIP.  Kernels only: may be captured. */
+#define MLA_WB_MAX_D_IN 16384
+#define MLA_WB_MX4_MAX_ROWS 1024
+mla_status mla_shared_wb_mx4(int64_t n_rows, int32_t d_in, int32_t d_out, const void* z, const void* w_codes,
+                             const void* w_scales, int32_t out_dtype, void* y, void* stream);
+
+/* ----------------------------------------------------------------------------
+ * The paged 4-bit latent cache: what a decode loop keeps of every token once a
+ * request (or a document of its own) has been computed, 400 bytes a row in place
+ * of kv's 1152.  Built for (d_latent, d_rope) = (512, 64), the latent as the
+ * value.
+ *
+ * A cache is an array of cache_pages pages of page_rows rows (a multiple of 64,
+ * at most MLA_CACHE_MAX_PAGE_ROWS); a page is page_rows * 400 bytes:
+ *   codes   [page_rows, 256]     the latent in mx4, 16 groups a row
+ *   scales  [page_rows, 16]
+ *   rope    [page_rows, 64] bf16 the RoPE key, turned to its position in the
+ *                                page's frame
+ * Row r of page p has slot p * page_rows + r.
+ *
+ * mla_cache_append: rows of kv into the cache.
+ *   geom       d_latent, d_rope and rope_base are used
+ *   n_rows     N rows (>= 0)
+ *   kv         device bf16 [N, D]: latent and RoPE key, rows kv_stride elements
+ *              apart (a multiple of 8, at least D), 16-byte aligned
+ *   pos        device int32 [N] or NULL: the RoPE key is turned by R(pos[n]) on
+ *              its way (in fp32, rounded to bf16 once); NULL: it is already in the
+ *              page's frame (the kv of mla_online_attend) and is copied
+ *   slots      device int32 [N]: where each row goes; a slot outside the cache
+ *              (any negative number: a padded row) skips the row.  A slot must not
+ *              be given twice in a call: what it then holds is not defined, all
+ *              other rows are right
+ *   cache      device, 16-byte aligned
+ * mla_cache_gather: rows of the cache back as kv (what mla_online_attend and
+ * mla_offline_produce take, where the pages are in their documents' frames);
+ * row n of kv is left as it was where slots[n] is outside the cache.  A slot may
+ * be given any number of times.
+ * Errors: NULL, SHAPE, UNSUPPORTED, HIP.  Kernels only: may be captured.
+ * ------------------------------------------------------------------------- */
+#define MLA_CACHE_MAX_PAGE_ROWS 65536
+mla_status mla_cache_append(const mla_geom* geom, int64_t n_rows, const void* kv, int64_t kv_stride, const int32_t* pos,
+                            const int32_t* slots, int64_t cache_pages, int32_t page_rows, void* cache, void* stream);
+
+mla_status mla_cache_gather(const mla_geom* geom, int64_t n_rows, const int32_t* slots, int64_t cache_pages,
+                            int32_t page_rows, const void* cache, void* kv, int64_t kv_stride, void* stream);
+
+/* One page of a request, as mla_cache_attend sees it.
+ *  page     page of the cache; outside [0, cache_pages): the entry holds no key
+ *  rows     rows of the page that may be keys, the first ones (clamped to
+ *           [0, page_rows]); a document may end inside a page
+ *  req_pos  request position of the page's first row; row i is at req_pos + i
+ *  frame    request position of the origin of the page's RoPE frame: 0 for keys
+ *           turned to their request positions, a document's offset (Delta_i) for
+ *           keys in its canonical frame.  Pages can so be shared by requests that
+ *           hold the document at different places. */
+typedef struct mla_page {
+  int32_t page;
+  int32_t rows;
+  int32_t req_pos;
+  int32_t frame;
+} mla_page;
+
+/* Attention of new tokens over the cache: every head of each token attends to the
+ * keys of its request at positions up to its own, the query's RoPE part turned by
+ * R(t - frame) for each page (eq:rope); the value is the latent.
+ *   geom       n_heads, rope_base and softmax_scale are used
+ *   n_seqs     requests in the batch (0 .. 65535)
+ *   n_q        new tokens of each request (>= 1; n_q * n_heads at most
+ *              MLA_CACHE_MAX_HEAD_ROWS)
+ *   q          device bf16 [n_seqs, n_q, H, D], RoPE part unrotated, 16-byte aligned
+ *   pos        device int32 [n_seqs, n_q]: request position t of each token, in any
+ *              order; negative: the token sees no key (padding)
+ *   pages      device [n_seqs, max_pages], 16-byte aligned: the requests' pages in
+ *              any order; a key at position p is seen iff p <= t, so rows allocated
+ *              but not yet written need no mark (their contents do not matter)
+ *   seq_pages  device int32 [n_seqs]: entries in use (clamped to [0, max_pages])
+ *   cache_pages, page_rows, cache   as for mla_cache_append
+ *   out_o      device bf16 [n_seqs, n_q, H, d_latent], 16-byte aligned: 0 where a
+ *              token sees no key
+ *   out_lse    device f32 [n_seqs, n_q, H] or NULL: natural-log lse of the scaled
+ *              scores, -infinity where a token sees no key
+ *   workspace  device, 256-byte aligned, mla_cache_attend_query bytes; overwritten
+ *              (calls that may overlap need one each)
+ * Everything that changes from token to token is read on the device, so a decode
+ * step is captured once and replayed as positions and pages change.  The result
+ * does not depend on timing: a call gives the same bits again.  The split of a request's keys, and with it the order of its
+ * sums, depends on the whole batch.
+ * A NaN in a key makes every row NaN that sees it, and may make NaN the rows of
+ * the same call and request that come before it.
+ * n_seqs, n_q, H and the pages' totals fix the workspace.
+ * Errors: NULL, SHAPE, UNSUPPORTED, WORKSPACE, HIP.  Kernels only. */
+#define MLA_CACHE_MAX_HEAD_ROWS 16384
+mla_status mla_cache_attend_query(const mla_geom* geom, int32_t n_seqs, int32_t n_q, int32_t max_pages, int32_t page_rows,
+                                  size_t* ws_bytes);
+
+mla_status mla_cache_attend(const mla_geom* geom, int32_t n_seqs, int32_t n_q, const void* q, const int32_t* pos,
+                            const mla_page* pages, const int32_t* seq_pages, int32_t max_pages, int64_t cache_pages,
+                            int32_t page_rows, const void* cache, void* out_o, float* out_lse, void* workspace,
+                            size_t ws_bytes, void* stream);
+
 /* Static description of a status code. */
 const char* mla_status_str(mla_status s);
 

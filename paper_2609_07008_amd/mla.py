@@ -24,7 +24,9 @@ EXPORTS = ("mla_online_attend_query", "mla_online_attend", "mla_segment_merge", 
            "mla_online_attend_planned_noalloc", "mla_sliced_oproj_add_planned",
            "mla_offline_produce_query", "mla_offline_produce", "mla_protected_rows_query", "mla_protected_rows",
            "mla_protected_rows_planned_query", "mla_protected_rows_planned",
-           "mla_moe_fanout", "mla_shared_wb", "mla_probe_mfma_bf16", "mla_status_str", "mla_last_error_detail",
+           "mla_moe_fanout", "mla_shared_wb", "mla_mx4_quantize", "mla_mx4_dequantize", "mla_shared_wb_mx4",
+           "mla_cache_append", "mla_cache_gather", "mla_cache_attend_query", "mla_cache_attend",
+           "mla_probe_mfma_bf16", "mla_status_str", "mla_last_error_detail",
            "mla_version")
 
 
@@ -84,13 +86,21 @@ def _load(path: str = LIB_PATH):
     lib.mla_protected_rows_planned.argtypes = [IP, P, ctypes.POINTER(ProtectCfg), P, P, P, P, P, SZ, P]
     lib.mla_moe_fanout.argtypes = [I64, I32, P, I32, I32, ctypes.c_float, P, P, P, P, P]
     lib.mla_shared_wb.argtypes = [I64, I32, I32, P, P, I32, P, P]
+    lib.mla_mx4_quantize.argtypes = [I64, I32, P, I64, P, P, P]
+    lib.mla_mx4_dequantize.argtypes = [I64, I32, P, P, P, I64, P]
+    lib.mla_shared_wb_mx4.argtypes = [I64, I32, I32, P, P, P, I32, P, P]
+    lib.mla_cache_append.argtypes = [GP, I64, P, I64, P, P, I64, I32, P, P]
+    lib.mla_cache_gather.argtypes = [GP, I64, P, I64, I32, P, P, I64, P]
+    lib.mla_cache_attend_query.argtypes = [GP, I32, I32, I32, I32, ctypes.POINTER(SZ)]
+    lib.mla_cache_attend.argtypes = [GP, I32, I32, P, P, P, P, I32, I64, I32, P, P, P, P, SZ, P]
     lib.mla_probe_mfma_bf16.argtypes = [I32, ctypes.POINTER(ctypes.c_double), P, P]
     for f in ("mla_online_attend_query", "mla_online_attend", "mla_segment_merge", "mla_sliced_oproj_add",
               "mla_online_plan_query", "mla_online_plan", "mla_online_attend_planned",
               "mla_online_attend_planned_noalloc", "mla_sliced_oproj_add_planned", "mla_offline_produce_query",
               "mla_offline_produce", "mla_protected_rows_query", "mla_protected_rows",
               "mla_protected_rows_planned_query", "mla_protected_rows_planned", "mla_moe_fanout", "mla_shared_wb",
-              "mla_probe_mfma_bf16"):
+              "mla_mx4_quantize", "mla_mx4_dequantize", "mla_shared_wb_mx4", "mla_cache_append", "mla_cache_gather",
+              "mla_cache_attend_query", "mla_cache_attend", "mla_probe_mfma_bf16"):
         getattr(lib, f).restype = ctypes.c_int
     lib.mla_status_str.argtypes = [ctypes.c_int]
     lib.mla_status_str.restype = ctypes.c_char_p
@@ -315,6 +325,141 @@ def shared_wb(z, w_b, y, stream=None):
     d_out = int(w_b.shape[0])
     out = MLA_BF16 if y.dtype == torch.bfloat16 else MLA_F32
     _check(LIB.mla_shared_wb(n, d_in, d_out, _ptr(z), _ptr(w_b), out, _ptr(y), _stream(stream)))
+
+
+# The calls below take tensors on the current device and check what the C ABI cannot see
+# (types, shapes, strides, the device); a refusal raises MlaError like the library's own.
+CACHE_ROW_BYTES = 400   # a row of the paged 4-bit cache: 256 code bytes, 16 scales, 64 bf16
+
+
+def _need(ok: bool, what: str, status: int = 2):
+    if not ok:
+        raise MlaError(status, what)
+
+
+def _tensor(name, t, dtype, shape=None, rows=False):
+    """t is a device tensor of dtype and, if given, shape; contiguous, or (rows) with
+    contiguous rows.  Empty tensors pass with any strides."""
+    _need(isinstance(t, torch.Tensor), f"{name} is not a tensor", 1)
+    _need(t.dtype == dtype, f"{name} is {t.dtype}, expected {dtype}")
+    _need(t.is_cuda and t.device.index == torch.cuda.current_device(), f"{name} is on {t.device}, not the current device")
+    if shape is not None:
+        _need(tuple(t.shape) == tuple(shape), f"{name} is {tuple(t.shape)}, expected {tuple(shape)}")
+    if rows:
+        _need(t.dim() == 2 and (t.stride(1) == 1 or t.numel() == 0), f"{name} has strides {t.stride()}")
+    else:
+        _need(t.is_contiguous(), f"{name} is not contiguous")
+
+
+def _row_stride(t) -> int:
+    """Elements between rows; of a single row (whose stride is arbitrary) its width rounded up."""
+    return int(t.stride(0)) if t.shape[0] > 1 else -(-int(t.shape[1]) // 8) * 8
+
+
+def mx4_quantize(x, codes, scales, stream=None):
+    """bf16 rows into the 4-bit format (mla_mx4_quantize): x [N, C] bfloat16 with
+    contiguous rows, codes [N, C/2] and scales [N, C/32] uint8, written."""
+    _tensor("x", x, torch.bfloat16, rows=True)
+    n, c = int(x.shape[0]), int(x.shape[1])
+    _tensor("codes", codes, torch.uint8, (n, c // 2))
+    _tensor("scales", scales, torch.uint8, (n, c // 32))
+    _check(LIB.mla_mx4_quantize(n, c, _ptr(x), _row_stride(x), _ptr(codes), _ptr(scales), _stream(stream)))
+
+
+def mx4_dequantize(codes, scales, x, stream=None):
+    """The values of codes [N, C/2] and scales [N, C/32] into x [N, C] bfloat16
+    (mla_mx4_dequantize)."""
+    _tensor("x", x, torch.bfloat16, rows=True)
+    n, c = int(x.shape[0]), int(x.shape[1])
+    _tensor("codes", codes, torch.uint8, (n, c // 2))
+    _tensor("scales", scales, torch.uint8, (n, c // 32))
+    _check(LIB.mla_mx4_dequantize(n, c, _ptr(codes), _ptr(scales), _ptr(x), _row_stride(x), _stream(stream)))
+
+
+def shared_wb_mx4(z, w_codes, w_scales, y, stream=None):
+    """y = W_b z with W_b in 4 bits (mla_shared_wb_mx4): z [N, d_in] bfloat16,
+    w_codes [d_out, d_in/2] and w_scales [d_out, d_in/32] uint8, y [N, d_out] float32
+    or bfloat16."""
+    _tensor("z", z, torch.bfloat16)
+    _need(z.dim() == 2, f"z is {tuple(z.shape)}")
+    n, d_in = int(z.shape[0]), int(z.shape[1])
+    _tensor("w_codes", w_codes, torch.uint8)
+    _need(w_codes.dim() == 2 and int(w_codes.shape[1]) * 2 == d_in, f"w_codes is {tuple(w_codes.shape)}, z {tuple(z.shape)}")
+    d_out = int(w_codes.shape[0])
+    _tensor("w_scales", w_scales, torch.uint8, (d_out, d_in // 32))
+    _need(isinstance(y, torch.Tensor) and y.dtype in (torch.float32, torch.bfloat16), "y is not float32 or bfloat16")
+    _tensor("y", y, y.dtype, (n, d_out))
+    out = MLA_BF16 if y.dtype == torch.bfloat16 else MLA_F32
+    _check(LIB.mla_shared_wb_mx4(n, d_in, d_out, _ptr(z), _ptr(w_codes), _ptr(w_scales), out, _ptr(y), _stream(stream)))
+
+
+def _cache_pages(cache, page_rows) -> int:
+    """Pages of a cache tensor [pages, page_rows * CACHE_ROW_BYTES] uint8."""
+    _tensor("cache", cache, torch.uint8)
+    _need(cache.dim() == 2 and int(cache.shape[1]) == int(page_rows) * CACHE_ROW_BYTES,
+          f"cache is {tuple(cache.shape)}, expected [pages, {int(page_rows)} * {CACHE_ROW_BYTES}]")
+    return int(cache.shape[0])
+
+
+def cache_append(geom, kv, slots, cache, page_rows: int, pos=None, stream=None):
+    """Rows of kv [N, d_latent + d_rope] bfloat16 (contiguous rows) into the paged 4-bit
+    cache [pages, page_rows * CACHE_ROW_BYTES] uint8 at slots [N] int32, the RoPE part
+    turned to pos [N] int32 if given (mla_cache_append)."""
+    g = make_geom(geom)
+    pages = _cache_pages(cache, page_rows)
+    _tensor("kv", kv, torch.bfloat16, rows=True)
+    n = int(kv.shape[0])
+    _need(int(kv.shape[1]) == g.d_latent + g.d_rope, f"kv is {tuple(kv.shape)}")
+    _tensor("slots", slots, torch.int32, (n,))
+    if pos is not None:
+        _tensor("pos", pos, torch.int32, (n,))
+    _check(LIB.mla_cache_append(ctypes.byref(g), n, _ptr(kv), _row_stride(kv), _ptr(pos), _ptr(slots), pages, int(page_rows),
+                                _ptr(cache), _stream(stream)))
+
+
+def cache_gather(geom, slots, cache, page_rows: int, kv, stream=None):
+    """Rows slots [N] int32 of the cache into kv [N, d_latent + d_rope] bfloat16
+    (mla_cache_gather); rows whose slot is outside the cache are left as they were."""
+    g = make_geom(geom)
+    pages = _cache_pages(cache, page_rows)
+    _tensor("kv", kv, torch.bfloat16, rows=True)
+    n = int(kv.shape[0])
+    _need(int(kv.shape[1]) == g.d_latent + g.d_rope, f"kv is {tuple(kv.shape)}")
+    _tensor("slots", slots, torch.int32, (n,))
+    _check(LIB.mla_cache_gather(ctypes.byref(g), n, _ptr(slots), pages, int(page_rows), _ptr(cache), _ptr(kv), _row_stride(kv),
+                                _stream(stream)))
+
+
+def cache_attend_query(geom, n_seqs: int, n_q: int, max_pages: int, page_rows: int) -> int:
+    """Host-only: workspace bytes of mla_cache_attend."""
+    g = make_geom(geom)
+    ws = ctypes.c_size_t()
+    _check(LIB.mla_cache_attend_query(ctypes.byref(g), int(n_seqs), int(n_q), int(max_pages), int(page_rows), ctypes.byref(ws)))
+    return ws.value
+
+
+def cache_attend(geom, q, pos, pages, seq_pages, cache, page_rows: int, out_o, out_lse=None, workspace=None, stream=None):
+    """Attention of new tokens over the paged 4-bit cache (mla_cache_attend): q
+    [B, n_q, H, d_latent + d_rope] bfloat16, pos [B, n_q] int32, pages [B, max_pages, 4]
+    int32 (page, rows, req_pos, frame), seq_pages [B] int32, out_o [B, n_q, H, d_latent]
+    bfloat16, out_lse [B, n_q, H] float32 or None."""
+    g = make_geom(geom)
+    n_pages = _cache_pages(cache, page_rows)
+    _need(isinstance(q, torch.Tensor) and q.dim() == 4, "q is not a tensor [B, n_q, H, D]")
+    b, n_q = int(q.shape[0]), int(q.shape[1])
+    _tensor("q", q, torch.bfloat16, (b, n_q, g.n_heads, g.d_latent + g.d_rope))
+    _tensor("pos", pos, torch.int32, (b, n_q))
+    _need(isinstance(pages, torch.Tensor) and pages.dim() == 3, "pages is not a tensor [B, max_pages, 4]")
+    _tensor("pages", pages, torch.int32, (b, int(pages.shape[1]), 4))
+    _tensor("seq_pages", seq_pages, torch.int32, (b,))
+    _tensor("out_o", out_o, torch.bfloat16, (b, n_q, g.n_heads, g.d_latent))
+    if out_lse is not None:
+        _tensor("out_lse", out_lse, torch.float32, (b, n_q, g.n_heads))
+    _need(workspace is not None, "workspace is None", 1)
+    _tensor("workspace", workspace, workspace.dtype)
+    _check(LIB.mla_cache_attend(ctypes.byref(g), b, n_q, _ptr(q), _ptr(pos), _ptr(pages), _ptr(seq_pages), int(pages.shape[1]),
+                                n_pages, int(page_rows), _ptr(cache), _ptr(out_o), _ptr(out_lse), _ptr(workspace),
+                                workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
 def probe_mfma_bf16(iters, sink, stream=None) -> float:
