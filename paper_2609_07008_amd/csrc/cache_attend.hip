@@ -30,22 +30,18 @@
 namespace mla {
 namespace {
 
-#define MLA_CONST __attribute__((address_space(4)))
-
 constexpr int kWaves = 8, kThreads = kWaves * 64;
 
-template <int NBQ>
+template <int NB>
 struct CaCfg {
-  static constexpr int BM = 32 * NBQ;        // head-rows of a workgroup
-  static constexpr int NB = 2 * NBQ;         // in blocks of 16
+  static constexpr int BM = 16 * NB;         // head-rows of a workgroup
   static constexpr int KBL = 8 * 1024 + 128; // latent of an 8-key block: a kilobyte per 64 dims
-  static constexpr int LAT = 8 * KBL;
-  static constexpr int KBR = 1024 + 128;     // RoPE keys of an 8-key block
-  static constexpr int ROPE_OFF = 2 * LAT;   // two latent buffers; RoPE keys are read before the next tile's arrive
-  static constexpr int P_OFF = ROPE_OFF + 8 * KBR;
-  static constexpr int QLO_OFF = P_OFF + 2 * NB * 1024;
-  static constexpr int EX_OFF = QLO_OFF + 2 * NB * 1024;   // [BM][4]: a value of each key wave
-  static constexpr int TH_OFF = EX_OFF + BM * 16;
+  static constexpr int LAT = 8 * KBL;        // a tile
+  static constexpr int P_OFF = 2 * LAT;      // weights of two tiles: 2 x NB KB each in the layout of the MFMA operand
+  static constexpr int P_BYTES = 2 * NB * 1024;
+  static constexpr int AL_OFF = P_OFF + 2 * P_BYTES;   // [2][BM]: factors of the sums before the tile
+  static constexpr int ML_OFF = AL_OFF + 2 * BM * 4;   // [BM][2]: reference and row sum at the end
+  static constexpr int TH_OFF = ML_OFF + BM * 8;
   static constexpr int LDS = TH_OFF + kMaxRopePairs * 8;
   static_assert(LDS <= 160 * 1024, "LDS of a compute unit");
 };
@@ -57,37 +53,58 @@ __device__ __forceinline__ int key_swz(int k) { return k ^ ((~k & 1) << 2); }
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 struct Tile {       // wave-uniform
-  int page, sub;    // page to read (0 where there is none), tile of the page
+  int page, off;    // page to read (0 where there is none), the tile's first row in it
   int rows;         // rows of the tile that hold keys, 0 .. 64
-  int frame;
-  int64_t pos0;     // request position of the tile's first row
+  int frame, pos0;  // RoPE frame, request position of the page's first row
 };
 
-__device__ __forceinline__ Tile tile_of(const CacheAttendArgs& a, const mla_page MLA_CONST* entries, int u, int tpp) {
-  const int e = u / tpp;
-  Tile t;
-  t.sub = u - e * tpp;
-  const mla_page MLA_CONST* en = entries + e;
-  const int rows = en->rows < a.page_rows ? en->rows : a.page_rows;
-  const bool there = (unsigned)en->page < (unsigned)a.cache_pages;
-  t.page = there ? en->page : 0;
-  const int left = (there ? rows : 0) - t.sub * kCacheTile;
-  t.rows = left < 0 ? 0 : left < kCacheTile ? left : kCacheTile;
-  t.frame = en->frame;
-  t.pos0 = (int64_t)en->req_pos + t.sub * kCacheTile;
-  return t;
-}
+// The tiles of a request from tile u on: entries are fetched one tile ahead.
+struct Cursor {
+  const mla_page* entries;
+  int e, sub, e_last, tpp, word;   // entry and tile of it to describe next; its words in lanes 0 .. 3
+  __device__ __forceinline__ void fetch() {
+    if (e <= e_last) word = ((const int32_t*)(entries + e))[threadIdx.x & 3];
+  }
+  __device__ __forceinline__ void open(const CacheAttendArgs& a, int b, int u0, int u1, int tiles_per_page) {
+    entries = a.pages + (int64_t)b * a.max_pages;
+    tpp = tiles_per_page;
+    e = u0 / tpp;
+    sub = u0 - e * tpp;
+    e_last = (u1 - 1) / tpp;
+    word = 0;
+    fetch();
+  }
+  __device__ __forceinline__ Tile next(const CacheAttendArgs& a) {
+    Tile t;
+    const int page = __builtin_amdgcn_readlane(word, 0), rows = __builtin_amdgcn_readlane(word, 1);
+    const bool there = (unsigned)page < (unsigned)a.cache_pages;
+    t.page = there ? page : 0;
+    t.off = sub * kCacheTile;
+    const int left = (there ? (rows < a.page_rows ? rows : a.page_rows) : 0) - t.off;
+    t.rows = left < 0 ? 0 : left < kCacheTile ? left : kCacheTile;
+    t.pos0 = __builtin_amdgcn_readlane(word, 2);
+    t.frame = __builtin_amdgcn_readlane(word, 3);
+    if (++sub == tpp) {
+      sub = 0;
+      ++e;
+    }
+    fetch();
+    return t;
+  }
+};
 
 // keys of the tile that a row at position t sees, 0 .. 64
 __device__ __forceinline__ int seen_keys(const Tile& x, int t) {
-  const int64_t d = (int64_t)t - x.pos0 + 1;
-  const int n = t < 0 || d < 0 ? 0 : d < x.rows ? (int)d : x.rows;
-  return n;
+  const int64_t d = (int64_t)t - x.pos0 - x.off + 1;
+  return t < 0 || d < 0 ? 0 : d < x.rows ? (int)d : x.rows;
 }
 
+// maximum / sum over the four lanes (l, l ^ 16, l ^ 32, l ^ 48) that hold a head-row's keys
 __device__ __forceinline__ float quad_max(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16, 64));
-  return fmaxf(v, __shfl_xor(v, 32, 64));
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
 }
 __device__ __forceinline__ float quad_sum(float v) {
   v += __shfl_xor(v, 16, 64);
@@ -100,16 +117,15 @@ __device__ __forceinline__ int tiles_of(const CacheAttendArgs& a, int b, int tpp
   return n * tpp;
 }
 
-template <int NBQ>
+template <int NB>
 __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendArgs a) {
-  using C = CaCfg<NBQ>;
-  constexpr int NB = C::NB, BM = C::BM;
+  using C = CaCfg<NB>;
+  constexpr int BM = C::BM;
   __shared__ __attribute__((aligned(16))) unsigned char lds[C::LDS];
   unsigned char MLA_LDS* L = (unsigned char MLA_LDS*)lds;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lg = lane >> 4, lc = lane & 15;
-  const int kb = wave & 3, hh = wave >> 2;
   const int tpp = a.page_rows / kCacheTile;
   const int R = a.n_q * a.n_heads;
 
@@ -168,45 +184,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendAr
   if (lo >= hi) return;
 
   double MLA_LDS* theta = (double MLA_LDS*)(L + C::TH_OFF);
-  float MLA_LDS* ex = (float MLA_LDS*)(L + C::EX_OFF);
-
-  // this lane's part of a tile's loads: row 8 wave + r of the tile, groups gq and gq + 8,
-  // RoPE chunk gq
-  const int r8 = lane & 7, gq = lane >> 3;
-  u32x4 cw[2], rp;
-  uint32_t sc[2];
-  auto load_tile = [&](const Tile& t) {
-    const unsigned char* p = a.cache + (int64_t)t.page * a.page_rows * kCacheRow;
-    const uint32_t row = (uint32_t)(t.sub * kCacheTile + wave * 8 + r8);
-    const unsigned char* ps = p + (uint32_t)a.page_rows * kCacheCodes;
-    const unsigned char* pr = ps + (uint32_t)a.page_rows * kCacheScales;
-    cw[0] = *(const u32x4*)(p + row * kCacheCodes + gq * 16);
-    cw[1] = *(const u32x4*)(p + row * kCacheCodes + gq * 16 + 128);
-    sc[0] = ps[row * kCacheScales + gq];
-    sc[1] = ps[row * kCacheScales + gq + 8];
-    rp = *(const u32x4*)(pr + row * kCacheRope + gq * 16);
-  };
-  auto store_tile = [&](int buf, int seen) {
-    const bool live = wave * 8 + r8 < seen;
-    unsigned char MLA_LDS* d = L + buf + wave * C::KBL + r8 * 128;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int g = gq + 8 * h;
-      const float s = mx4_scale(live ? sc[h] : 127u);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *(bf16x8 MLA_LDS*)(d + (g >> 1) * 1024 + ((((g & 1) * 4 + i) ^ key_swz(r8)) * 16)) = mx4_values(live ? cw[h][i] : 0u, s);
-    }
-    *(u32x4 MLA_LDS*)(L + C::ROPE_OFF + wave * C::KBR + r8 * 128 + ((gq ^ key_swz(r8)) * 16)) = live ? rp : u32x4{0, 0, 0, 0};
-  };
-
-  // K fragments (A operand, 16 keys x 32 dims) and V^T fragments (16 dims x 32 keys)
-  const int ksw = (lg ^ key_swz(lc & 7)) * 16;
-  const int kat = (kb * 2 + (lc >> 3)) * C::KBL + (lc & 7) * 128 + ksw;
-  const int rat = C::ROPE_OFF + (kb * 2 + (lc >> 3)) * C::KBR + (lc & 7) * 128 + ksw;
-  const int vkey = (lg & 1) * 4 + (lc >> 2), vcb = lc & 3;
-  const int vat = (lg >> 1) * C::KBL + vkey * 128 + (((vcb >> 1) ^ key_swz(vkey)) * 16) + (vcb & 1) * 8 + wave * 1024;
-
+  float MLA_LDS* ml = (float MLA_LDS*)(L + C::ML_OFF);
+  const uint32_t plane_s = (uint32_t)a.page_rows * kCacheCodes, plane_r = plane_s + (uint32_t)a.page_rows * kCacheScales;
   if (tid < kMaxRopePairs) theta[tid] = a.rope.theta[tid];
 
   int b = first_b, base = first_base;
@@ -216,216 +195,284 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendAr
     const int seq_base = base;
     base += n;
     if (u0 >= u1) continue;
-    const mla_page MLA_CONST* entries = (const mla_page MLA_CONST*)(uintptr_t)(a.pages + (int64_t)b * a.max_pages);
-
-    // the head-rows: block row i is head-row hb BM + i of the request; rows past the end
-    // repeat the last one and are not stored
-    const uint16_t* qrow[NBQ];
-    int tq[NBQ];
-    int t_max = INT32_MIN, t_min = INT32_MAX;
-#pragma unroll
-    for (int nb = 0; nb < NBQ; ++nb) {
-      int hr = hb * BM + (hh * NBQ + nb) * 16 + lc;
-      hr = hr < R ? hr : R - 1;
-      tq[nb] = a.pos[(int64_t)b * a.n_q + hr / a.n_heads];
-      qrow[nb] = a.q + ((int64_t)b * R + hr) * 576;
-    }
-    {
-      const int last = (hb + 1) * BM < R ? (hb + 1) * BM : R;
-      for (int j = hb * BM / a.n_heads; j <= (last - 1) / a.n_heads; ++j) {
-        const int t = __builtin_amdgcn_readfirstlane(a.pos[(int64_t)b * a.n_q + j]);
-        t_max = t > t_max ? t : t_max;
-        t_min = t < t_min ? t : t_min;
+    Cursor cur;
+    cur.open(a, b, u0, u1, tpp);
+    const int32_t* tseq = a.pos + (int64_t)b * a.n_q;
+    lds_barrier();   // the tables, and what the previous request left in LDS, are read
+    if (wave < 4) {
+      // ------------------------------------------------------------------ score wave
+      // Head-row lc of block `wave`; rows past the end repeat the last one and are not stored.
+      if (wave >= NB) {
+        lds_barrier();
+        for (int u = u0; u <= u1; ++u) lds_barrier();
+        continue;
       }
-    }
-    Tile cur = tile_of(a, entries, u0, tpp);
-    load_tile(cur);
-    bf16x8 qf[16][NBQ], qr[2][NBQ];
+      int hr = hb * BM + wave * 16 + lc;
+      hr = hr < R ? hr : R - 1;
+      const int t_row = tseq[hr / a.n_heads];
+      const uint16_t* qrow = a.q + ((int64_t)b * R + hr) * 576;
+      bf16x8 qf[16], qraw[2], qh[2], ql[2];   // Q fragments (B operand): dims ks*32 + lg*8 .. +7 of the head-row
 #pragma unroll
-    for (int nb = 0; nb < NBQ; ++nb)
+      for (int ks = 0; ks < 2; ++ks) qraw[ks] = *(const bf16x8*)(qrow + 512 + ks * 32 + lg * 8);
 #pragma unroll
-      for (int ks = 0; ks < 16; ++ks) qf[ks][nb] = *(const bf16x8*)(qrow[nb] + ks * 32 + lg * 8);
-    // the query's RoPE part in the page's frame: rounded in registers, the rest in LDS
-    auto relocate = [&](int frame) {
-#pragma unroll
-      for (int nb = 0; nb < NBQ; ++nb) {
-        const bf16x8 x1 = *(const bf16x8*)(qrow[nb] + 512 + lg * 8);
-        const bf16x8 x2 = *(const bf16x8*)(qrow[nb] + 544 + lg * 8);
-        const double dd = (double)((int64_t)tq[nb] - frame);
-        bf16x8 l1, l2;
+      for (int ks = 0; ks < 16; ++ks) qf[ks] = *(const bf16x8*)(qrow + ks * 32 + lg * 8);
+      // the RoPE part in a page's frame: the bf16 value and the bf16 of what it lost
+      auto relocate = [&](int frame) {
+        const double dd = (double)((int64_t)t_row - frame);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const double rev = dd * theta[lg * 8 + i];
           const float r = (float)(rev - rint(rev));
           const float sn = __builtin_amdgcn_sinf(r), cn = __builtin_amdgcn_cosf(r);
-          const float y1 = (float)x1[i] * cn - (float)x2[i] * sn, y2 = (float)x1[i] * sn + (float)x2[i] * cn;
-          qr[0][nb][i] = (__bf16)y1;
-          qr[1][nb][i] = (__bf16)y2;
-          l1[i] = (__bf16)(y1 - (float)qr[0][nb][i]);
-          l2[i] = (__bf16)(y2 - (float)qr[1][nb][i]);
+          const float f1 = (float)qraw[0][i], f2 = (float)qraw[1][i];
+          const float y1 = f1 * cn - f2 * sn, y2 = f1 * sn + f2 * cn;
+          qh[0][i] = (__bf16)y1;
+          qh[1][i] = (__bf16)y2;
+          ql[0][i] = (__bf16)(y1 - (float)qh[0][i]);
+          ql[1][i] = (__bf16)(y2 - (float)qh[1][i]);
         }
-        if (kb == 0) {
-          unsigned char MLA_LDS* p = L + C::QLO_OFF + (hh * NBQ + nb) * 2048 + lane * 16;
-          *(bf16x8 MLA_LDS*)p = l1;
-          *(bf16x8 MLA_LDS*)(p + 1024) = l2;
+      };
+      // RoPE keys as K fragments: key kb*16 + lc, chunks lg and lg + 4
+      bf16x8 kr[4][2];
+      auto load_rope = [&](const Tile& t) {
+        const unsigned char* p = a.cache + (int64_t)t.page * a.page_rows * kCacheRow + plane_r;
+        const uint32_t at = (uint32_t)(t.off + lc) * kCacheRope + (uint32_t)lg * 16;
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) {
+          kr[kb][0] = *(const bf16x8*)(p + at + kb * 16 * kCacheRope);
+          kr[kb][1] = *(const bf16x8*)(p + at + kb * 16 * kCacheRope + 64);
         }
-      }
-    };
-    lds_barrier();   // the tables and what the previous request left in LDS are read
-    relocate(cur.frame);
-    store_tile(0, seen_keys(cur, t_max));
-    Tile nxt = cur;
-    if (u0 + 1 < u1) {
-      nxt = tile_of(a, entries, u0 + 1, tpp);
-      load_tile(nxt);
-    }
-    f32x4 o[4][NB];
-    float m_run[NB], l_run[NBQ];
+      };
+      // K fragments (A operand, 16 keys x 32 dims): key kb*16 + lc, chunk 4 ks + lg
+      const int kat = (lc >> 3) * C::KBL + (lc & 7) * 128 + ((lg ^ key_swz(lc & 7)) * 16);
+      Tile t = cur.next(a);
+      load_rope(t);
+      relocate(t.frame);
+      float m_run = -INFINITY, l_run = 0.f;
+      int buf = 0, pb = 0;
+      lds_barrier();   // tiles 0 and 1 are stored
+      __builtin_amdgcn_s_setprio(1);
+      for (int u = u0; u < u1; ++u) {
+        f32x4 s[4];
+        const int k0 = buf + kat, k1 = k0 ^ 64;
+        auto kfrag = [&](int f) -> bf16x8 {   // f = ks * 4 + kb
+          const int ks = f >> 2, kb = f & 3;
+          return *(const bf16x8 MLA_LDS*)(L + (ks & 1 ? k1 : k0) + (ks >> 1) * 1024 + kb * 2 * C::KBL);
+        };
+        constexpr int KD = 6;   // fragments in the ring, one of them in use
+        bf16x8 ka[KD];
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
+        for (int j = 0; j < KD - 1; ++j) ka[j] = kfrag(j);
+        __builtin_amdgcn_sched_barrier(0);
+        // the RoPE steps while the first latent fragments arrive
 #pragma unroll
-      for (int h = 0; h < NB; ++h) o[d][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int kb = 0; kb < 4; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kr[kb][0], ql[0], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
-    for (int h = 0; h < NB; ++h) m_run[h] = -INFINITY;
+        for (int kb = 0; kb < 4; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kr[kb][1], ql[1], s[kb], 0, 0, 0);
 #pragma unroll
-    for (int nb = 0; nb < NBQ; ++nb) l_run[nb] = 0.f;
-    lds_barrier();
-
-    int buf = 0;
-    for (int u = u0; u < u1; ++u) {
-      Tile nn = nxt;
-      if (u + 2 < u1) nn = tile_of(a, entries, u + 2, tpp);
-      // ---- scores
-      f32x4 s[NBQ];
+        for (int kb = 0; kb < 4; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kr[kb][0], qh[0], s[kb], 0, 0, 0);
 #pragma unroll
-      for (int nb = 0; nb < NBQ; ++nb) s[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int ks = 0; ks < 16; ++ks) {
-        const bf16x8 k = *(const bf16x8 MLA_LDS*)(L + ((buf + kat) ^ ((ks & 1) * 64)) + (ks >> 1) * 1024);
-#pragma unroll
-        for (int nb = 0; nb < NBQ; ++nb) s[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qf[ks][nb], s[nb], 0, 0, 0);
-      }
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        const bf16x8 k = *(const bf16x8 MLA_LDS*)(L + (rat ^ (ks * 64)));
-#pragma unroll
-        for (int nb = 0; nb < NBQ; ++nb) {
-          const bf16x8 ql = *(const bf16x8 MLA_LDS*)(L + C::QLO_OFF + (hh * NBQ + nb) * 2048 + ks * 1024 + lane * 16);
-          s[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, ql, s[nb], 0, 0, 0);
-          s[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qr[ks][nb], s[nb], 0, 0, 0);
+        for (int kb = 0; kb < 4; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kr[kb][1], qh[1], s[kb], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        const Tile now = t;
+        if (u + 1 < u1) {
+          t = cur.next(a);
+          load_rope(t);
         }
-      }
-      // register i of s[nb]: key kb*16 + lg*4 + i, head-row lc of the block
-      if (seen_keys(cur, t_min) < kCacheTile) {
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int nb = 0; nb < NBQ; ++nb) {
-          const int rel = seen_keys(cur, tq[nb]) - (kb * 16 + lg * 4);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (i >= rel) s[nb][i] = -INFINITY;
+        for (int f = 0; f < 64; ++f) {
+          if (f + KD - 1 < 64) ka[(f + KD - 1) % KD] = kfrag(f + KD - 1);
+          __builtin_amdgcn_sched_barrier(0);
+          s[f & 3] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[f % KD], qf[f >> 2], s[f & 3], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
         }
-      }
+        // register i of s[kb]: key kb*16 + lg*4 + i, head-row lc
+        const int rel = seen_keys(now, t_row) - lg * 4;
+        if (__builtin_amdgcn_ballot_w64(rel + lg * 4 < kCacheTile) != 0) {
 #pragma unroll
-      for (int nb = 0; nb < NBQ; ++nb) {
-        const float m = quad_max(fmaxf(fmaxf(s[nb][0], s[nb][1]), fmaxf(s[nb][2], s[nb][3]))) * a.scale_log2;
-        if (lg == 0) ex[((hh * NBQ + nb) * 16 + lc) * 4 + kb] = m;
+          for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (kb * 16 + i >= rel) s[kb][i] = -INFINITY;
+        }
+        float m = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
+#pragma unroll
+        for (int kb = 1; kb < 4; ++kb) m = fmaxf(m, fmaxf(fmaxf(s[kb][0], s[kb][1]), fmaxf(s[kb][2], s[kb][3])));
+        m = quad_max(m) * a.scale_log2;
+        float al = 1.f;
+        if ((m > m_run + 8.f) | ((m_run == -INFINITY) & (m > -INFINITY))) {
+          al = __builtin_amdgcn_exp2f(m_run - m);
+          m_run = m;
+        }
+        const float ref = m_run == -INFINITY ? 0.f : m_run;   // nothing seen yet: every weight is 0
+        float w[4][4];
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], a.scale_log2, -ref));
+#pragma unroll
+        for (int k2 = 0; k2 < 2; ++k2)
+          *(u32x4 MLA_LDS*)(L + C::P_OFF + pb * C::P_BYTES + (k2 * NB + wave) * 1024 + lane * 16) =
+              u32x4{pack_bf16x2(w[2 * k2][0], w[2 * k2][1]), pack_bf16x2(w[2 * k2][2], w[2 * k2][3]),
+                    pack_bf16x2(w[2 * k2 + 1][0], w[2 * k2 + 1][1]), pack_bf16x2(w[2 * k2 + 1][2], w[2 * k2 + 1][3])};
+        if (lg == 0) *(float MLA_LDS*)(L + C::AL_OFF + (pb * BM + wave * 16 + lc) * 4) = al;
+        float l = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < 4; ++kb) l += (w[kb][0] + w[kb][1]) + (w[kb][2] + w[kb][3]);
+        l_run = l_run * al + l;
+        if (t.frame != now.frame) relocate(t.frame);
+        buf ^= C::LAT;
+        pb ^= 1;
+        lds_barrier();   // step u - u0 of the score waves
+      }
+      __builtin_amdgcn_s_setprio(0);
+      const float l = quad_sum(l_run);
+      if (lg == 0) {
+        ml[(wave * 16 + lc) * 2] = m_run;
+        ml[(wave * 16 + lc) * 2 + 1] = l;
       }
       lds_barrier();
-      // ---- reference, weights
-      bool moves = false;
-      float m_new[NB];
-#pragma unroll
-      for (int h = 0; h < NB; ++h) {
-        const f32x4 v = *(const f32x4 MLA_LDS*)(ex + (h * 16 + lc) * 4);
-        const float m = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
-        const bool up = m > m_run[h] + 8.f || (m_run[h] == -INFINITY && m > -INFINITY);
-        m_new[h] = up ? m : m_run[h];
-        moves |= up;
-      }
-      if (__builtin_amdgcn_ballot_w64(moves) != 0) {
-#pragma unroll
-        for (int h = 0; h < NB; ++h) {
-          const float al = m_new[h] == m_run[h] ? 1.f : __builtin_amdgcn_exp2f(m_run[h] - m_new[h]);
-          m_run[h] = m_new[h];
-#pragma unroll
-          for (int d = 0; d < 4; ++d) o[d][h] *= al;
-#pragma unroll
-          for (int nb = 0; nb < NBQ; ++nb)
-            if (h == hh * NBQ + nb) l_run[nb] *= al;
+    } else {
+      // ------------------------------------------------------------------ value wave
+      // Dims 128 w .. +127 of every head-row; it also converts its dims of the tiles: once
+      // it has read them as the value of tile u, tile u + 2 may take their place, since the
+      // score waves took tile u in the step before.
+      const int w = wave - 4;
+      int t_max = INT32_MIN;
+      {
+        const int last = (hb + 1) * BM < R ? (hb + 1) * BM : R;
+        for (int j = hb * BM / a.n_heads; j <= (last - 1) / a.n_heads; ++j) {
+          const int t = __builtin_amdgcn_readfirstlane(tseq[j]);
+          t_max = t > t_max ? t : t_max;
         }
       }
-#pragma unroll
-      for (int nb = 0; nb < NBQ; ++nb) {
-        float m = hh ? m_run[NBQ + nb] : m_run[nb];
-        m = m == -INFINITY ? 0.f : m;   // nothing seen yet: every weight is 0
-        float w[4];
+      // codes of 16 i + lane / 4, group 4 w + lane % 4
+      const int key = lane >> 2, grp = lane & 3;
+      u32x4 cw[4];
+      uint32_t sc[4];
+      auto load_codes = [&](const Tile& t) {
+        const unsigned char* p = a.cache + (int64_t)t.page * a.page_rows * kCacheRow;
+        const uint32_t row = (uint32_t)(t.off + key), g = (uint32_t)(4 * w + grp);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nb][i], a.scale_log2, -m));
-          l_run[nb] += w[i];
+          cw[i] = *(const u32x4*)(p + row * kCacheCodes + g * 16 + i * 16 * kCacheCodes);
+          sc[i] = (p + plane_s)[row * kCacheScales + g + i * 16 * kCacheScales];
         }
-        *(u32x2 MLA_LDS*)(L + C::P_OFF + ((kb >> 1) * NB + hh * NBQ + nb) * 1024 + lane * 16 + (kb & 1) * 8) =
-            u32x2{pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3])};
+      };
+      const int sat = (key >> 3) * C::KBL + (key & 7) * 128 + (2 * w + (grp >> 1)) * 1024 +
+                      (((grp & 1) * 4) ^ (grp >> 1) ^ key_swz(key & 7)) * 16;
+      auto store_tile = [&](int buf, int seen) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (seen < kCacheTile && i * 16 + key >= seen) {   // a key that no row sees: zeros
+            cw[i] = u32x4{0, 0, 0, 0};
+            sc[i] = 127;
+          }
+          const float s = mx4_scale(sc[i]);
+          // the four chunks of a group; lanes of the upper groups take neighbours swapped, so
+          // that a store meets all banks
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t c = grp >> 1 ? cw[i][j ^ 1] : cw[i][j];
+            *(bf16x8 MLA_LDS*)(L + ((buf + sat) ^ (j * 16)) + i * 2 * C::KBL) = mx4_values(c, s);
+          }
+        }
+      };
+      Tile t = cur.next(a);
+      load_codes(t);
+      store_tile(0, seen_keys(t, t_max));
+      if (u0 + 1 < u1) {
+        t = cur.next(a);
+        load_codes(t);
+        store_tile(C::LAT, seen_keys(t, t_max));
       }
-      // ---- the next tile into the other buffer, the one after it on its way
-      if (u + 1 < u1) {
-        store_tile(buf ^ C::LAT, seen_keys(nxt, t_max));
-        if (nxt.frame != cur.frame) relocate(nxt.frame);
-        if (u + 2 < u1) load_tile(nn);
+      if (u0 + 2 < u1) {
+        t = cur.next(a);
+        load_codes(t);
       }
-      lds_barrier();
-      // ---- values
+      f32x4 o[8][NB];
 #pragma unroll
-      for (int k2 = 0; k2 < 2; ++k2) {
-        bf16x8 p[NB];
+      for (int d = 0; d < 8; ++d)
 #pragma unroll
-        for (int h = 0; h < NB; ++h) p[h] = *(const bf16x8 MLA_LDS*)(L + C::P_OFF + (k2 * NB + h) * 1024 + lane * 16);
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          const unsigned char MLA_LDS* vp = L + ((buf + vat) ^ (d * 32)) + k2 * 4 * C::KBL;
+        for (int h = 0; h < NB; ++h) o[d][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+      // V^T fragments (A operand, 16 dims x 32 keys) by transposing reads (see attend_pair.hip)
+      const int vkey = (lg & 1) * 4 + (lc >> 2), vcb = lc & 3;
+      const int vat = (lg >> 1) * C::KBL + vkey * 128 + (((vcb >> 1) ^ key_swz(vkey)) * 16) + (vcb & 1) * 8 + w * 2048;
+      int buf = 0, pb = 0;
+      lds_barrier();   // tiles 0 and 1 are stored
+      lds_barrier();   // the weights of tile 0 are written
+      for (int u = u0; u < u1; ++u) {
+        auto vfrag = [&](int f) -> bf16x8 {   // f = k2 * 8 + d
+          const unsigned char MLA_LDS* vp = L + ((buf + vat) ^ ((f & 3) * 32)) + ((f >> 2) & 1) * 1024 + (f >> 3) * 4 * C::KBL;
           const bf16x4 vl = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((MLA_LDS bf16x4*)vp);
           const bf16x4 vh = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((MLA_LDS bf16x4*)(vp + 2 * C::KBL));
-          const bf16x8 v = __builtin_shufflevector(vl, vh, 0, 1, 2, 3, 4, 5, 6, 7);
+          return __builtin_shufflevector(vl, vh, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        constexpr int VD = 3;
+        bf16x8 vt[VD], p[2][NB];
+        float al[NB];
 #pragma unroll
-          for (int h = 0; h < NB; ++h) o[d][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[h], o[d][h], 0, 0, 0);
+        for (int h = 0; h < NB; ++h) al[h] = *(const float MLA_LDS*)(L + C::AL_OFF + (pb * BM + h * 16 + lc) * 4);
+#pragma unroll
+        for (int h = 0; h < NB; ++h) p[0][h] = *(const bf16x8 MLA_LDS*)(L + C::P_OFF + pb * C::P_BYTES + h * 1024 + lane * 16);
+#pragma unroll
+        for (int j = 0; j < VD - 1; ++j) vt[j] = vfrag(j);
+#pragma unroll
+        for (int h = 0; h < NB; ++h) p[1][h] = *(const bf16x8 MLA_LDS*)(L + C::P_OFF + pb * C::P_BYTES + (NB + h) * 1024 + lane * 16);
+        bool moved = false;
+#pragma unroll
+        for (int h = 0; h < NB; ++h) moved |= al[h] != 1.f;
+        if (__builtin_amdgcn_ballot_w64(moved) != 0) {
+#pragma unroll
+          for (int h = 0; h < NB; ++h)
+#pragma unroll
+            for (int d = 0; d < 8; ++d) o[d][h] *= al[h];
         }
+#pragma unroll
+        for (int f = 0; f < 16; ++f) {
+          if (f + VD - 1 < 16) vt[(f + VD - 1) % VD] = vfrag(f + VD - 1);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int h = 0; h < NB; ++h)
+            o[f & 7][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[f % VD], p[f >> 3][h], o[f & 7][h], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (u + 2 < u1) {
+          store_tile(buf, seen_keys(t, t_max));
+          if (u + 3 < u1) {
+            t = cur.next(a);
+            load_codes(t);
+          }
+        }
+        buf ^= C::LAT;
+        pb ^= 1;
+        lds_barrier();   // step u - u0 of the value waves; after the last one the sums are written
       }
-      cur = nxt;
-      nxt = nn;
-      buf ^= C::LAT;
-    }
-    // ---- row sums across lanes and key waves, then the rows
-    // (ex: every wave has read the last tile's maxima before the barrier above)
+      const bool whole = u0 == 0 && u1 == n;
+      const int slot = seq_base <= lo ? 2 * share : 2 * share + 1;
 #pragma unroll
-    for (int nb = 0; nb < NBQ; ++nb) {
-      const float l = quad_sum(l_run[nb]);
-      if (lg == 0) ex[((hh * NBQ + nb) * 16 + lc) * 4 + kb] = l;
-    }
-    lds_barrier();
-    const bool whole = u0 == 0 && u1 == n;
-    const int slot = seq_base <= lo ? 2 * share : 2 * share + 1;
+      for (int h = 0; h < NB; ++h) {
+        const float m = ml[(h * 16 + lc) * 2], l = ml[(h * 16 + lc) * 2 + 1];
+        const int row = hb * BM + h * 16 + lc;
+        if (row >= R) continue;
+        if (whole) {
+          const int64_t at = (int64_t)b * R + row;
+          const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-    for (int h = 0; h < NB; ++h) {
-      const f32x4 lv = *(const f32x4 MLA_LDS*)(ex + (h * 16 + lc) * 4);
-      const float l = lv[0] + lv[1] + lv[2] + lv[3];
-      const int row = hb * BM + h * 16 + lc;
-      if (row >= R) continue;
-      if (whole) {
-        const int64_t at = (int64_t)b * R + row;
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+          for (int d = 0; d < 8; ++d)
+            *(u32x2*)(a.out_o + at * 512 + w * 128 + d * 16 + lg * 4) =
+                u32x2{pack_bf16x2(o[d][h][0] * inv, o[d][h][1] * inv), pack_bf16x2(o[d][h][2] * inv, o[d][h][3] * inv)};
+          if (w == 0 && lg == 0 && a.out_lse != nullptr)
+            a.out_lse[at] = l == 0.f ? -INFINITY : (m + __log2f(l)) * 0.6931471805599453f;
+        } else {
+          const int64_t at = ((int64_t)slot * a.n_blocks + hb) * BM + h * 16 + lc;
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
-          *(u32x2*)(a.out_o + at * 512 + wave * 64 + d * 16 + lg * 4) =
-              u32x2{pack_bf16x2(o[d][h][0] * inv, o[d][h][1] * inv), pack_bf16x2(o[d][h][2] * inv, o[d][h][3] * inv)};
-        if (wave == 0 && lg == 0 && a.out_lse != nullptr)
-          a.out_lse[at] = l == 0.f ? -INFINITY : (m_run[h] + __log2f(l)) * 0.6931471805599453f;
-      } else {
-        const int64_t at = ((int64_t)slot * a.n_blocks + hb) * BM + h * 16 + lc;
-#pragma unroll
-        for (int d = 0; d < 4; ++d) *(f32x4*)(a.part_o + at * 512 + wave * 64 + d * 16 + lg * 4) = o[d][h];
-        if (wave == 0 && lg == 0) {
-          a.part_ml[at * 2] = m_run[h];
-          a.part_ml[at * 2 + 1] = l;
+          for (int d = 0; d < 8; ++d) *(f32x4*)(a.part_o + at * 512 + w * 128 + d * 16 + lg * 4) = o[d][h];
+          if (w == 0 && lg == 0) {
+            a.part_ml[at * 2] = m;
+            a.part_ml[at * 2 + 1] = l;
+          }
         }
       }
     }
@@ -492,10 +539,12 @@ __global__ __launch_bounds__(kThreads) void cache_merge_kernel(CacheAttendArgs a
 
 hipError_t launch_cache_attend(const CacheAttendArgs& a, hipStream_t s) {
   const unsigned grid = 8u * (unsigned)a.n_blocks * (unsigned)((a.shares + 7) / 8);
-  if (a.block == 32)
+  if (a.block == 16)
     cache_attend_kernel<1><<<dim3(grid), dim3(kThreads), 0, s>>>(a);
-  else
+  else if (a.block == 32)
     cache_attend_kernel<2><<<dim3(grid), dim3(kThreads), 0, s>>>(a);
+  else
+    cache_attend_kernel<4><<<dim3(grid), dim3(kThreads), 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   cache_merge_kernel<<<dim3((unsigned)(a.n_q * a.n_heads), (unsigned)a.n_seqs), dim3(kThreads), 0, s>>>(a);

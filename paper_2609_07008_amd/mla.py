@@ -332,48 +332,55 @@ def shared_wb(z, w_b, y, stream=None):
 CACHE_ROW_BYTES = 400   # a row of the paged 4-bit cache: 256 code bytes, 16 scales, 64 bf16
 
 
-def _need(ok: bool, what: str, status: int = 2):
-    if not ok:
-        raise MlaError(status, what)
+def _refuse(what: str, status: int = 2):
+    raise MlaError(status, what)
 
 
 def _tensor(name, t, dtype, shape=None, rows=False):
-    """t is a device tensor of dtype and, if given, shape; contiguous, or (rows) with
-    contiguous rows.  Empty tensors pass with any strides."""
-    _need(isinstance(t, torch.Tensor), f"{name} is not a tensor", 1)
-    _need(t.dtype == dtype, f"{name} is {t.dtype}, expected {dtype}")
-    _need(t.is_cuda and t.device.index == torch.cuda.current_device(), f"{name} is on {t.device}, not the current device")
-    if shape is not None:
-        _need(tuple(t.shape) == tuple(shape), f"{name} is {tuple(t.shape)}, expected {tuple(shape)}")
+    """t is a device tensor of dtype and, if given, shape (a tuple); contiguous, or (rows)
+    two-dimensional with contiguous rows."""
+    if not isinstance(t, torch.Tensor):
+        _refuse(f"{name} is not a tensor", 1)
+    if t.dtype != dtype:
+        _refuse(f"{name} is {t.dtype}, expected {dtype}")
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        _refuse(f"{name} is on {t.device}, not the current device")
+    if shape is not None and t.shape != shape:
+        _refuse(f"{name} is {tuple(t.shape)}, expected {shape}")
     if rows:
-        _need(t.dim() == 2 and (t.stride(1) == 1 or t.numel() == 0), f"{name} has strides {t.stride()}")
-    else:
-        _need(t.is_contiguous(), f"{name} is not contiguous")
+        if t.dim() != 2 or (t.stride(1) != 1 and t.numel() != 0):
+            _refuse(f"{name} is {tuple(t.shape)} with strides {t.stride()}")
+    elif not t.is_contiguous():
+        _refuse(f"{name} is not contiguous")
 
 
 def _row_stride(t) -> int:
     """Elements between rows; of a single row (whose stride is arbitrary) its width rounded up."""
-    return int(t.stride(0)) if t.shape[0] > 1 else -(-int(t.shape[1]) // 8) * 8
+    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 8) * 8
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
 
 
 def mx4_quantize(x, codes, scales, stream=None):
     """bf16 rows into the 4-bit format (mla_mx4_quantize): x [N, C] bfloat16 with
     contiguous rows, codes [N, C/2] and scales [N, C/32] uint8, written."""
     _tensor("x", x, torch.bfloat16, rows=True)
-    n, c = int(x.shape[0]), int(x.shape[1])
+    n, c = x.shape
     _tensor("codes", codes, torch.uint8, (n, c // 2))
     _tensor("scales", scales, torch.uint8, (n, c // 32))
-    _check(LIB.mla_mx4_quantize(n, c, _ptr(x), _row_stride(x), _ptr(codes), _ptr(scales), _stream(stream)))
+    _check(LIB.mla_mx4_quantize(n, c, _addr(x), _row_stride(x), _addr(codes), _addr(scales), _stream(stream)))
 
 
 def mx4_dequantize(codes, scales, x, stream=None):
-    """The values of codes [N, C/2] and scales [N, C/32] into x [N, C] bfloat16
-    (mla_mx4_dequantize)."""
+    """The values of codes [N, C/2] and scales [N, C/32] into x [N, C] bfloat16 with
+    contiguous rows (mla_mx4_dequantize)."""
     _tensor("x", x, torch.bfloat16, rows=True)
-    n, c = int(x.shape[0]), int(x.shape[1])
+    n, c = x.shape
     _tensor("codes", codes, torch.uint8, (n, c // 2))
     _tensor("scales", scales, torch.uint8, (n, c // 32))
-    _check(LIB.mla_mx4_dequantize(n, c, _ptr(codes), _ptr(scales), _ptr(x), _row_stride(x), _stream(stream)))
+    _check(LIB.mla_mx4_dequantize(n, c, _addr(codes), _addr(scales), _addr(x), _row_stride(x), _stream(stream)))
 
 
 def shared_wb_mx4(z, w_codes, w_scales, y, stream=None):
@@ -381,24 +388,24 @@ def shared_wb_mx4(z, w_codes, w_scales, y, stream=None):
     w_codes [d_out, d_in/2] and w_scales [d_out, d_in/32] uint8, y [N, d_out] float32
     or bfloat16."""
     _tensor("z", z, torch.bfloat16)
-    _need(z.dim() == 2, f"z is {tuple(z.shape)}")
-    n, d_in = int(z.shape[0]), int(z.shape[1])
     _tensor("w_codes", w_codes, torch.uint8)
-    _need(w_codes.dim() == 2 and int(w_codes.shape[1]) * 2 == d_in, f"w_codes is {tuple(w_codes.shape)}, z {tuple(z.shape)}")
-    d_out = int(w_codes.shape[0])
+    if z.dim() != 2 or w_codes.dim() != 2 or w_codes.shape[1] * 2 != z.shape[1]:
+        _refuse(f"z is {tuple(z.shape)}, w_codes {tuple(w_codes.shape)}")
+    n, d_in = z.shape
+    d_out = w_codes.shape[0]
     _tensor("w_scales", w_scales, torch.uint8, (d_out, d_in // 32))
-    _need(isinstance(y, torch.Tensor) and y.dtype in (torch.float32, torch.bfloat16), "y is not float32 or bfloat16")
-    _tensor("y", y, y.dtype, (n, d_out))
-    out = MLA_BF16 if y.dtype == torch.bfloat16 else MLA_F32
-    _check(LIB.mla_shared_wb_mx4(n, d_in, d_out, _ptr(z), _ptr(w_codes), _ptr(w_scales), out, _ptr(y), _stream(stream)))
+    bf16 = isinstance(y, torch.Tensor) and y.dtype == torch.bfloat16
+    _tensor("y", y, torch.bfloat16 if bf16 else torch.float32, (n, d_out))
+    _check(LIB.mla_shared_wb_mx4(n, d_in, d_out, _addr(z), _addr(w_codes), _addr(w_scales), MLA_BF16 if bf16 else MLA_F32,
+                                 _addr(y), _stream(stream)))
 
 
-def _cache_pages(cache, page_rows) -> int:
+def _cache_pages(cache, page_rows: int) -> int:
     """Pages of a cache tensor [pages, page_rows * CACHE_ROW_BYTES] uint8."""
     _tensor("cache", cache, torch.uint8)
-    _need(cache.dim() == 2 and int(cache.shape[1]) == int(page_rows) * CACHE_ROW_BYTES,
-          f"cache is {tuple(cache.shape)}, expected [pages, {int(page_rows)} * {CACHE_ROW_BYTES}]")
-    return int(cache.shape[0])
+    if cache.dim() != 2 or cache.shape[1] != page_rows * CACHE_ROW_BYTES:
+        _refuse(f"cache is {tuple(cache.shape)}, expected [pages, {page_rows} * {CACHE_ROW_BYTES}]")
+    return cache.shape[0]
 
 
 def cache_append(geom, kv, slots, cache, page_rows: int, pos=None, stream=None):
@@ -408,25 +415,28 @@ def cache_append(geom, kv, slots, cache, page_rows: int, pos=None, stream=None):
     g = make_geom(geom)
     pages = _cache_pages(cache, page_rows)
     _tensor("kv", kv, torch.bfloat16, rows=True)
-    n = int(kv.shape[0])
-    _need(int(kv.shape[1]) == g.d_latent + g.d_rope, f"kv is {tuple(kv.shape)}")
+    n, d = kv.shape
+    if d != g.d_latent + g.d_rope:
+        _refuse(f"kv is {tuple(kv.shape)}, expected [N, {g.d_latent + g.d_rope}]")
     _tensor("slots", slots, torch.int32, (n,))
     if pos is not None:
         _tensor("pos", pos, torch.int32, (n,))
-    _check(LIB.mla_cache_append(ctypes.byref(g), n, _ptr(kv), _row_stride(kv), _ptr(pos), _ptr(slots), pages, int(page_rows),
-                                _ptr(cache), _stream(stream)))
+    _check(LIB.mla_cache_append(ctypes.byref(g), n, _addr(kv), _row_stride(kv), _addr(pos), _addr(slots), pages, page_rows,
+                                _addr(cache), _stream(stream)))
 
 
 def cache_gather(geom, slots, cache, page_rows: int, kv, stream=None):
-    """Rows slots [N] int32 of the cache into kv [N, d_latent + d_rope] bfloat16
-    (mla_cache_gather); rows whose slot is outside the cache are left as they were."""
+    """Rows slots [N] int32 of the cache into kv [N, d_latent + d_rope] bfloat16 with
+    contiguous rows (mla_cache_gather); rows whose slot is outside the cache are left as
+    they were."""
     g = make_geom(geom)
     pages = _cache_pages(cache, page_rows)
     _tensor("kv", kv, torch.bfloat16, rows=True)
-    n = int(kv.shape[0])
-    _need(int(kv.shape[1]) == g.d_latent + g.d_rope, f"kv is {tuple(kv.shape)}")
+    n, d = kv.shape
+    if d != g.d_latent + g.d_rope:
+        _refuse(f"kv is {tuple(kv.shape)}, expected [N, {g.d_latent + g.d_rope}]")
     _tensor("slots", slots, torch.int32, (n,))
-    _check(LIB.mla_cache_gather(ctypes.byref(g), n, _ptr(slots), pages, int(page_rows), _ptr(cache), _ptr(kv), _row_stride(kv),
+    _check(LIB.mla_cache_gather(ctypes.byref(g), n, _addr(slots), pages, page_rows, _addr(cache), _addr(kv), _row_stride(kv),
                                 _stream(stream)))
 
 
@@ -445,21 +455,22 @@ def cache_attend(geom, q, pos, pages, seq_pages, cache, page_rows: int, out_o, o
     bfloat16, out_lse [B, n_q, H] float32 or None."""
     g = make_geom(geom)
     n_pages = _cache_pages(cache, page_rows)
-    _need(isinstance(q, torch.Tensor) and q.dim() == 4, "q is not a tensor [B, n_q, H, D]")
-    b, n_q = int(q.shape[0]), int(q.shape[1])
-    _tensor("q", q, torch.bfloat16, (b, n_q, g.n_heads, g.d_latent + g.d_rope))
+    _tensor("q", q, torch.bfloat16)
+    _tensor("pages", pages, torch.int32)
+    if q.dim() != 4 or q.shape[2] != g.n_heads or q.shape[3] != g.d_latent + g.d_rope:
+        _refuse(f"q is {tuple(q.shape)}, expected [B, n_q, {g.n_heads}, {g.d_latent + g.d_rope}]")
+    b, n_q, heads, _ = q.shape
+    if pages.dim() != 3 or pages.shape[0] != b or pages.shape[2] != 4:
+        _refuse(f"pages is {tuple(pages.shape)}, expected [{b}, max_pages, 4]")
     _tensor("pos", pos, torch.int32, (b, n_q))
-    _need(isinstance(pages, torch.Tensor) and pages.dim() == 3, "pages is not a tensor [B, max_pages, 4]")
-    _tensor("pages", pages, torch.int32, (b, int(pages.shape[1]), 4))
     _tensor("seq_pages", seq_pages, torch.int32, (b,))
-    _tensor("out_o", out_o, torch.bfloat16, (b, n_q, g.n_heads, g.d_latent))
+    _tensor("out_o", out_o, torch.bfloat16, (b, n_q, heads, g.d_latent))
     if out_lse is not None:
-        _tensor("out_lse", out_lse, torch.float32, (b, n_q, g.n_heads))
-    _need(workspace is not None, "workspace is None", 1)
-    _tensor("workspace", workspace, workspace.dtype)
-    _check(LIB.mla_cache_attend(ctypes.byref(g), b, n_q, _ptr(q), _ptr(pos), _ptr(pages), _ptr(seq_pages), int(pages.shape[1]),
-                                n_pages, int(page_rows), _ptr(cache), _ptr(out_o), _ptr(out_lse), _ptr(workspace),
-                                workspace.numel() * workspace.element_size(), _stream(stream)))
+        _tensor("out_lse", out_lse, torch.float32, (b, n_q, heads))
+    _tensor("workspace", workspace, torch.uint8)
+    _check(LIB.mla_cache_attend(ctypes.byref(g), b, n_q, _addr(q), _addr(pos), _addr(pages), _addr(seq_pages), pages.shape[1],
+                                n_pages, page_rows, _addr(cache), _addr(out_o), _addr(out_lse), _addr(workspace),
+                                workspace.numel(), _stream(stream)))
 
 
 def probe_mfma_bf16(iters, sink, stream=None) -> float:
