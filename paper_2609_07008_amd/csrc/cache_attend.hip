@@ -117,6 +117,17 @@ __device__ __forceinline__ int tiles_of(const CacheAttendArgs& a, int b, int tpp
   return n * tpp;
 }
 
+// The batch's tiles as `shares` runs in order: the first r of them a tile longer.
+struct Runs {
+  int q, r;
+  __device__ __forceinline__ Runs(int total, int shares) : q(total / shares), r(total - total / shares * shares) {}
+  __device__ __forceinline__ int first(int s) const { return q * s + (s < r ? s : r); }   // share s's first tile
+  __device__ __forceinline__ int share(int tile) const {                                  // the share that holds it
+    const int longer = r * (q + 1);
+    return tile < longer ? tile / (q + 1) : r + (tile - longer) / q;
+  }
+};
+
 template <int NB>
 __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendArgs a) {
   using C = CaCfg<NB>;
@@ -162,7 +173,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendAr
       total += v;
     }
     int base = before + inc - mine;
-    const int lo = (int)((int64_t)total * share / a.shares);
+    const int lo = Runs(total, a.shares).first(share);
     const bool writes = blockIdx.x == 0;
     for (int b = b0; b < b1; ++b) {
       const int n = tiles_of(a, b, tpp);
@@ -179,8 +190,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendAr
     first_base = __builtin_amdgcn_readfirstlane(sums[17]);
     total = __builtin_amdgcn_readfirstlane(total);
   }
-  const int lo = (int)((int64_t)total * share / a.shares);
-  const int hi = (int)((int64_t)total * (share + 1) / a.shares);
+  const Runs runs(total, a.shares);
+  const int lo = runs.first(share), hi = runs.first(share + 1);
   if (lo >= hi) return;
 
   double MLA_LDS* theta = (double MLA_LDS*)(L + C::TH_OFF);
@@ -480,59 +491,88 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendAr
 }
 
 // Joins the sums of requests that several shares hold (and writes those without a tile):
-// a workgroup takes a head-row, its waves the shares in turn, eight dims a lane.
+// G waves take a head-row, eight dims a lane, and its shares in turn.  Bound by the
+// latency of three dependent reads, then by the sums themselves (2 KB a share and head-row).
+template <int G>
 __global__ __launch_bounds__(kThreads) void cache_merge_kernel(CacheAttendArgs a) {
-  __shared__ __attribute__((aligned(16))) float acc[kWaves][512];
-  __shared__ float sums[kWaves];
+  __shared__ __attribute__((aligned(16))) float acc[G == 1 ? 1 : kWaves][512];
   const int R = a.n_q * a.n_heads;
-  const int b = blockIdx.y, row = blockIdx.x;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int b = blockIdx.y, row = blockIdx.x * (kWaves / G) + wave / G, sub = wave % G;
+  if (row >= R) return;   // whole workgroups where waves share a head-row
   const int base = a.tile_base[b], n = a.tile_base[b + 1] - base;
-  const int64_t total = a.tile_base[a.n_seqs];
   const int64_t at = (int64_t)b * R + row;
   if (n == 0) {
-    a.out_o[at * 512 + tid] = 0;
-    if (tid == 0 && a.out_lse != nullptr) a.out_lse[at] = -INFINITY;
+    if (sub != 0) return;
+    *(u32x4*)(a.out_o + at * 512 + lane * 8) = u32x4{0, 0, 0, 0};
+    if (lane == 0 && a.out_lse != nullptr) a.out_lse[at] = -INFINITY;
     return;
   }
-  // the last share s with total s / shares <= tile
-  const int s0 = (int)((((int64_t)base + 1) * a.shares - 1) / total);
-  const int s1 = (int)((((int64_t)base + n) * a.shares - 1) / total);
+  const Runs runs(a.tile_base[a.n_seqs], a.shares);
+  const int s0 = runs.share(base), s1 = runs.share(base + n - 1);
   if (s0 == s1) return;
+  const int block = row / a.block, in_block = row - block * a.block;
+  // share s's sums: its first request's or, where another request ends in it, its last one's
+  const int first_slot = base <= runs.first(s0) ? 2 * s0 : 2 * s0 + 1;
   auto place = [&](int s) -> int64_t {
-    const int lo = (int)(total * s / a.shares);
-    const int slot = base <= lo ? 2 * s : 2 * s + 1;
-    return ((int64_t)slot * a.n_blocks + row / a.block) * a.block + row % a.block;
+    return ((int64_t)(s == s0 ? first_slot : 2 * s) * a.n_blocks + block) * a.block + in_block;
   };
+  constexpr int kAhead = 4;
+  f32x4 v[kAhead][2];
+  auto load = [&](int s) {   // shares s, s + G, ..: past the end the last one again, not used
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int at_s = s + j * G <= s1 ? s + j * G : s1;
+      const f32x4* src = (const f32x4*)(a.part_o + place(at_s) * 512 + lane * 8);
+      v[j][0] = src[0];
+      v[j][1] = src[1];
+    }
+  };
+  load(s0 + sub);
   float m = -INFINITY;
-  for (int s = s0 + lane; s <= s1; s += 64)
-    if (total * s / a.shares < total * (s + 1) / a.shares) m = fmaxf(m, a.part_ml[place(s) * 2]);
+  for (int s = s0 + lane; s <= s1; s += 64) m = fmaxf(m, a.part_ml[place(s) * 2]);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
   const float ref = m == -INFINITY ? 0.f : m;
   f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = {0.f, 0.f, 0.f, 0.f};
   float l = 0.f;
-  for (int s = s0 + wave; s <= s1; s += kWaves) {
-    if (total * s / a.shares >= total * (s + 1) / a.shares) continue;   // a share without tiles
-    const int64_t p = place(s);
-    const float w = __builtin_amdgcn_exp2f(a.part_ml[p * 2] - ref);
-    l += w * a.part_ml[p * 2 + 1];
-    const f32x4* src = (const f32x4*)(a.part_o + p * 512 + lane * 8);
-    x += src[0] * w;
-    y += src[1] * w;
-  }
-  *(f32x4*)&acc[wave][lane * 8] = x;
-  *(f32x4*)&acc[wave][lane * 8 + 4] = y;
-  if (lane == 0) sums[wave] = l;
-  __syncthreads();
-  float v = 0.f, lt = 0.f;
+  for (int c = s0; c <= s1; c += 64) {   // 64 shares: lane j holds the weight of share c + j
+    float w = 0.f;
+    if (c + lane <= s1) {
+      const float* ml = a.part_ml + place(c + lane) * 2;
+      w = __builtin_amdgcn_exp2f(ml[0] - ref);
+      l += w * ml[1];
+    }
+    for (int i = sub; i < 64 && c + i <= s1; i += kAhead * G) {
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    v += acc[w][tid];
-    lt += sums[w];
+      for (int j = 0; j < kAhead; ++j) {
+        if (c + i + j * G > s1) break;
+        const float wj = __shfl(w, i + j * G, 64);
+        x += v[j][0] * wj;
+        y += v[j][1] * wj;
+      }
+      if (c + i + kAhead * G <= s1) load(c + i + kAhead * G);
+    }
   }
-  a.out_o[at * 512 + tid] = __builtin_bit_cast(uint16_t, (__bf16)(lt == 0.f ? 0.f : v / lt));
-  if (tid == 0 && a.out_lse != nullptr) a.out_lse[at] = lt == 0.f ? -INFINITY : (ref + __log2f(lt)) * 0.6931471805599453f;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (sub == 0 && lane == 0 && a.out_lse != nullptr)
+    a.out_lse[at] = l == 0.f ? -INFINITY : (ref + __log2f(l)) * 0.6931471805599453f;
+  if constexpr (G == 1) {
+    *(u32x4*)(a.out_o + at * 512 + lane * 8) = u32x4{pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv),
+                                                     pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv)};
+  } else {
+    static_assert(G == 1 || G == kWaves, "a head-row's waves are a workgroup");
+    *(f32x4*)&acc[wave][lane * 8] = x;
+    *(f32x4*)&acc[wave][lane * 8 + 4] = y;
+    __syncthreads();
+    float o = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) o += acc[w][threadIdx.x];
+    a.out_o[at * 512 + threadIdx.x] = __builtin_bit_cast(uint16_t, (__bf16)(o * inv));
+  }
 }
 
 }  // namespace
@@ -547,7 +587,14 @@ hipError_t launch_cache_attend(const CacheAttendArgs& a, hipStream_t s) {
     cache_attend_kernel<4><<<dim3(grid), dim3(kThreads), 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  cache_merge_kernel<<<dim3((unsigned)(a.n_q * a.n_heads), (unsigned)a.n_seqs), dim3(kThreads), 0, s>>>(a);
+  const unsigned R = (unsigned)(a.n_q * a.n_heads), n_seqs = (unsigned)a.n_seqs;
+  // A wave a head-row where it can hold all its shares' sums in flight at once, else eight
+  // (64 requests of 16k keys, 4 shares each: 209 against 216 us for the whole call; 48
+  // requests of 6k, 5.3 shares: 47.7 against 47.0; one of 264k, 256 shares: 99 against 64)
+  if (a.shares <= 4 * a.n_seqs)
+    cache_merge_kernel<1><<<dim3((R + kWaves - 1) / kWaves, n_seqs), dim3(kThreads), 0, s>>>(a);
+  else
+    cache_merge_kernel<kWaves><<<dim3(R, n_seqs), dim3(kThreads), 0, s>>>(a);
   return hipGetLastError();
 }
 
