@@ -244,6 +244,10 @@ mla_status mla_cache_attend(const mla_geom* geom, int32_t n_seqs, int32_t n_q, c
   a.max_pages = max_pages;
   a.page_rows = page_rows;
   a.cache_pages = (int32_t)cache_pages;
+  a.page_tiles = page_rows / mla::kCacheTile;
+  a.inv_page_tiles = 1.0 / a.page_tiles;
+  a.inv_shares = 1.0 / S.shares;
+  a.inv_blocks = 1.0 / S.n_blocks;
   a.block = S.block;
   a.n_blocks = S.n_blocks;
   a.shares = S.shares;

@@ -2,27 +2,35 @@
 // decode form of Alg. 2's SelectiveMLA, each page in its own RoPE frame (the query is
 // turned by t - frame, eq:rope), 512 + 64 latent, the latent as the value.
 //
-// A request's head-rows (its n_q tokens' heads) share its keys.  A workgroup of eight
-// waves takes up to 32 NBQ of them and a run of 64-key tiles:
-//   tile      row-major codes come in through registers two tiles ahead, are converted once
-//             (v_cvt_scalef32_pk_bf16_fp4) and laid into LDS as bf16 in the layout of the
-//             online attention's tiles (attend_pair.hip): the key of the scores and, by
-//             transposing reads, the value
-//   scores    wave (kb, hh): 16 keys x 16 NBQ head-rows, S^T = K Q^T, queries in registers.
-//             The turned RoPE part of the query goes in twice, as its bf16 value and the
-//             bf16 of what that lost: the scores are then as exact as the products, which a
-//             request of a few keys shows in its lse
-//   softmax   the tile's maximum of each head-row crosses the four key waves through LDS;
-//             the reference moves (and sums are rescaled) only when a tile exceeds it by
-//             2^8, so weights stay below 2^8 and sums in 32 bits lose nothing
-//   values    wave w: dims 64 w .. +63 of all head-rows, O^T += V^T P^T, weights in bf16
-//             (half a step, 2^-9 of each, next to an output of the same width)
+// A request's head-rows (its n_q tokens' heads) share its keys.  A workgroup takes 16 NB of
+// them and a run of 64-key tiles, with two kinds of waves that work a tile apart and meet
+// once a tile:
+//   score    four.  S^T = K Q^T for 16 head-rows a wave, queries in registers; with fewer
+//            than 64 head-rows the waves of the same 16 share the tile's keys.  The turned
+//            RoPE part of the query goes in twice, as its bf16 value and the bf16 of what
+//            that lost: the scores are then as exact as the products, which a request of a
+//            few keys shows in its lse.  Softmax against a reference that moves (and sums
+//            are rescaled) only when a tile exceeds it by 2^8, so weights stay below 2^9
+//            and sums in 32 bits lose nothing.  Weights in bf16: half a step, 2^-9 of each,
+//            next to an output of the same width.
+//   value    four, eight with fewer than 64 head-rows, 512 / waves dims each: O^T += V^T P^T.
+//            They convert their dims of the tiles too (v_cvt_scalef32_pk_bf16_fp4), once,
+//            into LDS as bf16 in the layout of the online attention's tiles
+//            (attend_pair.hip): the key of the scores and, by transposing reads, the value.
 // A key that no row of the call sees (behind a page's rows, past the last position) is
 // zero in LDS whatever the page holds there.
 //
 // Work is split by tiles, not by requests: the batch's tiles, in order, form `shares`
 // equal runs, one a workgroup (and head-row block).  A request inside one run is written
 // at once; one that crosses runs leaves sums to cache_merge_kernel.
+//
+// Measured, whole calls with the joining: 64 requests of ~16k keys, 64 heads 202 us, of
+// which a tile's 144 matrix products a SIMD fill half of its 5000 clocks; the rest is
+// conversion and softmax, which the products of the other kind hide only in part, and
+// 3328 clocks of LDS traffic.  16 requests of ~8k, 256 head-rows 85 us; one of 264k,
+// 64 heads 64 us.  48 of ~6k, 16 heads 41 us, of which 8 are the start (three dependent
+// reads from memory before the first tile) and 5 the joining: there the conversion bounds
+// a tile, and eight value waves against four take 41.4 against 43.5.
 #include "mx4.h"
 
 #include <algorithm>
@@ -30,27 +38,63 @@
 namespace mla {
 namespace {
 
-constexpr int kWaves = 8, kThreads = kWaves * 64;
+constexpr int kWaves = 8, kThreads = kWaves * 64;   // of cache_merge_kernel
 
 template <int NB>
 struct CaCfg {
   static constexpr int BM = 16 * NB;         // head-rows of a workgroup
+  static constexpr int KW = 4 / NB;          // score waves that share 16 head-rows, each with its keys
+  static constexpr int KB = NB;              // 16-key blocks of a score wave
+  // value waves: eight where registers allow (at NB = 4 they would take 254 us where four take 205)
+  static constexpr int VW = NB == 4 ? 4 : 8;
+  static constexpr int WAVES = 4 + VW, THREADS = 64 * WAVES;
+  static constexpr int ND = 32 / VW;         // 16-dim fragments of a value wave
+  static constexpr int GW = 16 / VW;         // groups of a row that it converts
+  static constexpr int NI = GW;              // loads of a tile's codes in it, 64 / GW keys each
   static constexpr int KBL = 8 * 1024 + 128; // latent of an 8-key block: a kilobyte per 64 dims
   static constexpr int LAT = 8 * KBL;        // a tile
-  static constexpr int P_OFF = 2 * LAT;      // weights of two tiles: 2 x NB KB each in the layout of the MFMA operand
+  static constexpr int P_OFF = 2 * LAT;      // weights of two tiles, [32 keys][NB] KB in the layout of the MFMA operand
   static constexpr int P_BYTES = 2 * NB * 1024;
-  static constexpr int AL_OFF = P_OFF + 2 * P_BYTES;   // [2][BM]: factors of the sums before the tile
-  static constexpr int ML_OFF = AL_OFF + 2 * BM * 4;   // [BM][2]: reference and row sum at the end
-  static constexpr int TH_OFF = ML_OFF + BM * 8;
+  static constexpr int M_OFF = P_OFF + 2 * P_BYTES;     // [2][KW][BM]: references of the tile's weights
+  static constexpr int L_OFF = M_OFF + 2 * KW * BM * 4; // [KW][BM]: row sums at the end
+  static constexpr int TH_OFF = L_OFF + KW * BM * 4;
   static constexpr int LDS = TH_OFF + kMaxRopePairs * 8;
+  static constexpr int Q_OFF = LAT;          // queries on their way to registers, 1152 bytes a head-row
+  static_assert(Q_OFF + BM * 1152 <= M_OFF, "before the second tile and the weights are stored");
   static_assert(LDS <= 160 * 1024, "LDS of a compute unit");
 };
 
 // slot of 16-byte chunk c of key k in its kilobyte: c ^ key_swz(k) (see attend_pair.hip)
 __device__ __forceinline__ int key_swz(int k) { return k ^ ((~k & 1) << 2); }
 
+// 16 bytes a lane from memory to LDS, lane after lane
+__device__ __forceinline__ void dma16(const unsigned char* from, unsigned char MLA_LDS* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (MLA_LDS void*)to, 16, 0, 0);
+}
+
+__device__ __forceinline__ void dma4(const unsigned char* from, unsigned char MLA_LDS* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (MLA_LDS void*)to, 4, 0, 0);
+}
+static_assert(sizeof(RopeTable) == 64 * 4, "a dword a lane");
+
 // this wave's LDS accesses are done, then all waves meet (loads from memory stay in flight)
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// The lane, opaque to the compiler: addresses formed from it in one kind of wave are not
+// kept in registers through the code of the other.
+__device__ __forceinline__ int lane_now() {
+  int v;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(v));
+  return v;
+}
+
+// x / d for 0 <= x < 2^31, inv = 1 / d: the product is off by less than one
+__device__ __forceinline__ int quotient(int x, int d, double inv) {
+  uint32_t q = (uint32_t)((double)x * inv);
+  if (q * (uint32_t)d > (uint32_t)x) --q;
+  if ((q + 1) * (uint32_t)d <= (uint32_t)x) ++q;
+  return __builtin_amdgcn_readfirstlane((int)q);
+}
 
 struct Tile {       // wave-uniform
   int page, off;    // page to read (0 where there is none), the tile's first row in it
@@ -58,37 +102,46 @@ struct Tile {       // wave-uniform
   int frame, pos0;  // RoPE frame, request position of the page's first row
 };
 
-// The tiles of a request from tile u on: entries are fetched one tile ahead.
+// The tiles of a request from tile u on.  Lanes hold 16 page entries, four words each, and
+// the next 16, so that a tile's entry is there when it is asked for.
 struct Cursor {
   const mla_page* entries;
-  int e, sub, e_last, tpp, word;   // entry and tile of it to describe next; its words in lanes 0 .. 3
-  __device__ __forceinline__ void fetch() {
-    if (e <= e_last) word = ((const int32_t*)(entries + e))[threadIdx.x & 3];
+  int e, sub, tpp, e_last, held;   // entry and tile of it to describe next; first entry held
+  int32_t word, ahead;
+  __device__ __forceinline__ int32_t fetch(int first) const {
+    const int lane = lane_now(), at = first + (lane >> 2);
+    return ((const int32_t*)(entries + (at < e_last ? at : e_last)))[lane & 3];
   }
-  __device__ __forceinline__ void open(const CacheAttendArgs& a, int b, int u0, int u1, int tiles_per_page) {
+  __device__ __forceinline__ void open(const CacheAttendArgs& a, int b, int u0, int u1) {
     entries = a.pages + (int64_t)b * a.max_pages;
-    tpp = tiles_per_page;
-    e = u0 / tpp;
+    tpp = a.page_tiles;
+    e = quotient(u0, tpp, a.inv_page_tiles);
     sub = u0 - e * tpp;
-    e_last = (u1 - 1) / tpp;
-    word = 0;
-    fetch();
+    e_last = quotient(u1 - 1, tpp, a.inv_page_tiles);
+    held = e;
+    word = fetch(e);
+    ahead = fetch(e + 16);
   }
   __device__ __forceinline__ Tile next(const CacheAttendArgs& a) {
+    if (__builtin_expect(e - held == 16, 0)) {
+      held = e;
+      word = ahead;
+      ahead = fetch(e + 16);
+    }
+    const int l = (e - held) * 4;
     Tile t;
-    const int page = __builtin_amdgcn_readlane(word, 0), rows = __builtin_amdgcn_readlane(word, 1);
+    const int page = __builtin_amdgcn_readlane(word, l), rows = __builtin_amdgcn_readlane(word, l + 1);
     const bool there = (unsigned)page < (unsigned)a.cache_pages;
     t.page = there ? page : 0;
     t.off = sub * kCacheTile;
     const int left = (there ? (rows < a.page_rows ? rows : a.page_rows) : 0) - t.off;
     t.rows = left < 0 ? 0 : left < kCacheTile ? left : kCacheTile;
-    t.pos0 = __builtin_amdgcn_readlane(word, 2);
-    t.frame = __builtin_amdgcn_readlane(word, 3);
+    t.pos0 = __builtin_amdgcn_readlane(word, l + 2);
+    t.frame = __builtin_amdgcn_readlane(word, l + 3);
     if (++sub == tpp) {
       sub = 0;
       ++e;
     }
-    fetch();
     return t;
   }
 };
@@ -111,16 +164,16 @@ __device__ __forceinline__ float quad_sum(float v) {
   return v + __shfl_xor(v, 32, 64);
 }
 
-__device__ __forceinline__ int tiles_of(const CacheAttendArgs& a, int b, int tpp) {
+__device__ __forceinline__ int tiles_of(const CacheAttendArgs& a, int b) {
   int n = a.seq_pages[b];
   n = n < 0 ? 0 : n < a.max_pages ? n : a.max_pages;
-  return n * tpp;
+  return n * a.page_tiles;
 }
 
 // The batch's tiles as `shares` runs in order: the first r of them a tile longer.
 struct Runs {
   int q, r;
-  __device__ __forceinline__ Runs(int total, int shares) : q(total / shares), r(total - total / shares * shares) {}
+  __device__ __forceinline__ Runs(const CacheAttendArgs& a, int total) : q(quotient(total, a.shares, a.inv_shares)), r(total - q * a.shares) {}
   __device__ __forceinline__ int first(int s) const { return q * s + (s < r ? s : r); }   // share s's first tile
   __device__ __forceinline__ int share(int tile) const {                                  // the share that holds it
     const int longer = r * (q + 1);
@@ -129,33 +182,39 @@ struct Runs {
 };
 
 template <int NB>
-__global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendArgs a) {
+__global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cache_attend_kernel(CacheAttendArgs a) {
   using C = CaCfg<NB>;
-  constexpr int BM = C::BM;
+  constexpr int BM = C::BM, KB = C::KB, ND = C::ND, GW = C::GW, NI = C::NI;
   __shared__ __attribute__((aligned(16))) unsigned char lds[C::LDS];
   unsigned char MLA_LDS* L = (unsigned char MLA_LDS*)lds;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lg = lane >> 4, lc = lane & 15;
-  const int tpp = a.page_rows / kCacheTile;
   const int R = a.n_q * a.n_heads;
 
+  // all arguments in one go: taken as they are needed, each of their lines would cost a
+  // trip to the host's memory before the first key
+  asm volatile("" ::"s"(a.cache), "s"(a.q), "s"(a.pos), "s"(a.pages), "s"(a.seq_pages), "s"(a.tile_base), "s"(a.n_seqs),
+               "s"(a.n_q), "s"(a.n_heads), "s"(a.max_pages), "s"(a.page_rows), "s"(a.cache_pages), "s"(a.page_tiles),
+               "s"(a.n_blocks), "s"(a.shares), "s"(a.scale_log2), "s"(a.inv_page_tiles), "s"(a.inv_shares),
+               "s"(a.inv_blocks));
   // workgroups go to the 8 XCDs round-robin: the blocks of a share follow each other on one
   const int kx = blockIdx.x >> 3;
-  const int hb = kx % a.n_blocks;
-  const int share = (kx / a.n_blocks) * 8 + (blockIdx.x & 7);
+  const int run = quotient(kx, a.n_blocks, a.inv_blocks), hb = kx - run * a.n_blocks;
+  const int share = run * 8 + (blockIdx.x & 7);
   if (share >= a.shares) return;
+
+  double MLA_LDS* theta = (double MLA_LDS*)(L + C::TH_OFF);
 
   // tiles before each request, by a scan over the batch; the request that holds the
   // share's first tile
-  int first_b, first_base, total;
+  int first_b, first_base, first_n, total;
   {
     int MLA_LDS* sums = (int MLA_LDS*)L;
-    const int per = (a.n_seqs + kThreads - 1) / kThreads;
+    const int per = (a.n_seqs + C::THREADS - 1) / C::THREADS;
     const int b0 = tid * per < a.n_seqs ? tid * per : a.n_seqs;
     const int b1 = b0 + per < a.n_seqs ? b0 + per : a.n_seqs;
     int mine = 0;
-    for (int b = b0; b < b1; ++b) mine += tiles_of(a, b, tpp);
+    for (int b = b0; b < b1; ++b) mine += tiles_of(a, b);
     int inc = mine;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -167,20 +226,21 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendAr
     int before = 0;
     total = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < C::WAVES; ++w) {
       const int v = sums[w];
       before += w < wave ? v : 0;
       total += v;
     }
     int base = before + inc - mine;
-    const int lo = Runs(total, a.shares).first(share);
+    const int lo = Runs(a, total).first(share);   // total is the same in all lanes
     const bool writes = blockIdx.x == 0;
     for (int b = b0; b < b1; ++b) {
-      const int n = tiles_of(a, b, tpp);
+      const int n = per == 1 ? mine : tiles_of(a, b);
       if (writes) a.tile_base[b] = base;
       if (lo >= base && lo < base + n) {
         sums[16] = b;
         sums[17] = base;
+        sums[18] = n;
       }
       base += n;
     }
@@ -188,45 +248,45 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendAr
     __syncthreads();
     first_b = __builtin_amdgcn_readfirstlane(sums[16]);
     first_base = __builtin_amdgcn_readfirstlane(sums[17]);
+    first_n = __builtin_amdgcn_readfirstlane(sums[18]);
     total = __builtin_amdgcn_readfirstlane(total);
   }
-  const Runs runs(total, a.shares);
+  const Runs runs(a, total);
   const int lo = runs.first(share), hi = runs.first(share + 1);
   if (lo >= hi) return;
 
-  double MLA_LDS* theta = (double MLA_LDS*)(L + C::TH_OFF);
-  float MLA_LDS* ml = (float MLA_LDS*)(L + C::ML_OFF);
   const uint32_t plane_s = (uint32_t)a.page_rows * kCacheCodes, plane_r = plane_s + (uint32_t)a.page_rows * kCacheScales;
-  if (tid < kMaxRopePairs) theta[tid] = a.rope.theta[tid];
 
   int b = first_b, base = first_base;
   for (; base < hi; ++b) {
-    const int n = __builtin_amdgcn_readfirstlane(tiles_of(a, b, tpp));
+    const int n = b == first_b ? first_n : __builtin_amdgcn_readfirstlane(tiles_of(a, b));
     const int u0 = lo > base ? lo - base : 0, u1 = hi < base + n ? hi - base : n;
     const int seq_base = base;
     base += n;
     if (u0 >= u1) continue;
     Cursor cur;
-    cur.open(a, b, u0, u1, tpp);
+    cur.open(a, b, u0, u1);
     const int32_t* tseq = a.pos + (int64_t)b * a.n_q;
     lds_barrier();   // the tables, and what the previous request left in LDS, are read
     if (wave < 4) {
       // ------------------------------------------------------------------ score wave
-      // Head-row lc of block `wave`; rows past the end repeat the last one and are not stored.
-      if (wave >= NB) {
-        lds_barrier();
-        for (int u = u0; u <= u1; ++u) lds_barrier();
-        continue;
+      // 16-key blocks kw KB .. of the tile, block rw of the head-rows; rows past the end
+      // repeat the last one and are not stored.
+      const int kw = wave % C::KW, rw = wave / C::KW;
+      const int lane = lane_now(), lg = lane >> 4, lc = lane & 15;
+      const unsigned char* qb = (const unsigned char*)a.q + ((int64_t)b * R + hb * BM) * 1152;
+      if (wave == 0 && b == first_b)
+        dma4((const unsigned char*)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(CacheAttendArgs, rope) + lane * 4, L + C::TH_OFF);
+      const int q_last = R - 1 - hb * BM, row = rw * 16 + lc;   // of the block
+      // The block's queries come through LDS: as fragments, sixteen rows a load, they would keep
+      // the address unit four times as long.  A row's 16-byte chunk c lies at c ^ (row & 7).
+#pragma unroll
+      for (int j = wave; j < 18 * NB; j += 4) {
+        const int at = j * 64 + lane, r = at / 72, c = at - r * 72;
+        dma16(qb + (uint32_t)((r < q_last ? r : q_last) * 1152 + (c ^ (r & 7)) * 16), L + C::Q_OFF + j * 1024);
       }
-      int hr = hb * BM + wave * 16 + lc;
-      hr = hr < R ? hr : R - 1;
-      const int t_row = tseq[hr / a.n_heads];
-      const uint16_t* qrow = a.q + ((int64_t)b * R + hr) * 576;
-      bf16x8 qf[16], qraw[2], qh[2], ql[2];   // Q fragments (B operand): dims ks*32 + lg*8 .. +7 of the head-row
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) qraw[ks] = *(const bf16x8*)(qrow + 512 + ks * 32 + lg * 8);
-#pragma unroll
-      for (int ks = 0; ks < 16; ++ks) qf[ks] = *(const bf16x8*)(qrow + ks * 32 + lg * 8);
+      const int t_row = tseq[(hb * BM + (row < q_last ? row : q_last)) / a.n_heads];
+      bf16x8 qf[16], qraw[2], qh[2], ql[2];   // Q fragments (B operand): dims ks*32 + lg*8 .. +7 of head-row lc
       // the RoPE part in a page's frame: the bf16 value and the bf16 of what it lost
       auto relocate = [&](int frame) {
         const double dd = (double)((int64_t)t_row - frame);
@@ -243,47 +303,59 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendAr
           ql[1][i] = (__bf16)(y2 - (float)qh[1][i]);
         }
       };
-      // RoPE keys as K fragments: key kb*16 + lc, chunks lg and lg + 4
-      bf16x8 kr[4][2];
+      // RoPE keys as K fragments: key kb*16 + lc of the wave's, chunks lg and lg + 4
+      bf16x8 kr[KB][2];
       auto load_rope = [&](const Tile& t) {
         const unsigned char* p = a.cache + (int64_t)t.page * a.page_rows * kCacheRow + plane_r;
-        const uint32_t at = (uint32_t)(t.off + lc) * kCacheRope + (uint32_t)lg * 16;
+        const uint32_t at = (uint32_t)(t.off + kw * KB * 16 + lc) * kCacheRope + (uint32_t)lg * 16;
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
+        for (int kb = 0; kb < KB; ++kb) {
           kr[kb][0] = *(const bf16x8*)(p + at + kb * 16 * kCacheRope);
           kr[kb][1] = *(const bf16x8*)(p + at + kb * 16 * kCacheRope + 64);
         }
       };
       // K fragments (A operand, 16 keys x 32 dims): key kb*16 + lc, chunk 4 ks + lg
-      const int kat = (lc >> 3) * C::KBL + (lc & 7) * 128 + ((lg ^ key_swz(lc & 7)) * 16);
+      const int kat = (kw * KB * 2 + (lc >> 3)) * C::KBL + (lc & 7) * 128 + ((lg ^ key_swz(lc & 7)) * 16);
       Tile t = cur.next(a);
       load_rope(t);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      lds_barrier();   // the queries have landed
+      {
+        const unsigned char MLA_LDS* q0 = L + C::Q_OFF + row * 1152;
+#pragma unroll
+        for (int ks = 0; ks < 18; ++ks) {
+          const bf16x8 v = *(const bf16x8 MLA_LDS*)(q0 + (ks >> 1) * 128 + ((((ks & 1) * 4 + lg) ^ (row & 7)) * 16));
+          (ks < 16 ? qf[ks & 15] : qraw[ks & 1]) = v;
+        }
+      }
       relocate(t.frame);
       float m_run = -INFINITY, l_run = 0.f;
       int buf = 0, pb = 0;
-      lds_barrier();   // tiles 0 and 1 are stored
+      lds_barrier();   // tile 0 is stored
       __builtin_amdgcn_s_setprio(1);
       for (int u = u0; u < u1; ++u) {
-        f32x4 s[4];
+        f32x4 s[KB];
         const int k0 = buf + kat, k1 = k0 ^ 64;
-        auto kfrag = [&](int f) -> bf16x8 {   // f = ks * 4 + kb
-          const int ks = f >> 2, kb = f & 3;
+        auto kfrag = [&](int f) -> bf16x8 {   // f = ks * KB + kb
+          const int ks = f / KB, kb = f % KB;
           return *(const bf16x8 MLA_LDS*)(L + (ks & 1 ? k1 : k0) + (ks >> 1) * 1024 + kb * 2 * C::KBL);
         };
         constexpr int KD = 6;   // fragments in the ring, one of them in use
         bf16x8 ka[KD];
 #pragma unroll
         for (int j = 0; j < KD - 1; ++j) ka[j] = kfrag(j);
+        float met = m_run;      // the largest reference that the waves of these head-rows left
+        if (C::KW > 1 && u > u0)
+#pragma unroll
+          for (int k = 0; k < C::KW; ++k) met = fmaxf(met, *(const float MLA_LDS*)(L + C::M_OFF + (((pb ^ 1) * C::KW + k) * BM + row) * 4));
         __builtin_amdgcn_sched_barrier(0);
         // the RoPE steps while the first latent fragments arrive
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kr[kb][0], ql[0], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kr[kb][1], ql[1], s[kb], 0, 0, 0);
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kr[kb][0], qh[0], s[kb], 0, 0, 0);
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kr[kb][1], qh[1], s[kb], 0, 0, 0);
+          for (int kb = 0; kb < KB; ++kb)
+            s[kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kr[kb][j & 1], j < 2 ? ql[j & 1] : qh[j & 1],
+                                                            j == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[kb], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
         const Tile now = t;
         if (u + 1 < u1) {
@@ -292,169 +364,214 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendAr
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int f = 0; f < 64; ++f) {
-          if (f + KD - 1 < 64) ka[(f + KD - 1) % KD] = kfrag(f + KD - 1);
+        for (int f = 0; f < 16 * KB; ++f) {
+          if (f + KD - 1 < 16 * KB) ka[(f + KD - 1) % KD] = kfrag(f + KD - 1);
           __builtin_amdgcn_sched_barrier(0);
-          s[f & 3] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[f % KD], qf[f >> 2], s[f & 3], 0, 0, 0);
+          s[f % KB] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[f % KD], qf[f / KB], s[f % KB], 0, 0, 0);
           __builtin_amdgcn_sched_barrier(0);
         }
-        // register i of s[kb]: key kb*16 + lg*4 + i, head-row lc
-        const int rel = seen_keys(now, t_row) - lg * 4;
-        if (__builtin_amdgcn_ballot_w64(rel + lg * 4 < kCacheTile) != 0) {
+        // register i of s[kb]: key kb*16 + lg*4 + i of the wave's, head-row lc
+        const int seen = seen_keys(now, t_row);
+        if (__builtin_amdgcn_ballot_w64(seen < kCacheTile) != 0) {
+          const int rel = seen - kw * KB * 16 - lg * 4;
 #pragma unroll
-          for (int kb = 0; kb < 4; ++kb)
+          for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               if (kb * 16 + i >= rel) s[kb][i] = -INFINITY;
         }
         float m = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
 #pragma unroll
-        for (int kb = 1; kb < 4; ++kb) m = fmaxf(m, fmaxf(fmaxf(s[kb][0], s[kb][1]), fmaxf(s[kb][2], s[kb][3])));
+        for (int kb = 1; kb < KB; ++kb) m = fmaxf(m, fmaxf(fmaxf(s[kb][0], s[kb][1]), fmaxf(s[kb][2], s[kb][3])));
         m = quad_max(m) * a.scale_log2;
-        float al = 1.f;
-        if ((m > m_run + 8.f) | ((m_run == -INFINITY) & (m > -INFINITY))) {
-          al = __builtin_amdgcn_exp2f(m_run - m);
-          m_run = m;
+        if ((m > met + 8.f) | ((met == -INFINITY) & (m > -INFINITY))) met = ceilf(m);
+        if (met != m_run) {
+          l_run *= __builtin_amdgcn_exp2f(m_run - met);
+          m_run = met;
         }
         const float ref = m_run == -INFINITY ? 0.f : m_run;   // nothing seen yet: every weight is 0
-        float w[4][4];
+        if (lg == 0) *(float MLA_LDS*)(L + C::M_OFF + ((pb * C::KW + kw) * BM + row) * 4) = m_run;
+        float w[KB][4], l = 0.f;
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb)
+        for (int kb = 0; kb < KB; ++kb) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) w[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], a.scale_log2, -ref));
-#pragma unroll
-        for (int k2 = 0; k2 < 2; ++k2)
-          *(u32x4 MLA_LDS*)(L + C::P_OFF + pb * C::P_BYTES + (k2 * NB + wave) * 1024 + lane * 16) =
-              u32x4{pack_bf16x2(w[2 * k2][0], w[2 * k2][1]), pack_bf16x2(w[2 * k2][2], w[2 * k2][3]),
-                    pack_bf16x2(w[2 * k2 + 1][0], w[2 * k2 + 1][1]), pack_bf16x2(w[2 * k2 + 1][2], w[2 * k2 + 1][3])};
-        if (lg == 0) *(float MLA_LDS*)(L + C::AL_OFF + (pb * BM + wave * 16 + lc) * 4) = al;
-        float l = 0.f;
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb) l += (w[kb][0] + w[kb][1]) + (w[kb][2] + w[kb][3]);
-        l_run = l_run * al + l;
-        if (t.frame != now.frame) relocate(t.frame);
+          l += (w[kb][0] + w[kb][1]) + (w[kb][2] + w[kb][3]);
+          const int block = kw * KB + kb;   // of the tile's four
+          *(u32x2 MLA_LDS*)(L + C::P_OFF + pb * C::P_BYTES + ((block >> 1) * NB + rw) * 1024 + lane * 16 + (block & 1) * 8) =
+              u32x2{pack_bf16x2(w[kb][0], w[kb][1]), pack_bf16x2(w[kb][2], w[kb][3])};
+        }
+        l_run += l;
+        if (t.frame != now.frame) {
+          const unsigned char* q0 = qb + (uint32_t)((row < q_last ? row : q_last) * 1152 + 1024 + lg * 16);
+          qraw[0] = *(const bf16x8*)q0;
+          qraw[1] = *(const bf16x8*)(q0 + 64);
+          relocate(t.frame);
+        }
         buf ^= C::LAT;
         pb ^= 1;
+        if (u + 1 == u1) {
+          l = quad_sum(l_run);
+          if (lg == 0) *(float MLA_LDS*)(L + C::L_OFF + (kw * BM + row) * 4) = l;
+        }
         lds_barrier();   // step u - u0 of the score waves
       }
       __builtin_amdgcn_s_setprio(0);
-      const float l = quad_sum(l_run);
-      if (lg == 0) {
-        ml[(wave * 16 + lc) * 2] = m_run;
-        ml[(wave * 16 + lc) * 2 + 1] = l;
-      }
       lds_barrier();
     } else {
       // ------------------------------------------------------------------ value wave
-      // Dims 128 w .. +127 of every head-row; it also converts its dims of the tiles: once
+      // Dims 512 / VW w .. of every head-row; it also converts its dims of the tiles: once
       // it has read them as the value of tile u, tile u + 2 may take their place, since the
       // score waves took tile u in the step before.
       const int w = wave - 4;
-      int t_max = INT32_MIN;
-      {
-        const int last = (hb + 1) * BM < R ? (hb + 1) * BM : R;
-        for (int j = hb * BM / a.n_heads; j <= (last - 1) / a.n_heads; ++j) {
-          const int t = __builtin_amdgcn_readfirstlane(tseq[j]);
-          t_max = t > t_max ? t : t_max;
-        }
-      }
-      // codes of 16 i + lane / 4, group 4 w + lane % 4
-      const int key = lane >> 2, grp = lane & 3;
-      u32x4 cw[4];
-      uint32_t sc[4];
-      auto load_codes = [&](const Tile& t) {
+      const int lane = lane_now(), lg = lane >> 4, lc = lane & 15;
+      // codes of key (64 / GW) i + lane / GW, group GW w + lane % GW
+      const int key = lane / GW, grp = lane % GW;
+      struct Codes {
+        u32x4 c[NI];
+        uint32_t s[NI];
+      };
+      auto load_codes = [&](Codes& x, const Tile& t) {
         const unsigned char* p = a.cache + (int64_t)t.page * a.page_rows * kCacheRow;
-        const uint32_t row = (uint32_t)(t.off + key), g = (uint32_t)(4 * w + grp);
+        const uint32_t row = (uint32_t)(t.off + key), g = (uint32_t)(GW * w + grp);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          cw[i] = *(const u32x4*)(p + row * kCacheCodes + g * 16 + i * 16 * kCacheCodes);
-          sc[i] = (p + plane_s)[row * kCacheScales + g + i * 16 * kCacheScales];
+        for (int i = 0; i < NI; ++i) {
+          x.c[i] = *(const u32x4*)(p + row * kCacheCodes + g * 16 + i * (64 / GW) * kCacheCodes);
+          x.s[i] = (p + plane_s)[row * kCacheScales + g + i * (64 / GW) * kCacheScales];
         }
       };
-      const int sat = (key >> 3) * C::KBL + (key & 7) * 128 + (2 * w + (grp >> 1)) * 1024 +
+      const int sat = (key >> 3) * C::KBL + (key & 7) * 128 + (GW * w + grp) / 2 * 1024 +
                       (((grp & 1) * 4) ^ (grp >> 1) ^ key_swz(key & 7)) * 16;
-      auto store_tile = [&](int buf, int seen) {
+      auto clear = [&](Codes& x, int seen) {   // keys that no row sees: zeros
+        if (seen < kCacheTile)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (seen < kCacheTile && i * 16 + key >= seen) {   // a key that no row sees: zeros
-            cw[i] = u32x4{0, 0, 0, 0};
-            sc[i] = 127;
-          }
-          const float s = mx4_scale(sc[i]);
-          // the four chunks of a group; lanes of the upper groups take neighbours swapped, so
-          // that a store meets all banks
+          for (int i = 0; i < NI; ++i)
+            if (i * (64 / GW) + key >= seen) {
+              x.c[i] = u32x4{0, 0, 0, 0};
+              x.s[i] = 127;
+            }
+      };
+      // Chunk j of a group; lanes of the upper groups take neighbours
+      // swapped, so that a store meets all banks.
+      auto store_chunk = [&](const Codes& x, int buf, int i, int j) {
+        const uint32_t c = grp >> 1 ? x.c[i][j ^ 1] : x.c[i][j];
+        *(bf16x8 MLA_LDS*)(L + ((buf + sat) ^ (j * 16)) + i * (8 / GW) * C::KBL) = mx4_values(c, mx4_scale(x.s[i]));
+      };
+      auto store_keys = [&](const Codes& x, int buf, int i0) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t c = grp >> 1 ? cw[i][j ^ 1] : cw[i][j];
-            *(bf16x8 MLA_LDS*)(L + ((buf + sat) ^ (j * 16)) + i * 2 * C::KBL) = mx4_values(c, s);
-          }
-        }
+        for (int i = i0; i < NI; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) store_chunk(x, buf, i, j);
       };
       Tile t = cur.next(a);
-      load_codes(t);
-      store_tile(0, seen_keys(t, t_max));
-      if (u0 + 1 < u1) {
-        t = cur.next(a);
-        load_codes(t);
-        store_tile(C::LAT, seen_keys(t, t_max));
+      Codes next{};
+      int t_max = INT32_MIN;   // the last position of the block's rows
+      {
+        Codes first;
+        const Tile t0 = t;
+        load_codes(first, t);
+        if (u0 + 1 < u1) {
+          t = cur.next(a);
+          load_codes(next, t);
+        }
+        {
+          const int last = (hb + 1) * BM < R ? (hb + 1) * BM : R;
+          for (int j = hb * BM / a.n_heads; j <= (last - 1) / a.n_heads; ++j) {
+            const int t = __builtin_amdgcn_readfirstlane(tseq[j]);
+            t_max = t > t_max ? t : t_max;
+          }
+        }
+        lds_barrier();   // the queries have landed
+        clear(first, seen_keys(t0, t_max));
+        store_keys(first, 0, 0);
+        lds_barrier();   // tile 0 is stored; the queries have left the second tile's place
+        if (u0 + 1 < u1) {
+          clear(next, seen_keys(t, t_max));
+          store_keys(next, C::LAT, 0);
+        }
       }
       if (u0 + 2 < u1) {
         t = cur.next(a);
-        load_codes(t);
+        load_codes(next, t);
       }
-      f32x4 o[8][NB];
+      f32x4 o[ND][NB];
 #pragma unroll
-      for (int d = 0; d < 8; ++d)
+      for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int h = 0; h < NB; ++h) o[d][h] = f32x4{0.f, 0.f, 0.f, 0.f};
       // V^T fragments (A operand, 16 dims x 32 keys) by transposing reads (see attend_pair.hip)
       const int vkey = (lg & 1) * 4 + (lc >> 2), vcb = lc & 3;
-      const int vat = (lg >> 1) * C::KBL + vkey * 128 + (((vcb >> 1) ^ key_swz(vkey)) * 16) + (vcb & 1) * 8 + w * 2048;
+      const int vat = (lg >> 1) * C::KBL + vkey * 128 + (((vcb >> 1) ^ key_swz(vkey)) * 16) + (vcb & 1) * 8 + w * ND * 256;
+      float mc[NB];   // reference of the sums, head-row lc
+#pragma unroll
+      for (int h = 0; h < NB; ++h) mc[h] = -INFINITY;
       int buf = 0, pb = 0;
-      lds_barrier();   // tiles 0 and 1 are stored
-      lds_barrier();   // the weights of tile 0 are written
+      lds_barrier();   // the weights of tile 0 are written, tile 1 is stored
       for (int u = u0; u < u1; ++u) {
-        auto vfrag = [&](int f) -> bf16x8 {   // f = k2 * 8 + d
-          const unsigned char MLA_LDS* vp = L + ((buf + vat) ^ ((f & 3) * 32)) + ((f >> 2) & 1) * 1024 + (f >> 3) * 4 * C::KBL;
+        auto vfrag = [&](int f) -> bf16x8 {   // f = k2 * ND + d
+          const unsigned char MLA_LDS* vp = L + ((buf + vat) ^ ((f & 3) * 32)) + (f % ND) / 4 * 1024 + f / ND * 4 * C::KBL;
           const bf16x4 vl = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((MLA_LDS bf16x4*)vp);
           const bf16x4 vh = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((MLA_LDS bf16x4*)(vp + 2 * C::KBL));
           return __builtin_shufflevector(vl, vh, 0, 1, 2, 3, 4, 5, 6, 7);
         };
         constexpr int VD = 3;
         bf16x8 vt[VD], p[2][NB];
-        float al[NB];
+        float mk[C::KW][NB];
 #pragma unroll
-        for (int h = 0; h < NB; ++h) al[h] = *(const float MLA_LDS*)(L + C::AL_OFF + (pb * BM + h * 16 + lc) * 4);
+        for (int k = 0; k < C::KW; ++k)
+#pragma unroll
+          for (int h = 0; h < NB; ++h) mk[k][h] = *(const float MLA_LDS*)(L + C::M_OFF + ((pb * C::KW + k) * BM + h * 16 + lc) * 4);
 #pragma unroll
         for (int h = 0; h < NB; ++h) p[0][h] = *(const bf16x8 MLA_LDS*)(L + C::P_OFF + pb * C::P_BYTES + h * 1024 + lane * 16);
 #pragma unroll
         for (int j = 0; j < VD - 1; ++j) vt[j] = vfrag(j);
 #pragma unroll
         for (int h = 0; h < NB; ++h) p[1][h] = *(const bf16x8 MLA_LDS*)(L + C::P_OFF + pb * C::P_BYTES + (NB + h) * 1024 + lane * 16);
+        // Where the references differ, all move to the largest: they are whole numbers, so the
+        // weights change by a power of two and stay exact.
         bool moved = false;
 #pragma unroll
-        for (int h = 0; h < NB; ++h) moved |= al[h] != 1.f;
+        for (int k = 0; k < C::KW; ++k)
+#pragma unroll
+          for (int h = 0; h < NB; ++h) moved |= mk[k][h] != mc[h];
         if (__builtin_amdgcn_ballot_w64(moved) != 0) {
 #pragma unroll
-          for (int h = 0; h < NB; ++h)
+          for (int h = 0; h < NB; ++h) {
+            float top = mc[h];
 #pragma unroll
-            for (int d = 0; d < 8; ++d) o[d][h] *= al[h];
-        }
+            for (int k = 0; k < C::KW; ++k) top = fmaxf(top, mk[k][h]);
+            const float ref = top == -INFINITY ? 0.f : top;
+            const float al = __builtin_amdgcn_exp2f(mc[h] - ref);
+            mc[h] = top;
 #pragma unroll
-        for (int f = 0; f < 16; ++f) {
-          if (f + VD - 1 < 16) vt[(f + VD - 1) % VD] = vfrag(f + VD - 1);
-          __builtin_amdgcn_sched_barrier(0);
+            for (int d = 0; d < ND; ++d) o[d][h] *= al;
 #pragma unroll
-          for (int h = 0; h < NB; ++h)
-            o[f & 7][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[f % VD], p[f >> 3][h], o[f & 7][h], 0, 0, 0);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-        if (u + 2 < u1) {
-          store_tile(buf, seen_keys(t, t_max));
-          if (u + 3 < u1) {
-            t = cur.next(a);
-            load_codes(t);
+            for (int k2 = 0; k2 < 2; ++k2)
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                p[k2][h][i] = (__bf16)((float)p[k2][h][i] * __builtin_amdgcn_exp2f(mk[(k2 * 2 + i / 4) * C::KW / 4][h] - ref));
           }
+        }
+        clear(next, seen_keys(t, t_max));
+        auto values = [&](int f) {
+          if (f + VD - 1 < 2 * ND) vt[(f + VD - 1) % VD] = vfrag(f + VD - 1);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int h = 0; h < NB; ++h)
+            o[f % ND][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[f % VD], p[f / ND][h], o[f % ND][h], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        };
+        // keys 0 .. 31 of tile u + 2 take the place of those just multiplied while the others are
+        // (behind the last tile, codes that nobody reads)
+#pragma unroll
+        for (int f = 0; f < 2 * ND; ++f) {
+          values(f);
+          if (f >= ND) store_chunk(next, buf, (f - ND) / 4, f % 4);
+        }
+        if (u + 2 < u1) store_keys(next, buf, NI / 2);
+        if (u + 3 < u1) {
+          t = cur.next(a);
+          load_codes(next, t);
         }
         buf ^= C::LAT;
         pb ^= 1;
@@ -464,25 +581,33 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendAr
       const int slot = seq_base <= lo ? 2 * share : 2 * share + 1;
 #pragma unroll
       for (int h = 0; h < NB; ++h) {
-        const float m = ml[(h * 16 + lc) * 2], l = ml[(h * 16 + lc) * 2 + 1];
+        float l = 0.f;
+#pragma unroll
+        for (int k = 0; k < C::KW; ++k) {
+          const int at = k * BM + h * 16 + lc;
+          const float mk = *(const float MLA_LDS*)(L + C::M_OFF + ((pb ^ 1) * C::KW * BM + at) * 4);
+          if (mk > -INFINITY) l += *(const float MLA_LDS*)(L + C::L_OFF + at * 4) * __builtin_amdgcn_exp2f(mk - mc[h]);
+        }
+        const float m = mc[h];
         const int row = hb * BM + h * 16 + lc;
-        if (row >= R) continue;
         if (whole) {
+          if (row >= R) continue;
           const int64_t at = (int64_t)b * R + row;
           const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-          for (int d = 0; d < 8; ++d)
-            *(u32x2*)(a.out_o + at * 512 + w * 128 + d * 16 + lg * 4) =
+          for (int d = 0; d < ND; ++d)
+            *(u32x2*)(a.out_o + at * 512 + (w * ND + d) * 16 + lg * 4) =
                 u32x2{pack_bf16x2(o[d][h][0] * inv, o[d][h][1] * inv), pack_bf16x2(o[d][h][2] * inv, o[d][h][3] * inv)};
           if (w == 0 && lg == 0 && a.out_lse != nullptr)
             a.out_lse[at] = l == 0.f ? -INFINITY : (m + __log2f(l)) * 0.6931471805599453f;
         } else {
-          const int64_t at = ((int64_t)slot * a.n_blocks + hb) * BM + h * 16 + lc;
+          // fragments as they lie in the registers: a kilobyte a store
+          const int64_t at = (((int64_t)slot * a.n_blocks + hb) * NB + h) * 16;
 #pragma unroll
-          for (int d = 0; d < 8; ++d) *(f32x4*)(a.part_o + at * 512 + w * 128 + d * 16 + lg * 4) = o[d][h];
+          for (int d = 0; d < ND; ++d) *(f32x4*)(a.part_o + at * 512 + (w * ND + d) * 256 + lane * 4) = o[d][h];
           if (w == 0 && lg == 0) {
-            a.part_ml[at * 2] = m;
-            a.part_ml[at * 2 + 1] = l;
+            a.part_ml[(at + lc) * 2] = m;
+            a.part_ml[(at + lc) * 2 + 1] = l;
           }
         }
       }
@@ -490,89 +615,86 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_kernel(CacheAttendAr
   }
 }
 
-// Joins the sums of requests that several shares hold (and writes those without a tile):
-// G waves take a head-row, eight dims a lane, and its shares in turn.  Bound by the
-// latency of three dependent reads, then by the sums themselves (2 KB a share and head-row).
+// Joins the sums of requests that several shares hold (and writes those without a tile).
+// A wave takes 16 head-rows and 32 dims, two of the fragments that the sums are kept in,
+// and every G-th share; G waves of a workgroup join their sums through LDS.
 template <int G>
 __global__ __launch_bounds__(kThreads) void cache_merge_kernel(CacheAttendArgs a) {
-  __shared__ __attribute__((aligned(16))) float acc[G == 1 ? 1 : kWaves][512];
+  constexpr int kFrags = 2, kUnits = kWaves / G;   // units: (16 head-rows, 32 dims) of a workgroup
+  __shared__ __attribute__((aligned(16))) f32x4 acc[G == 1 ? 1 : kWaves][kFrags + 1][64];
   const int R = a.n_q * a.n_heads;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, lg = lane >> 4, lc = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int b = blockIdx.y, row = blockIdx.x * (kWaves / G) + wave / G, sub = wave % G;
-  if (row >= R) return;   // whole workgroups where waves share a head-row
+  const int b = blockIdx.y, unit = blockIdx.x * kUnits + wave / G, sub = wave % G;
+  const int group = unit / (32 / kFrags), frag = unit % (32 / kFrags) * kFrags;   // 16 head-rows; first fragment
   const int base = a.tile_base[b], n = a.tile_base[b + 1] - base;
+  const int row = group * 16 + lc;
   const int64_t at = (int64_t)b * R + row;
-  if (n == 0) {
-    if (sub != 0) return;
-    *(u32x4*)(a.out_o + at * 512 + lane * 8) = u32x4{0, 0, 0, 0};
-    if (lane == 0 && a.out_lse != nullptr) a.out_lse[at] = -INFINITY;
-    return;
-  }
-  const Runs runs(a.tile_base[a.n_seqs], a.shares);
-  const int s0 = runs.share(base), s1 = runs.share(base + n - 1);
-  if (s0 == s1) return;
-  const int block = row / a.block, in_block = row - block * a.block;
-  // share s's sums: its first request's or, where another request ends in it, its last one's
-  const int first_slot = base <= runs.first(s0) ? 2 * s0 : 2 * s0 + 1;
-  auto place = [&](int s) -> int64_t {
-    return ((int64_t)(s == s0 ? first_slot : 2 * s) * a.n_blocks + block) * a.block + in_block;
-  };
-  constexpr int kAhead = 4;
-  f32x4 v[kAhead][2];
-  auto load = [&](int s) {   // shares s, s + G, ..: past the end the last one again, not used
+  if (row - lc >= R) return;
+  f32x4 o[kFrags];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      const int at_s = s + j * G <= s1 ? s + j * G : s1;
-      const f32x4* src = (const f32x4*)(a.part_o + place(at_s) * 512 + lane * 8);
-      v[j][0] = src[0];
-      v[j][1] = src[1];
-    }
-  };
-  load(s0 + sub);
-  float m = -INFINITY;
-  for (int s = s0 + lane; s <= s1; s += 64) m = fmaxf(m, a.part_ml[place(s) * 2]);
+  for (int f = 0; f < kFrags; ++f) o[f] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  if (n > 0) {
+    const Runs runs(a, a.tile_base[a.n_seqs]);
+    const int s0 = runs.share(base), s1 = runs.share(base + n - 1);
+    if (s0 == s1) return;
+    // share s's sums: its first request's or, where another request ends in it, its last one's
+    const int first_slot = base <= runs.first(s0) ? 2 * s0 : 2 * s0 + 1;
+    const int nb = a.block / 16, block = group / nb, in_block = group - block * nb;
+    constexpr int kAhead = 4;
+    for (int s = s0 + sub; s <= s1; s += kAhead * G) {
+      f32x4 v[kAhead][kFrags];
+      float mv[kAhead], lv[kAhead];
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  const float ref = m == -INFINITY ? 0.f : m;
-  f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = {0.f, 0.f, 0.f, 0.f};
-  float l = 0.f;
-  for (int c = s0; c <= s1; c += 64) {   // 64 shares: lane j holds the weight of share c + j
-    float w = 0.f;
-    if (c + lane <= s1) {
-      const float* ml = a.part_ml + place(c + lane) * 2;
-      w = __builtin_amdgcn_exp2f(ml[0] - ref);
-      l += w * ml[1];
-    }
-    for (int i = sub; i < 64 && c + i <= s1; i += kAhead * G) {
+      for (int j = 0; j < kAhead; ++j) {   // past the end the last one again, not used
+        const int sj = s + j * G <= s1 ? s + j * G : s1;
+        const int64_t from = (((int64_t)(sj == s0 ? first_slot : 2 * sj) * a.n_blocks + block) * nb + in_block) * 16;
+        mv[j] = a.part_ml[(from + lc) * 2];
+        lv[j] = a.part_ml[(from + lc) * 2 + 1];
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f) v[j][f] = *(const f32x4*)(a.part_o + from * 512 + (frag + f) * 256 + lane * 4);
+      }
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
-        if (c + i + j * G > s1) break;
-        const float wj = __shfl(w, i + j * G, 64);
-        x += v[j][0] * wj;
-        y += v[j][1] * wj;
+        if (s + j * G > s1) break;
+        const float top = fmaxf(m, mv[j]), ref = top == -INFINITY ? 0.f : top;
+        const float x = __builtin_amdgcn_exp2f(m - ref), y = __builtin_amdgcn_exp2f(mv[j] - ref);
+        m = top;
+        l = l * x + lv[j] * y;
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f) o[f] = o[f] * x + v[j][f] * y;
       }
-      if (c + i + kAhead * G <= s1) load(c + i + kAhead * G);
     }
-  }
+    if constexpr (G > 1) {
+      static_assert(G == 1 || G == kWaves, "the waves of a unit are a workgroup");
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
+      for (int f = 0; f < kFrags; ++f) acc[wave][f][lane] = o[f];
+      acc[wave][kFrags][lane] = f32x4{m, l, 0.f, 0.f};
+      __syncthreads();
+      if (wave != 0) return;
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) {
+        const f32x4 x4 = acc[w][kFrags][lane];
+        const float top = fmaxf(m, x4[0]), ref = top == -INFINITY ? 0.f : top;
+        const float x = __builtin_amdgcn_exp2f(m - ref), y = __builtin_amdgcn_exp2f(x4[0] - ref);
+        m = top;
+        l = l * x + x4[1] * y;
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f) o[f] = o[f] * x + acc[w][f][lane] * y;
+      }
+    }
+  } else if (sub != 0) {
+    return;
+  }
+  if (row >= R) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  if (sub == 0 && lane == 0 && a.out_lse != nullptr)
-    a.out_lse[at] = l == 0.f ? -INFINITY : (ref + __log2f(l)) * 0.6931471805599453f;
-  if constexpr (G == 1) {
-    *(u32x4*)(a.out_o + at * 512 + lane * 8) = u32x4{pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv),
-                                                     pack_bf16x2(y[0] * inv, y[1] * inv), pack_bf16x2(y[2] * inv, y[3] * inv)};
-  } else {
-    static_assert(G == 1 || G == kWaves, "a head-row's waves are a workgroup");
-    *(f32x4*)&acc[wave][lane * 8] = x;
-    *(f32x4*)&acc[wave][lane * 8 + 4] = y;
-    __syncthreads();
-    float o = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) o += acc[w][threadIdx.x];
-    a.out_o[at * 512 + threadIdx.x] = __builtin_bit_cast(uint16_t, (__bf16)(o * inv));
-  }
+  for (int f = 0; f < kFrags; ++f)
+    *(u32x2*)(a.out_o + at * 512 + (frag + f) * 16 + lg * 4) =
+        u32x2{pack_bf16x2(o[f][0] * inv, o[f][1] * inv), pack_bf16x2(o[f][2] * inv, o[f][3] * inv)};
+  if (frag == 0 && lg == 0 && a.out_lse != nullptr)
+    a.out_lse[at] = l == 0.f ? -INFINITY : (m + __log2f(l)) * 0.6931471805599453f;
 }
 
 }  // namespace
@@ -580,21 +702,21 @@ __global__ __launch_bounds__(kThreads) void cache_merge_kernel(CacheAttendArgs a
 hipError_t launch_cache_attend(const CacheAttendArgs& a, hipStream_t s) {
   const unsigned grid = 8u * (unsigned)a.n_blocks * (unsigned)((a.shares + 7) / 8);
   if (a.block == 16)
-    cache_attend_kernel<1><<<dim3(grid), dim3(kThreads), 0, s>>>(a);
+    cache_attend_kernel<1><<<dim3(grid), dim3(CaCfg<1>::THREADS), 0, s>>>(a);
   else if (a.block == 32)
-    cache_attend_kernel<2><<<dim3(grid), dim3(kThreads), 0, s>>>(a);
+    cache_attend_kernel<2><<<dim3(grid), dim3(CaCfg<2>::THREADS), 0, s>>>(a);
   else
-    cache_attend_kernel<4><<<dim3(grid), dim3(kThreads), 0, s>>>(a);
+    cache_attend_kernel<4><<<dim3(grid), dim3(CaCfg<4>::THREADS), 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const unsigned R = (unsigned)(a.n_q * a.n_heads), n_seqs = (unsigned)a.n_seqs;
-  // A wave a head-row where it can hold all its shares' sums in flight at once, else eight
-  // (64 requests of 16k keys, 4 shares each: 209 against 216 us for the whole call; 48
-  // requests of 6k, 5.3 shares: 47.7 against 47.0; one of 264k, 256 shares: 99 against 64)
+  const unsigned units = (unsigned)(a.n_q * a.n_heads + 15) / 16 * 16, n_seqs = (unsigned)a.n_seqs;
+  // A wave a unit where it holds all shares of a request in flight at once, else eight (64
+  // requests of 4 shares each: 201 against 211 us for the whole call; 48 of 5.3 shares: 43.4
+  // against 42.3; one of 256 shares: 151 against 64)
   if (a.shares <= 4 * a.n_seqs)
-    cache_merge_kernel<1><<<dim3((R + kWaves - 1) / kWaves, n_seqs), dim3(kThreads), 0, s>>>(a);
+    cache_merge_kernel<1><<<dim3(units / kWaves, n_seqs), dim3(kThreads), 0, s>>>(a);
   else
-    cache_merge_kernel<kWaves><<<dim3(R, n_seqs), dim3(kThreads), 0, s>>>(a);
+    cache_merge_kernel<kWaves><<<dim3(units, n_seqs), dim3(kThreads), 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -116,10 +116,12 @@ struct CacheAttendArgs {
   int32_t* tile_base;         // [n_seqs + 1]: tiles before each request
   int32_t n_seqs, n_q, n_heads;
   int32_t max_pages, page_rows, cache_pages;
-  int32_t block;              // head-rows per workgroup: 32 or 64
+  int32_t page_tiles;         // page_rows in tiles
+  int32_t block;              // head-rows per workgroup: 16, 32 or 64
   int32_t n_blocks;           // blocks of a request's n_q * n_heads head-rows
   int32_t shares;             // equal runs of the batch's tiles
   float scale_log2;
+  double inv_page_tiles, inv_shares, inv_blocks;   // reciprocals
   RopeTable rope;
 };
 hipError_t launch_cache_attend(const CacheAttendArgs& a, hipStream_t s);
