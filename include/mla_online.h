@@ -520,7 +520,8 @@ mla_status mla_mx4_dequantize(int64_t n_rows, int32_t n_cols, const void* codes,
  * matrix cores, not by the weight: dequantize once and call mla_shared_wb).
  * Products and sums as in mla_shared_wb (bf16 MFMA, fp32 sums), in an order that
  * depends on d_in alone: a row of z gives the same bits in any call.
- *   n_rows, d_in, d_out  as for mla_shared_wb (d_in up to MLA_WB_MAX_D_IN)
+ *   n_rows, d_in, d_out  as for mla_shared_wb (d_in up to MLA_WB_MAX_D_IN, d_out up
+ *                  to MLA_WB_MX4_MAX_D_OUT)
  *   z              [N, d_in] bf16 device, 16-byte aligned
  *   w_codes        [d_out, d_in/2] device, 16-byte aligned
  *   w_scales       [d_out, d_in/32] device, 4-byte aligned
@@ -528,6 +529,7 @@ mla_status mla_mx4_dequantize(int64_t n_rows, int32_t n_cols, const void* codes,
  * Errors: NULL, SHAPE, UNSUPPORTED, HIP.  Kernels only: may be captured. */
 #define MLA_WB_MAX_D_IN 16384
 #define MLA_WB_MX4_MAX_ROWS 1024
+#define MLA_WB_MX4_MAX_D_OUT 16777216
 mla_status mla_shared_wb_mx4(int64_t n_rows, int32_t d_in, int32_t d_out, const void* z, const void* w_codes,
                              const void* w_scales, int32_t out_dtype, void* y, void* stream);
 

@@ -155,7 +155,8 @@ mla_status mla_shared_wb_mx4(int64_t n_rows, int32_t d_in, int32_t d_out, const 
   if (d_in < 64 || d_in % 64 != 0) return fail(MLA_ERR_SHAPE, "d_in = %d must be a positive multiple of 64", d_in);
   if (d_in > MLA_WB_MAX_D_IN) return fail(MLA_ERR_UNSUPPORTED, "d_in = %d; built: up to %d", d_in, MLA_WB_MAX_D_IN);
   if (d_out < 1) return fail(MLA_ERR_SHAPE, "d_out = %d", d_out);
-  if (d_out > INT32_MAX - 64) return fail(MLA_ERR_UNSUPPORTED, "d_out = %d", d_out);
+  if (d_out > MLA_WB_MX4_MAX_D_OUT)
+    return fail(MLA_ERR_UNSUPPORTED, "d_out = %d; built: up to %d", d_out, MLA_WB_MX4_MAX_D_OUT);
   if (out_dtype != MLA_BF16 && out_dtype != MLA_F32) return fail(MLA_ERR_SHAPE, "out_dtype %d", out_dtype);
   if (n_rows > MLA_WB_MX4_MAX_ROWS)
     return fail(MLA_ERR_UNSUPPORTED, "n_rows = %lld; built: up to %d (mla_mx4_dequantize, then mla_shared_wb)",

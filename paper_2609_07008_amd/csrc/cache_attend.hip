@@ -67,11 +67,7 @@ struct CaCfg {
 // slot of 16-byte chunk c of key k in its kilobyte: c ^ key_swz(k) (see attend_pair.hip)
 __device__ __forceinline__ int key_swz(int k) { return k ^ ((~k & 1) << 2); }
 
-// 16 bytes a lane from memory to LDS, lane after lane
-__device__ __forceinline__ void dma16(const unsigned char* from, unsigned char MLA_LDS* to) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (MLA_LDS void*)to, 16, 0, 0);
-}
-
+// four bytes a lane from memory to LDS, lane after lane
 __device__ __forceinline__ void dma4(const unsigned char* from, unsigned char MLA_LDS* to) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (MLA_LDS void*)to, 4, 0, 0);
 }

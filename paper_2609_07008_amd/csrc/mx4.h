@@ -15,6 +15,11 @@ typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
 // (0 is 2^-127, 255 gives NaN; checked over all scales and bytes).
 __device__ __forceinline__ float mx4_scale(uint32_t e) { return __uint_as_float(e << 23); }
 
+// 16 bytes a lane from memory to LDS, lane after lane
+__device__ __forceinline__ void dma16(const void* from, unsigned char MLA_LDS* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (MLA_LDS void*)to, 16, 0, 0);
+}
+
 // eight codes (one register) as eight bf16 values, in order
 __device__ __forceinline__ bf16x8 mx4_values(uint32_t codes, float scale) {
   const bf16x2v a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0);

@@ -49,6 +49,10 @@ def test_wb_refusals(mla, over, status):
                                      _p(d["y"]), None) == status
 
 
+def test_wb_channels_past_the_grid(mla):
+    assert mla.LIB.mla_shared_wb_mx4(1, 64, 2 ** 24 + 1, _p(A), _p(A), _p(A), 1, _p(A), None) == UNSUPPORTED
+
+
 ROWS = dict(g={}, n=2, kv=A, stride=576, slots=A, pages=4, page_rows=64, cache=A)
 
 

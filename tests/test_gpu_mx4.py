@@ -144,6 +144,25 @@ def test_wb_mx4_rows_alike_in_any_call():
         assert torch.equal(_wb(z[lo:hi].contiguous(), c, s, "f32").view(torch.int32), full[lo:hi].contiguous().view(torch.int32))
 
 
+# every tile, its last block of rows and of channels ragged; d_in: whole steps, a half slab, fewer slabs than a step
+TILES = [(5, 200, 1088), (31, 1001, 192), (16, 6150, 320), (32, 6150, 1088), (9, 12300, 448), (30, 12300, 576), (150, 6150, 1088),
+         (190, 12300, 320)]
+
+
+@pytest.mark.parametrize("n,d_out,d_in", TILES)
+def test_wb_mx4_tiles(n, d_out, d_in):
+    """One answer from every tile: against 64 bits, and a row alone in the same bits."""
+    import torch
+    rng = np.random.default_rng(n + d_in + d_out)
+    z = _bf16_dev(rng.standard_normal((n, d_in)))
+    c, s = _weight(d_out, d_in, d_in + d_out)
+    y = _wb(z, c, s, "f32")
+    w, zz = R.values(c, s), _host(z)
+    assert (np.abs(_host(y) - zz @ w.T) <= d_in * 2.0 ** -24 * (np.abs(zz) @ np.abs(w).T) + 1e-30).all()
+    for row in (0, n // 2, n - 1):
+        assert torch.equal(_wb(z[row:row + 1].contiguous(), c, s, "f32").view(torch.int32), y[row:row + 1].view(torch.int32))
+
+
 def test_wb_mx4_nan_scale_and_infinite_row():
     """A NaN group reaches its channel alone, an infinite z its row alone."""
     rng = np.random.default_rng(8)
