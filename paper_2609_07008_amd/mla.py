@@ -336,14 +336,25 @@ def _refuse(what: str, status: int = 2):
     raise MlaError(status, what)
 
 
-def _tensor(name, t, dtype, shape=None, rows=False):
-    """t is a device tensor of dtype and, if given, shape (a tuple); contiguous, or (rows)
+def _device():
+    """The current device; None before the first use of one, when no tensor lies on any."""
+    return torch.cuda.current_device() if torch.cuda.is_initialized() else None
+
+
+def _queue(stream, dev) -> int:
+    """The handle of stream, or of the current stream of dev (an object for it would cost a
+    quarter of a small call)."""
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
+def _tensor(name, t, dev, dtype, shape=None, rows=False):
+    """t is a tensor on dev, of dtype and, if given, shape (a tuple); contiguous, or (rows)
     two-dimensional with contiguous rows."""
     if not isinstance(t, torch.Tensor):
         _refuse(f"{name} is not a tensor", 1)
     if t.dtype != dtype:
         _refuse(f"{name} is {t.dtype}, expected {dtype}")
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+    if t.get_device() != dev:
         _refuse(f"{name} is on {t.device}, not the current device")
     if shape is not None and t.shape != shape:
         _refuse(f"{name} is {tuple(t.shape)}, expected {shape}")
@@ -366,43 +377,46 @@ def _addr(t):
 def mx4_quantize(x, codes, scales, stream=None):
     """bf16 rows into the 4-bit format (mla_mx4_quantize): x [N, C] bfloat16 with
     contiguous rows, codes [N, C/2] and scales [N, C/32] uint8, written."""
-    _tensor("x", x, torch.bfloat16, rows=True)
+    dev = _device()
+    _tensor("x", x, dev, torch.bfloat16, rows=True)
     n, c = x.shape
-    _tensor("codes", codes, torch.uint8, (n, c // 2))
-    _tensor("scales", scales, torch.uint8, (n, c // 32))
-    _check(LIB.mla_mx4_quantize(n, c, _addr(x), _row_stride(x), _addr(codes), _addr(scales), _stream(stream)))
+    _tensor("codes", codes, dev, torch.uint8, (n, c // 2))
+    _tensor("scales", scales, dev, torch.uint8, (n, c // 32))
+    _check(LIB.mla_mx4_quantize(n, c, _addr(x), _row_stride(x), _addr(codes), _addr(scales), _queue(stream, dev)))
 
 
 def mx4_dequantize(codes, scales, x, stream=None):
     """The values of codes [N, C/2] and scales [N, C/32] into x [N, C] bfloat16 with
     contiguous rows (mla_mx4_dequantize)."""
-    _tensor("x", x, torch.bfloat16, rows=True)
+    dev = _device()
+    _tensor("x", x, dev, torch.bfloat16, rows=True)
     n, c = x.shape
-    _tensor("codes", codes, torch.uint8, (n, c // 2))
-    _tensor("scales", scales, torch.uint8, (n, c // 32))
-    _check(LIB.mla_mx4_dequantize(n, c, _addr(codes), _addr(scales), _addr(x), _row_stride(x), _stream(stream)))
+    _tensor("codes", codes, dev, torch.uint8, (n, c // 2))
+    _tensor("scales", scales, dev, torch.uint8, (n, c // 32))
+    _check(LIB.mla_mx4_dequantize(n, c, _addr(codes), _addr(scales), _addr(x), _row_stride(x), _queue(stream, dev)))
 
 
 def shared_wb_mx4(z, w_codes, w_scales, y, stream=None):
     """y = W_b z with W_b in 4 bits (mla_shared_wb_mx4): z [N, d_in] bfloat16,
     w_codes [d_out, d_in/2] and w_scales [d_out, d_in/32] uint8, y [N, d_out] float32
     or bfloat16."""
-    _tensor("z", z, torch.bfloat16)
-    _tensor("w_codes", w_codes, torch.uint8)
+    dev = _device()
+    _tensor("z", z, dev, torch.bfloat16)
+    _tensor("w_codes", w_codes, dev, torch.uint8)
     if z.dim() != 2 or w_codes.dim() != 2 or w_codes.shape[1] * 2 != z.shape[1]:
         _refuse(f"z is {tuple(z.shape)}, w_codes {tuple(w_codes.shape)}")
     n, d_in = z.shape
     d_out = w_codes.shape[0]
-    _tensor("w_scales", w_scales, torch.uint8, (d_out, d_in // 32))
+    _tensor("w_scales", w_scales, dev, torch.uint8, (d_out, d_in // 32))
     bf16 = isinstance(y, torch.Tensor) and y.dtype == torch.bfloat16
-    _tensor("y", y, torch.bfloat16 if bf16 else torch.float32, (n, d_out))
+    _tensor("y", y, dev, torch.bfloat16 if bf16 else torch.float32, (n, d_out))
     _check(LIB.mla_shared_wb_mx4(n, d_in, d_out, _addr(z), _addr(w_codes), _addr(w_scales), MLA_BF16 if bf16 else MLA_F32,
-                                 _addr(y), _stream(stream)))
+                                 _addr(y), _queue(stream, dev)))
 
 
-def _cache_pages(cache, page_rows: int) -> int:
+def _cache_pages(cache, dev, page_rows: int) -> int:
     """Pages of a cache tensor [pages, page_rows * CACHE_ROW_BYTES] uint8."""
-    _tensor("cache", cache, torch.uint8)
+    _tensor("cache", cache, dev, torch.uint8)
     if cache.dim() != 2 or cache.shape[1] != page_rows * CACHE_ROW_BYTES:
         _refuse(f"cache is {tuple(cache.shape)}, expected [pages, {page_rows} * {CACHE_ROW_BYTES}]")
     return cache.shape[0]
@@ -412,32 +426,32 @@ def cache_append(geom, kv, slots, cache, page_rows: int, pos=None, stream=None):
     """Rows of kv [N, d_latent + d_rope] bfloat16 (contiguous rows) into the paged 4-bit
     cache [pages, page_rows * CACHE_ROW_BYTES] uint8 at slots [N] int32, the RoPE part
     turned to pos [N] int32 if given (mla_cache_append)."""
-    g = make_geom(geom)
-    pages = _cache_pages(cache, page_rows)
-    _tensor("kv", kv, torch.bfloat16, rows=True)
+    g, dev = make_geom(geom), _device()
+    pages = _cache_pages(cache, dev, page_rows)
+    _tensor("kv", kv, dev, torch.bfloat16, rows=True)
     n, d = kv.shape
     if d != g.d_latent + g.d_rope:
         _refuse(f"kv is {tuple(kv.shape)}, expected [N, {g.d_latent + g.d_rope}]")
-    _tensor("slots", slots, torch.int32, (n,))
+    _tensor("slots", slots, dev, torch.int32, (n,))
     if pos is not None:
-        _tensor("pos", pos, torch.int32, (n,))
+        _tensor("pos", pos, dev, torch.int32, (n,))
     _check(LIB.mla_cache_append(ctypes.byref(g), n, _addr(kv), _row_stride(kv), _addr(pos), _addr(slots), pages, page_rows,
-                                _addr(cache), _stream(stream)))
+                                _addr(cache), _queue(stream, dev)))
 
 
 def cache_gather(geom, slots, cache, page_rows: int, kv, stream=None):
     """Rows slots [N] int32 of the cache into kv [N, d_latent + d_rope] bfloat16 with
     contiguous rows (mla_cache_gather); rows whose slot is outside the cache are left as
     they were."""
-    g = make_geom(geom)
-    pages = _cache_pages(cache, page_rows)
-    _tensor("kv", kv, torch.bfloat16, rows=True)
+    g, dev = make_geom(geom), _device()
+    pages = _cache_pages(cache, dev, page_rows)
+    _tensor("kv", kv, dev, torch.bfloat16, rows=True)
     n, d = kv.shape
     if d != g.d_latent + g.d_rope:
         _refuse(f"kv is {tuple(kv.shape)}, expected [N, {g.d_latent + g.d_rope}]")
-    _tensor("slots", slots, torch.int32, (n,))
+    _tensor("slots", slots, dev, torch.int32, (n,))
     _check(LIB.mla_cache_gather(ctypes.byref(g), n, _addr(slots), pages, page_rows, _addr(cache), _addr(kv), _row_stride(kv),
-                                _stream(stream)))
+                                _queue(stream, dev)))
 
 
 def cache_attend_query(geom, n_seqs: int, n_q: int, max_pages: int, page_rows: int) -> int:
@@ -453,24 +467,24 @@ def cache_attend(geom, q, pos, pages, seq_pages, cache, page_rows: int, out_o, o
     [B, n_q, H, d_latent + d_rope] bfloat16, pos [B, n_q] int32, pages [B, max_pages, 4]
     int32 (page, rows, req_pos, frame), seq_pages [B] int32, out_o [B, n_q, H, d_latent]
     bfloat16, out_lse [B, n_q, H] float32 or None."""
-    g = make_geom(geom)
-    n_pages = _cache_pages(cache, page_rows)
-    _tensor("q", q, torch.bfloat16)
-    _tensor("pages", pages, torch.int32)
+    g, dev = make_geom(geom), _device()
+    n_pages = _cache_pages(cache, dev, page_rows)
+    _tensor("q", q, dev, torch.bfloat16)
+    _tensor("pages", pages, dev, torch.int32)
     if q.dim() != 4 or q.shape[2] != g.n_heads or q.shape[3] != g.d_latent + g.d_rope:
         _refuse(f"q is {tuple(q.shape)}, expected [B, n_q, {g.n_heads}, {g.d_latent + g.d_rope}]")
     b, n_q, heads, _ = q.shape
     if pages.dim() != 3 or pages.shape[0] != b or pages.shape[2] != 4:
         _refuse(f"pages is {tuple(pages.shape)}, expected [{b}, max_pages, 4]")
-    _tensor("pos", pos, torch.int32, (b, n_q))
-    _tensor("seq_pages", seq_pages, torch.int32, (b,))
-    _tensor("out_o", out_o, torch.bfloat16, (b, n_q, heads, g.d_latent))
+    _tensor("pos", pos, dev, torch.int32, (b, n_q))
+    _tensor("seq_pages", seq_pages, dev, torch.int32, (b,))
+    _tensor("out_o", out_o, dev, torch.bfloat16, (b, n_q, heads, g.d_latent))
     if out_lse is not None:
-        _tensor("out_lse", out_lse, torch.float32, (b, n_q, heads))
-    _tensor("workspace", workspace, torch.uint8)
+        _tensor("out_lse", out_lse, dev, torch.float32, (b, n_q, heads))
+    _tensor("workspace", workspace, dev, torch.uint8)
     _check(LIB.mla_cache_attend(ctypes.byref(g), b, n_q, _addr(q), _addr(pos), _addr(pages), _addr(seq_pages), pages.shape[1],
                                 n_pages, page_rows, _addr(cache), _addr(out_o), _addr(out_lse), _addr(workspace),
-                                workspace.numel(), _stream(stream)))
+                                workspace.numel(), _queue(stream, dev)))
 
 
 def probe_mfma_bf16(iters, sink, stream=None) -> float:
