@@ -6,6 +6,8 @@ and allocation only; every computation is a call into libmla_online.so.
 """
 from __future__ import annotations
 
+from types import SimpleNamespace
+
 import numpy as np
 import torch
 
@@ -113,3 +115,59 @@ class PlannedStep:
         self.attend(prot_rows, n_prot, kv, q_glob, q_loc, stream)
         self.oproj(prot_rows, n_prot, w_o, z_off, stream)
         return self.z
+
+
+class DecodeStep:
+    """The attention part of a decode layer on the paged 4-bit cache, for a fixed batch of
+    n_seqs requests of n_q new tokens each (a padded request: slots and positions -1):
+      mla_cache_append  the tokens' rows into their pages,
+      mla_cache_attend  every head over the request's pages,
+      mla_sliced_oproj_add_planned  z = W_a O with every head Global (new tokens have no
+                        artifact, so all rows are protected and z_off is never read),
+      mla_shared_wb_mx4 y = W_b z.
+    Every call only enqueues kernels: run() may be captured and replayed while positions,
+    slots and pages change in their tensors.  Buffers and argument marshalling only."""
+
+    def __init__(self, geom, n_seqs: int, n_q: int, max_pages: int, page_rows: int, d_out: int, device="cuda",
+                 y_dtype=torch.bfloat16, with_lse: bool = False):
+        self.geom = geom
+        self.page_rows = int(page_rows)
+        heads, self.n_rows = int(geom.n_heads), int(n_seqs) * int(n_q)
+        fields = ("d_latent", "d_rope", "d_model", "n_proj_groups", "softmax_scale", "rope_base")
+        self.all_global = SimpleNamespace(n_heads=heads, n_groups=heads, **{f: getattr(geom, f) for f in fields})
+        self.info = mla.plan_query(self.all_global, [(0, self.n_rows, 0)], 0, self.n_rows)
+        dev = torch.device(device)
+        ws = mla.cache_attend_query(geom, n_seqs, n_q, max_pages, page_rows)
+        self.ws = torch.empty((max(ws, 256),), dtype=torch.uint8, device=dev)
+        d_c = int(geom.d_latent)
+        self.out_o = torch.empty((n_seqs, n_q, heads, d_c), dtype=torch.bfloat16, device=dev)
+        self.out_lse = torch.empty((n_seqs, n_q, heads), dtype=torch.float32, device=dev) if with_lse else None
+        self.glob_head = np.zeros((heads,), dtype=np.int32)
+        self.all_rows = torch.arange(self.n_rows, dtype=torch.int32, device=dev)
+        self.n_prot = torch.full((1,), self.n_rows, dtype=torch.int32, device=dev)
+        self.z = torch.empty((self.n_rows, int(geom.d_model)), dtype=torch.bfloat16, device=dev)
+        self.y = torch.empty((self.n_rows, int(d_out)), dtype=y_dtype, device=dev)
+
+    def append(self, kv, slots, cache, turn, stream=None):
+        mla.cache_append(self.geom, kv, slots, cache, self.page_rows, pos=turn, stream=stream)
+
+    def attend(self, q, pos, pages, seq_pages, cache, stream=None):
+        mla.cache_attend(self.geom, q, pos, pages, seq_pages, cache, self.page_rows, self.out_o, self.out_lse,
+                         workspace=self.ws, stream=stream)
+
+    def oproj(self, w_o, stream=None):
+        mla.sliced_oproj_add_planned(self.all_global, self.info, self.out_o, None, self.glob_head, self.all_rows,
+                                     self.n_prot, w_o, self.z, self.z, stream)
+
+    def project(self, wb_codes, wb_scales, stream=None):
+        mla.shared_wb_mx4(self.z, wb_codes, wb_scales, self.y, stream)
+
+    def run(self, kv, slots, q, pos, pages, seq_pages, cache, w_o, wb_codes, wb_scales, turn=None, stream=None):
+        """kv [n_rows, D] bfloat16, slots [n_rows] int32, q [n_seqs, n_q, H, D], pos [n_seqs,
+        n_q] int32; turn [n_rows] int32: each row's position in its page's RoPE frame (pos
+        where the frame is 0).  Returns y [n_rows, d_out]."""
+        self.append(kv, slots, cache, pos.view(-1) if turn is None else turn, stream)
+        self.attend(q, pos, pages, seq_pages, cache, stream)
+        self.oproj(w_o, stream)
+        self.project(wb_codes, wb_scales, stream)
+        return self.y
