@@ -33,10 +33,10 @@
  *    slot waits for the copy that last read it, so a third back-to-back call
  *    may block the host until the first call's copy has run.  Every other
  *    call only enqueues kernels and never blocks.
- *  - HIP graph capture: the merge, o-proj, W_b, MoE and the planned
- *    protected-set, attend and o-proj calls enqueue kernels only (no memset or
- *    memcpy nodes) and may be captured.  The calls that upload a plan return MLA_ERR_UNSUPPORTED on a
- *    capturing stream, before enqueueing anything: their staging buffer is
+ *  - HIP graph capture: the merge, o-proj, W_b, MoE, 4-bit and cache calls and the
+ *    planned protected-set, attend and o-proj calls enqueue kernels only (no memset
+ *    or memcpy nodes) and may be captured.  The calls that upload a plan return
+ *    MLA_ERR_UNSUPPORTED on a capturing stream, before enqueueing anything: their staging buffer is
  *    reused by later calls, so a replay would not read the captured plan.
  *  - Every entry point validates its arguments on the host before enqueueing
  *    anything and returns a status; it never aborts and never falls back to a
