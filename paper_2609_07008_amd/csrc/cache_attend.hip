@@ -582,7 +582,7 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
         for (int k = 0; k < C::KW; ++k) {
           const int at = k * BM + h * 16 + lc;
           const float mk = *(const float MLA_LDS*)(L + C::M_OFF + ((pb ^ 1) * C::KW * BM + at) * 4);
-          if (mk > -INFINITY) l += *(const float MLA_LDS*)(L + C::L_OFF + at * 4) * __builtin_amdgcn_exp2f(mk - mc[h]);
+          l += *(const float MLA_LDS*)(L + C::L_OFF + at * 4) * (mk == mc[h] ? 1.f : __builtin_amdgcn_exp2f(mk - mc[h]));   // a NaN stays
         }
         const float m = mc[h];
         const int row = hb * BM + h * 16 + lc;

@@ -214,3 +214,18 @@ def test_references_that_differ_between_score_waves(heads):
     pages, count = table([[(0, n, 0, True)]] * 3, pr, list(range(full)) * 3)
     pos = np.array([[n - 1], [17], [64]], dtype=np.int32)
     check_attend(R.geom(heads), q, pos, pages, count, raw, pr)
+
+
+@pytest.mark.parametrize("heads", [4, 24, 64])
+def test_a_request_of_nan_keys_alone(heads):
+    """Nothing but NaN scores, in one tile and over several workgroups: NaN, not an empty row."""
+    import torch
+    rng = np.random.default_rng(heads)
+    raw = random_cache(rng, 6, 64)
+    raw[:5, 64 * 256: 64 * 272] = 255
+    pages, count = table([[(0, 1, 0, True)], [(0, 70, 0, True)], [(0, 128, 0, True)], [(0, 64, 0, True)]], 64, [0, 1, 2, 3, 4, 5])
+    pos = np.array([[0], [69], [127], [63]], dtype=np.int32)
+    q = rng.standard_normal((4, 1, heads, 576)) * 0.5
+    out, lse = run_attend(R.geom(heads), _bf16_dev(q), _dev(pos), _dev(pages), _dev(count), _dev(raw), 64)
+    assert torch.isnan(out[:3]).all() and torch.isnan(lse[:3]).all()
+    assert torch.isfinite(out[3]).all() and torch.isfinite(lse[3]).all()
