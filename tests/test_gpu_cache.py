@@ -193,6 +193,17 @@ def test_attend_plain_requests(name):
     check_attend(R.geom(heads), q, pos, pages, count, raw, pr, name)
 
 
+@pytest.mark.parametrize("heads,nq", [(128, 20), (128, 66), (96, 3)])
+def test_attend_many_head_rows(heads, nq):
+    """Shares of many head-row blocks, fewer than the XCDs or not a multiple of them."""
+    rng = np.random.default_rng(nq)
+    lens = [150, nq]
+    raw = random_cache(rng, 8, 64)
+    pages, count = table([own(n) for n in lens], 64, rng.permutation(8))
+    pos = np.array([[n - nq + j for j in range(nq)] for n in lens], dtype=np.int32)
+    check_attend(R.geom(heads), rng.standard_normal((2, nq, heads, 576)) * 0.5, pos, pages, count, raw, 64)
+
+
 @pytest.mark.parametrize("heads,nq,pr", [(64, 1, 64), (16, 2, 128), (128, 1, 64)])
 def test_attend_relocated_documents(heads, nq, pr):
     """Documents in their canonical frames at far request positions, stored in any order and
