@@ -502,13 +502,15 @@ mla_status mla_shared_wb(int64_t n_rows, int32_t d_in, int32_t d_out, const void
  * so the result does not depend on the machine.
  * mla_mx4_dequantize: back to bf16 (with mla_shared_wb, W_b for many rows).
  *
- *   n_rows, n_cols  N rows (>= 0) of n_cols values (a multiple of 32)
+ *   n_rows, n_cols  N rows (>= 0) of n_cols values (a multiple of 32, at most
+ *                   MLA_MX4_MAX_COLS)
  *   x               device bf16 [N, n_cols], rows x_stride elements apart (a
  *                   multiple of 8, at least n_cols), 16-byte aligned
  *   codes           device [N, n_cols/2] bytes, 16-byte aligned
  *   scales          device [N, n_cols/32] bytes
- * Errors: NULL, SHAPE, HIP.  Kernels only: may be captured.
+ * Errors: NULL, SHAPE, UNSUPPORTED, HIP.  Kernels only: may be captured.
  * ------------------------------------------------------------------------- */
+#define MLA_MX4_MAX_COLS 1073741824
 mla_status mla_mx4_quantize(int64_t n_rows, int32_t n_cols, const void* x, int64_t x_stride, void* codes, void* scales,
                             void* stream);
 
@@ -612,8 +614,8 @@ typedef struct mla_page {
  *              (calls that may overlap need one each)
  * Everything that changes from token to token is read on the device, so a decode
  * step is captured once and replayed as positions and pages change.  The result
- * does not depend on timing: a call gives the same bits again.  The split of a request's keys, and with it the order of its
- * sums, depends on the whole batch.
+ * does not depend on timing: a call gives the same bits again.  The split of a
+ * request's keys, and with it the order of its sums, depends on the whole batch.
  * A NaN in a key makes every row NaN that sees it, and may make NaN the rows of
  * the same call and request that come before it.
  * n_seqs, n_q, H and the pages' totals fix the workspace.

@@ -82,6 +82,7 @@ mla::CacheRowsArgs rows_args(const mla_geom* geom, int64_t n_rows, const void* k
 mla_status check_mx4(int64_t n_rows, int32_t n_cols, const void* x, int64_t x_stride, const void* codes, const void* scales) {
   if (n_rows < 0) return fail(MLA_ERR_SHAPE, "n_rows = %lld", (long long)n_rows);
   if (n_cols < 32 || n_cols % 32 != 0) return fail(MLA_ERR_SHAPE, "n_cols = %d must be a positive multiple of 32", n_cols);
+  if (n_cols > MLA_MX4_MAX_COLS) return fail(MLA_ERR_UNSUPPORTED, "n_cols = %d; built: up to %d", n_cols, MLA_MX4_MAX_COLS);
   if (x_stride < n_cols || x_stride % 8 != 0)
     return fail(MLA_ERR_SHAPE, "x_stride = %lld must be a multiple of 8, at least n_cols", (long long)x_stride);
   if (n_rows > INT64_MAX / 2 / x_stride) return fail(MLA_ERR_SHAPE, "n_rows * x_stride overflows");

@@ -344,7 +344,11 @@ def _device():
 def _queue(stream, dev) -> int:
     """The handle of stream, or of the current stream of dev (an object for it would cost a
     quarter of a small call)."""
-    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        _refuse(f"the stream is of device {stream.device_index}, not the current device")
+    return stream.cuda_stream
 
 
 def _tensor(name, t, dev, dtype, shape=None, rows=False):

@@ -49,6 +49,21 @@ def test_wb_refusals(mla, over, status):
                                      _p(d["y"]), None) == status
 
 
+def test_quantize_columns_past_32_bits(mla):
+    for cols, status in ((2 ** 30 + 32, UNSUPPORTED), (2 ** 31 - 32, UNSUPPORTED)):
+        assert mla.LIB.mla_mx4_quantize(1, cols, _p(A), 2 ** 31, _p(A), _p(A), None) == status
+        assert mla.LIB.mla_mx4_dequantize(1, cols, _p(A), _p(A), _p(A), 2 ** 31, None) == status
+
+
+def test_stream_of_another_device(mla, monkeypatch):
+    """A stream that is not of the current device is refused before anything is enqueued."""
+    from types import SimpleNamespace
+    other = SimpleNamespace(device_index=1, cuda_stream=0)
+    with pytest.raises(mla.MlaError):
+        mla._queue(other, 0)
+    assert mla._queue(SimpleNamespace(device_index=0, cuda_stream=7), 0) == 7
+
+
 def test_wb_channels_past_the_grid(mla):
     assert mla.LIB.mla_shared_wb_mx4(1, 64, 2 ** 24 + 1, _p(A), _p(A), _p(A), 1, _p(A), None) == UNSUPPORTED
 
