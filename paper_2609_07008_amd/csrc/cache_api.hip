@@ -120,7 +120,7 @@ mla_status attend_split(const mla_geom* geom, int32_t n_seqs, int32_t n_q, int32
   auto up = [](int64_t x) { return (x + 255) / 256 * 256; };
   const int64_t part_rows = (int64_t)2 * S->shares * S->n_blocks * S->block;
   S->off_ml = up(((int64_t)n_seqs + 1) * 4);
-  S->off_o = S->off_ml + up(part_rows * 2 * 4);
+  S->off_o = S->off_ml + up(part_rows * 4 * 4);
   S->total = (size_t)(S->off_o + part_rows * 512 * 4);
   return MLA_OK;
 }

@@ -11,8 +11,10 @@
 //            that lost: the scores are then as exact as the products, which a request of a
 //            few keys shows in its lse.  Softmax against a reference that moves (and sums
 //            are rescaled) only when a tile exceeds it by 2^8, so weights stay below 2^9
-//            and sums in 32 bits lose nothing.  Weights in bf16: half a step, 2^-9 of each,
-//            next to an output of the same width.
+//            and sums in 32 bits lose nothing.  Weights in bf16: half a step of each, next
+//            to an output of the same width; outputs are divided by the sum of the rounded
+//            weights, so that a request of one key answers with its value, and the lse takes
+//            the sum of the weights themselves.
 //   value    four, eight with fewer than 64 head-rows, 512 / waves dims each: O^T += V^T P^T.
 //            They convert their dims of the tiles too (v_cvt_scalef32_pk_bf16_fp4), once,
 //            into LDS as bf16 in the layout of the online attention's tiles
@@ -40,6 +42,8 @@ namespace {
 
 constexpr int kWaves = 8, kThreads = kWaves * 64;   // of cache_merge_kernel
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
 template <int NB>
 struct CaCfg {
   static constexpr int BM = 16 * NB;         // head-rows of a workgroup
@@ -56,8 +60,8 @@ struct CaCfg {
   static constexpr int P_OFF = 2 * LAT;      // weights of two tiles, [32 keys][NB] KB in the layout of the MFMA operand
   static constexpr int P_BYTES = 2 * NB * 1024;
   static constexpr int M_OFF = P_OFF + 2 * P_BYTES;     // [2][KW][BM]: references of the tile's weights
-  static constexpr int L_OFF = M_OFF + 2 * KW * BM * 4; // [KW][BM]: row sums at the end
-  static constexpr int TH_OFF = L_OFF + KW * BM * 4;
+  static constexpr int L_OFF = M_OFF + 2 * KW * BM * 4; // [KW][BM][2]: row sums at the end, of the weights and of their bf16 values
+  static constexpr int TH_OFF = L_OFF + KW * BM * 8;
   static constexpr int LDS = TH_OFF + kMaxRopePairs * 8;
   static constexpr int Q_OFF = LAT;          // queries on their way to registers, 1152 bytes a head-row
   static_assert(Q_OFF + BM * 1152 <= M_OFF, "before the second tile and the weights are stored");
@@ -334,7 +338,7 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
         }
       }
       relocate(t.frame);
-      float m_run = -INFINITY, l_run = 0.f;
+      float m_run = -INFINITY, l_run = 0.f, r_run = 0.f;   // reference; row sums of the weights and of their bf16 values
       int buf = 0, pb = 0;
       lds_barrier();   // tile 0 is stored
       __builtin_amdgcn_s_setprio(1);
@@ -391,22 +395,26 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
         m = quad_max(m) * a.scale_log2;
         if ((m > met + 8.f) | ((met == -INFINITY) & (m > -INFINITY))) met = ceilf(m);
         if (met != m_run) {
-          l_run *= __builtin_amdgcn_exp2f(m_run - met);
+          const float al = __builtin_amdgcn_exp2f(m_run - met);
+          l_run *= al;
+          r_run *= al;
           m_run = met;
         }
         const float ref = m_run == -INFINITY ? 0.f : m_run;   // nothing seen yet: every weight is 0
         if (lg == 0) *(float MLA_LDS*)(L + C::M_OFF + ((pb * C::KW + kw) * BM + row) * 4) = m_run;
-        float w[KB][4], l = 0.f;
+        float w[KB][4], l = 0.f, r = 0.f;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) w[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], a.scale_log2, -ref));
           l += (w[kb][0] + w[kb][1]) + (w[kb][2] + w[kb][3]);
           const int block = kw * KB + kb;   // of the tile's four
-          *(u32x2 MLA_LDS*)(L + C::P_OFF + pb * C::P_BYTES + ((block >> 1) * NB + rw) * 1024 + lane * 16 + (block & 1) * 8) =
-              u32x2{pack_bf16x2(w[kb][0], w[kb][1]), pack_bf16x2(w[kb][2], w[kb][3])};
+          const u32x2 b = {pack_bf16x2(w[kb][0], w[kb][1]), pack_bf16x2(w[kb][2], w[kb][3])};
+          *(u32x2 MLA_LDS*)(L + C::P_OFF + pb * C::P_BYTES + ((block >> 1) * NB + rw) * 1024 + lane * 16 + (block & 1) * 8) = b;
+          r += (bf16_lo(b[0]) + bf16_hi(b[0])) + (bf16_lo(b[1]) + bf16_hi(b[1]));
         }
         l_run += l;
+        r_run += r;
         if (t.frame != now.frame) {
           const unsigned char* q0 = qb + (uint32_t)((row < q_last ? row : q_last) * 1152 + 1024 + lg * 16);
           qraw[0] = *(const bf16x8*)q0;
@@ -417,7 +425,8 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
         pb ^= 1;
         if (u + 1 == u1) {
           l = quad_sum(l_run);
-          if (lg == 0) *(float MLA_LDS*)(L + C::L_OFF + (kw * BM + row) * 4) = l;
+          r = quad_sum(r_run);
+          if (lg == 0) *(f32x2 MLA_LDS*)(L + C::L_OFF + (kw * BM + row) * 8) = f32x2{l, r};
         }
         lds_barrier();   // step u - u0 of the score waves
       }
@@ -586,19 +595,22 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
       const int slot = seq_base <= lo ? 2 * share : 2 * share + 1;
 #pragma unroll
       for (int h = 0; h < NB; ++h) {
-        float l = 0.f;
+        float l = 0.f, r = 0.f;
 #pragma unroll
         for (int k = 0; k < C::KW; ++k) {
           const int at = k * BM + h * 16 + lc;
           const float mk = *(const float MLA_LDS*)(L + C::M_OFF + ((pb ^ 1) * C::KW * BM + at) * 4);
-          l += *(const float MLA_LDS*)(L + C::L_OFF + at * 4) * (mk == mc[h] ? 1.f : __builtin_amdgcn_exp2f(mk - mc[h]));   // a NaN stays
+          const f32x2 lr = *(const f32x2 MLA_LDS*)(L + C::L_OFF + at * 8);
+          const float al = mk == mc[h] ? 1.f : __builtin_amdgcn_exp2f(mk - mc[h]);
+          l += lr[0] * al;   // a NaN stays
+          r += lr[1] * al;
         }
         const float m = mc[h];
         const int row = hb * BM + h * 16 + lc;
         if (whole) {
           if (row >= R) continue;
           const int64_t at = (int64_t)b * R + row;
-          const float inv = l == 0.f ? 0.f : 1.f / l;
+          const float inv = r == 0.f ? 0.f : 1.f / r;
 #pragma unroll
           for (int d = 0; d < ND; ++d)
             *(u32x2*)(a.out_o + at * 512 + (w * ND + d) * 16 + lg * 4) =
@@ -611,8 +623,7 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
 #pragma unroll
           for (int d = 0; d < ND; ++d) *(f32x4*)(a.part_o + at * 512 + (w * ND + d) * 256 + lane * 4) = o[d][h];
           if (w == 0 && lg == 0) {
-            a.part_ml[(at + lc) * 2] = m;
-            a.part_ml[(at + lc) * 2 + 1] = l;
+            *(f32x4*)(a.part_ml + (at + lc) * 4) = f32x4{m, l, r, 0.f};
           }
         }
       }
@@ -639,7 +650,7 @@ __global__ __launch_bounds__(kThreads) void cache_merge_kernel(CacheAttendArgs a
   f32x4 o[kFrags];
 #pragma unroll
   for (int f = 0; f < kFrags; ++f) o[f] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, l = 0.f, r = 0.f;
   if (n > 0) {
     const Runs runs(a, a.tile_base[a.n_seqs]);
     const int s0 = runs.share(base), s1 = runs.share(base + n - 1);
@@ -650,23 +661,23 @@ __global__ __launch_bounds__(kThreads) void cache_merge_kernel(CacheAttendArgs a
     constexpr int kAhead = 4;
     for (int s = s0 + sub; s <= s1; s += kAhead * G) {
       f32x4 v[kAhead][kFrags];
-      float mv[kAhead], lv[kAhead];
+      f32x4 ml[kAhead];
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {   // past the end the last one again, not used
         const int sj = s + j * G <= s1 ? s + j * G : s1;
         const int64_t from = (((int64_t)(sj == s0 ? first_slot : 2 * sj) * a.n_blocks + block) * nb + in_block) * 16;
-        mv[j] = a.part_ml[(from + lc) * 2];
-        lv[j] = a.part_ml[(from + lc) * 2 + 1];
+        ml[j] = *(const f32x4*)(a.part_ml + (from + lc) * 4);
 #pragma unroll
         for (int f = 0; f < kFrags; ++f) v[j][f] = *(const f32x4*)(a.part_o + from * 512 + (frag + f) * 256 + lane * 4);
       }
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
         if (s + j * G > s1) break;
-        const float top = fmaxf(m, mv[j]), ref = top == -INFINITY ? 0.f : top;
-        const float x = __builtin_amdgcn_exp2f(m - ref), y = __builtin_amdgcn_exp2f(mv[j] - ref);
+        const float top = fmaxf(m, ml[j][0]), ref = top == -INFINITY ? 0.f : top;
+        const float x = __builtin_amdgcn_exp2f(m - ref), y = __builtin_amdgcn_exp2f(ml[j][0] - ref);
         m = top;
-        l = l * x + lv[j] * y;
+        l = l * x + ml[j][1] * y;
+        r = r * x + ml[j][2] * y;
 #pragma unroll
         for (int f = 0; f < kFrags; ++f) o[f] = o[f] * x + v[j][f] * y;
       }
@@ -675,7 +686,7 @@ __global__ __launch_bounds__(kThreads) void cache_merge_kernel(CacheAttendArgs a
       static_assert(G == 1 || G == kWaves, "the waves of a unit are a workgroup");
 #pragma unroll
       for (int f = 0; f < kFrags; ++f) acc[wave][f][lane] = o[f];
-      acc[wave][kFrags][lane] = f32x4{m, l, 0.f, 0.f};
+      acc[wave][kFrags][lane] = f32x4{m, l, r, 0.f};
       __syncthreads();
       if (wave != 0) return;
 #pragma unroll
@@ -685,6 +696,7 @@ __global__ __launch_bounds__(kThreads) void cache_merge_kernel(CacheAttendArgs a
         const float x = __builtin_amdgcn_exp2f(m - ref), y = __builtin_amdgcn_exp2f(x4[0] - ref);
         m = top;
         l = l * x + x4[1] * y;
+        r = r * x + x4[2] * y;
 #pragma unroll
         for (int f = 0; f < kFrags; ++f) o[f] = o[f] * x + acc[w][f][lane] * y;
       }
@@ -693,7 +705,7 @@ __global__ __launch_bounds__(kThreads) void cache_merge_kernel(CacheAttendArgs a
     return;
   }
   if (row >= R) return;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float inv = r == 0.f ? 0.f : 1.f / r;
 #pragma unroll
   for (int f = 0; f < kFrags; ++f)
     *(u32x2*)(a.out_o + at * 512 + (frag + f) * 16 + lg * 4) =

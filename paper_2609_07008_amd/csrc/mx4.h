@@ -117,7 +117,7 @@ struct CacheAttendArgs {
   uint16_t* out_o;            // [n_seqs, n_q, n_heads, 512] bf16
   float* out_lse;             // [n_seqs, n_q, n_heads] or NULL
   float* part_o;              // [2 shares, n_blocks, block / 16, 32, 64, 4]: sums of a request that several shares hold, as 16-dim fragments
-  float* part_ml;             // [2 shares, n_blocks, block, 2]: reference (log2 units) and row sum
+  float* part_ml;             // [2 shares, n_blocks, block, 4]: reference (log2 units), row sums of the weights and of their bf16 values
   int32_t* tile_base;         // [n_seqs + 1]: tiles before each request
   int32_t n_seqs, n_q, n_heads;
   int32_t max_pages, page_rows, cache_pages;

@@ -229,3 +229,24 @@ def test_a_request_of_nan_keys_alone(heads):
     out, lse = run_attend(R.geom(heads), _bf16_dev(q), _dev(pos), _dev(pages), _dev(count), _dev(raw), 64)
     assert torch.isnan(out[:3]).all() and torch.isnan(lse[:3]).all()
     assert torch.isfinite(out[3]).all() and torch.isfinite(lse[3]).all()
+
+
+@pytest.mark.parametrize("heads,n", [(4, 1), (64, 1), (24, 90), (64, 200)])
+def test_one_value_is_answered_exactly(heads, n):
+    """A request of one key, or of keys with one latent: the output is that latent, whatever the
+    weights and their rounding (its bf16 values are exact); over several workgroups too."""
+    import torch
+    from paper_2609_07008_amd import mla
+    rng = np.random.default_rng(n + heads)
+    raw = random_cache(rng, 4, 64)
+    raw[:, : 64 * 256] = np.tile(raw[0, :256], (4, 64))
+    raw[:, 64 * 256: 64 * 272] = np.tile(raw[0, 64 * 256: 64 * 256 + 16], (4, 64))
+    pages, count = table([[(0, n, 0, True)]], 64, [0, 1, 2, 3])
+    q = _bf16_dev(rng.standard_normal((1, 1, heads, 576)))
+    out, _ = run_attend(R.geom(heads), q, _dev(np.array([[n - 1]], dtype=np.int32)), _dev(pages), _dev(count), _dev(raw), 64)
+    lat, _ = R.Cache(raw, 64).rows(0)
+    want = np.broadcast_to(lat[0], (heads, 512))
+    got = _host(out)[0, 0]
+    # sums of n terms w v and n terms w in 32 bits, one division, one rounding to bf16: next to
+    # an exact bf16 value the 32-bit errors (n 2^-24 each) do not reach half a bf16 step
+    assert np.array_equal(got, want)
