@@ -133,6 +133,11 @@ class DecodeStep:
         self.geom = geom
         self.page_rows = int(page_rows)
         heads, self.n_rows = int(geom.n_heads), int(n_seqs) * int(n_q)
+        if self.n_rows > mla.WB_MX4_MAX_ROWS:
+            raise mla.MlaError(3, f"{self.n_rows} new tokens; the 4-bit W_b takes up to {mla.WB_MX4_MAX_ROWS}")
+        npg, d_model = int(geom.n_proj_groups), int(geom.d_model)
+        if npg < 1 or heads % npg or d_model < 1 or d_model % (32 * npg) or d_model % 64:
+            raise mla.MlaError(2, f"{heads} heads, d_model {d_model}, {npg} projection groups")
         fields = ("d_latent", "d_rope", "d_model", "n_proj_groups", "softmax_scale", "rope_base")
         self.all_global = SimpleNamespace(n_heads=heads, n_groups=heads, **{f: getattr(geom, f) for f in fields})
         self.info = mla.plan_query(self.all_global, [(0, self.n_rows, 0)], 0, self.n_rows)

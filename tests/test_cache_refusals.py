@@ -55,6 +55,17 @@ def test_quantize_columns_past_32_bits(mla):
         assert mla.LIB.mla_mx4_dequantize(1, cols, _p(A), _p(A), _p(A), 2 ** 31, None) == status
 
 
+def test_decode_step_refusals(mla):
+    """What a step could not run is refused where it is made."""
+    import mx4_reference as R
+    from paper_2609_07008_amd.step import DecodeStep
+    for bad in (dict(n_seqs=513, n_q=2), dict(page_rows=63), dict(n_q=0), dict(n_seqs=-1), dict(geom=R.geom(64, d_c=64, d_r=16)),
+                dict(geom=R.geom(129)), dict(geom=R.geom(16, n_proj_groups=3))):
+        a = {**dict(geom=R.geom(16), n_seqs=2, n_q=1, max_pages=3, page_rows=64, d_out=64), **bad}
+        with pytest.raises(mla.MlaError):
+            DecodeStep(**a, device="cpu")
+
+
 def test_stream_of_another_device(mla, monkeypatch):
     """A stream that is not of the current device is refused before anything is enqueued."""
     from types import SimpleNamespace
