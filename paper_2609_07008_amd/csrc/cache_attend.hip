@@ -223,6 +223,7 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
     const int b0 = tid * per < a.n_seqs ? tid * per : a.n_seqs;
     const int b1 = b0 + per < a.n_seqs ? b0 + per : a.n_seqs;
     int mine = 0;
+#pragma unroll 4
     for (int b = b0; b < b1; ++b) mine += tiles_of(a, b);
     int inc = mine;
 #pragma unroll
@@ -266,13 +267,15 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
 
   const uint32_t plane_s = (uint32_t)a.page_rows * kCacheCodes, plane_r = plane_s + (uint32_t)a.page_rows * kCacheScales;
 
-  int b = first_b, base = first_base;
-  for (; base < hi; ++b) {
-    const int n = b == first_b ? first_n : __builtin_amdgcn_readfirstlane(tiles_of(a, b));
+  // Lanes hold the tiles of 64 requests, so that the next one with any is found at once,
+  // however many of a padded batch lie between.
+  int b = first_b, base = first_base, n = first_n, held = first_b;
+  auto tiles_from = [&](int from) { return from + lane < a.n_seqs ? tiles_of(a, from + lane) : 0; };
+  int next_tiles = tiles_from(held);
+  for (;;) {
     const int u0 = lo > base ? lo - base : 0, u1 = hi < base + n ? hi - base : n;
     const int seq_base = base;
     base += n;
-    if (u0 >= u1) continue;
     Cursor cur;
     cur.open(a, b, u0, u1);
     const int32_t* tseq = a.pos + (int64_t)b * a.n_q;
@@ -627,6 +630,19 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
           }
         }
       }
+    }
+    if (base >= hi) return;
+    for (;;) {
+      const uint64_t with = __builtin_amdgcn_ballot_w64(next_tiles > 0 && held + lane > b);
+      if (with != 0) {
+        const int at = __builtin_ctzll(with);
+        b = held + at;
+        n = __builtin_amdgcn_readlane(next_tiles, at);
+        break;
+      }
+      held += 64;
+      if (held >= a.n_seqs) return;
+      next_tiles = tiles_from(held);
     }
   }
 }

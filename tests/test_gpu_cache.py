@@ -331,6 +331,19 @@ def test_attend_many_requests(seqs):
     check_attend(R.geom(4), q, pos, pages, count, raw, 64)
 
 
+@pytest.mark.parametrize("heads", [4, 64])
+def test_attend_batch_with_holes(heads):
+    """A few requests far apart in a padded batch, several of them in one workgroup's share."""
+    rng = np.random.default_rng(heads)
+    lens = np.zeros(1300, dtype=np.int64)
+    lens[[3, 66, 67, 400, 831, 1299]] = 130, 64, 1, 200, 65, 700
+    need = int(sum(-(-n // 64) for n in lens))
+    raw = random_cache(rng, need, 64)
+    pages, count = table([own(n) if n else [] for n in lens], 64, rng.permutation(need))
+    pos = (lens[:, None] - 1).astype(np.int32)
+    check_attend(R.geom(heads), rng.standard_normal((1300, 1, heads, 576)) * 0.5, pos, pages, count, raw, 64)
+
+
 def test_attend_batch_of_none_and_without_pages():
     import torch
     from paper_2609_07008_amd import mla
