@@ -611,15 +611,23 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
         const float m = mc[h];
         const int row = hb * BM + h * 16 + lc;
         if (whole) {
-          if (row >= R) continue;
-          const int64_t at = (int64_t)b * R + row;
+          // Through LDS, in which no tile is read any more, to rows: stored as they lie, sixteen
+          // head-rows a store, they would keep the address unit four times as long.
+          constexpr int RS = ND * 32 + 16, CR = ND * 2;   // a row's bytes there; its 16-byte chunks
+          unsigned char MLA_LDS* own = L + w * 16 * RS;
           const float inv = r == 0.f ? 0.f : 1.f / r;
 #pragma unroll
           for (int d = 0; d < ND; ++d)
-            *(u32x2*)(a.out_o + at * 512 + (w * ND + d) * 16 + lg * 4) =
+            *(u32x2 MLA_LDS*)(own + lc * RS + d * 32 + lg * 8) =
                 u32x2{pack_bf16x2(o[d][h][0] * inv, o[d][h][1] * inv), pack_bf16x2(o[d][h][2] * inv, o[d][h][3] * inv)};
-          if (w == 0 && lg == 0 && a.out_lse != nullptr)
-            a.out_lse[at] = l == 0.f ? -INFINITY : (m + __log2f(l)) * 0.6931471805599453f;
+#pragma unroll
+          for (int i = 0; i < CR / 4; ++i) {
+            const int rr = i * (64 / CR) + lane / CR, at_row = hb * BM + h * 16 + rr;
+            const u32x4 v = *(const u32x4 MLA_LDS*)(own + rr * RS + lane % CR * 16);
+            if (at_row < R) *(u32x4*)(a.out_o + ((int64_t)b * R + at_row) * 512 + w * ND * 16 + lane % CR * 8) = v;
+          }
+          if (w == 0 && lg == 0 && a.out_lse != nullptr && row < R)
+            a.out_lse[(int64_t)b * R + row] = l == 0.f ? -INFINITY : (m + __log2f(l)) * 0.6931471805599453f;
         } else {
           // fragments as they lie in the registers: a kilobyte a store
           const int64_t at = (((int64_t)slot * a.n_blocks + hb) * NB + h) * 16;
