@@ -26,13 +26,13 @@
 // equal runs, one a workgroup (and head-row block).  A request inside one run is written
 // at once; one that crosses runs leaves sums to cache_merge_kernel.
 //
-// Measured, whole calls with the joining: 64 requests of ~16k keys, 64 heads 202 us, of
-// which a tile's 144 matrix products a SIMD fill half of its 5000 clocks; the rest is
-// conversion and softmax, which the products of the other kind hide only in part, and
-// 3328 clocks of LDS traffic.  16 requests of ~8k, 256 head-rows 85 us; one of 264k,
-// 64 heads 64 us.  48 of ~6k, 16 heads 41 us, of which 8 are the start (three dependent
-// reads from memory before the first tile) and 5 the joining: there the conversion bounds
-// a tile, and eight value waves against four take 41.4 against 43.5.
+// Measured, whole calls with the joining: 64 requests of ~16k keys (18,474 tiles), 64 heads
+// 200 to 212 us, 2.5 us a tile and compute unit; a tile's products keep the matrix cores
+// busy 2300 of its 5000 clocks, its LDS traffic takes 2600, its vector instructions 2100: the
+// two kinds of waves hide each other only in part.  16 requests of ~8k, 256 head-rows 85 us;
+// one of 264k, 64 heads 65 us.  48 of ~6k, 16 heads 41 us, of which 8 are the start (three
+// dependent reads from memory before the first tile) and 5 the joining: there the
+// conversion bounds a tile, and eight value waves against four take 41.4 against 43.5.
 #include "mx4.h"
 
 #include <algorithm>
@@ -405,16 +405,25 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
         }
         const float ref = m_run == -INFINITY ? 0.f : m_run;   // nothing seen yet: every weight is 0
         if (lg == 0) *(float MLA_LDS*)(L + C::M_OFF + ((pb * C::KW + kw) * BM + row) * 4) = m_run;
-        float w[KB][4], l = 0.f, r = 0.f;
+        float l = 0.f, r = 0.f;
+        u32x2 b[KB];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
+          float w[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], a.scale_log2, -ref));
-          l += (w[kb][0] + w[kb][1]) + (w[kb][2] + w[kb][3]);
-          const int block = kw * KB + kb;   // of the tile's four
-          const u32x2 b = {pack_bf16x2(w[kb][0], w[kb][1]), pack_bf16x2(w[kb][2], w[kb][3])};
-          *(u32x2 MLA_LDS*)(L + C::P_OFF + pb * C::P_BYTES + ((block >> 1) * NB + rw) * 1024 + lane * 16 + (block & 1) * 8) = b;
-          r += (bf16_lo(b[0]) + bf16_hi(b[0])) + (bf16_lo(b[1]) + bf16_hi(b[1]));
+          for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], a.scale_log2, -ref));
+          l += (w[0] + w[1]) + (w[2] + w[3]);
+          b[kb] = u32x2{pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3])};
+          r += (bf16_lo(b[kb][0]) + bf16_hi(b[kb][0])) + (bf16_lo(b[kb][1]) + bf16_hi(b[kb][1]));
+        }
+        // key blocks 2 k2 and 2 k2 + 1 of the tile: a lane's eight keys of a fragment
+        unsigned char MLA_LDS* at = L + C::P_OFF + pb * C::P_BYTES + rw * 1024 + lane * 16;
+        if constexpr (KB == 1) {
+          *(u32x2 MLA_LDS*)(at + (kw >> 1) * NB * 1024 + (kw & 1) * 8) = b[0];
+        } else {
+#pragma unroll
+          for (int k = 0; k < KB / 2; ++k)
+            *(u32x4 MLA_LDS*)(at + (kw * KB / 2 + k) * NB * 1024) = u32x4{b[2 * k][0], b[2 * k][1], b[2 * k + 1][0], b[2 * k + 1][1]};
         }
         l_run += l;
         r_run += r;
@@ -570,6 +579,7 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
           }
         }
         clear(next, seen_keys(t, t_max));
+        __builtin_amdgcn_s_setprio(2);   // the longer way: 85 us where the scores alone come first takes 86 (16 requests, 256 head-rows)
         auto values = [&](int f) {
           if (f + VD - 1 < 2 * ND) vt[(f + VD - 1) % VD] = vfrag(f + VD - 1);
           __builtin_amdgcn_sched_barrier(0);
@@ -585,6 +595,7 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
           values(f);
           if (f >= ND) store_chunk(next, buf, (f - ND) / 4, f % 4);
         }
+        __builtin_amdgcn_s_setprio(0);
         if (u + 2 < u1) store_keys(next, buf, NI / 2);
         if (u + 3 < u1) {
           t = cur.next(a);
