@@ -49,7 +49,8 @@ struct CaCfg {
   static constexpr int BM = 16 * NB;         // head-rows of a workgroup
   static constexpr int KW = 4 / NB;          // score waves that share 16 head-rows, each with its keys
   static constexpr int KB = NB;              // 16-key blocks of a score wave
-  // value waves: eight where registers allow (at NB = 4 they would take 254 us where four take 205)
+  // value waves: eight up to 32 head-rows (41.4 against 43.5 us with four, 48 requests of 6k keys
+  // and 16 heads); at NB = 4 eight, in 168 registers each, take as long as four
   static constexpr int VW = NB == 4 ? 4 : 8;
   static constexpr int WAVES = 4 + VW, THREADS = 64 * WAVES;
   static constexpr int ND = 32 / VW;         // 16-dim fragments of a value wave
@@ -667,11 +668,11 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
 }
 
 // Joins the sums of requests that several shares hold (and writes those without a tile).
-// A wave takes 16 head-rows and 32 dims, two of the fragments that the sums are kept in,
+// A wave takes 16 head-rows and 16 kFrags dims, the fragments that the sums are kept in,
 // and every G-th share; G waves of a workgroup join their sums through LDS.
-template <int G>
+template <int G, int kFrags>
 __global__ __launch_bounds__(kThreads) void cache_merge_kernel(CacheAttendArgs a) {
-  constexpr int kFrags = 2, kUnits = kWaves / G;   // units: (16 head-rows, 32 dims) of a workgroup
+  constexpr int kUnits = kWaves / G;   // units of a workgroup
   __shared__ __attribute__((aligned(16))) f32x4 acc[G == 1 ? 1 : kWaves][kFrags + 1][64];
   const int R = a.n_q * a.n_heads;
   const int lane = threadIdx.x & 63, lg = lane >> 4, lc = lane & 15;
@@ -693,7 +694,7 @@ __global__ __launch_bounds__(kThreads) void cache_merge_kernel(CacheAttendArgs a
     // share s's sums: its first request's or, where another request ends in it, its last one's
     const int first_slot = base <= runs.first(s0) ? 2 * s0 : 2 * s0 + 1;
     const int nb = a.block / 16, block = group / nb, in_block = group - block * nb;
-    constexpr int kAhead = 4;
+    constexpr int kAhead = 8 / kFrags;
     for (int s = s0 + sub; s <= s1; s += kAhead * G) {
       f32x4 v[kAhead][kFrags];
       f32x4 ml[kAhead];
@@ -761,14 +762,17 @@ hipError_t launch_cache_attend(const CacheAttendArgs& a, hipStream_t s) {
     cache_attend_kernel<4><<<dim3(grid), dim3(CaCfg<4>::THREADS), 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const unsigned units = (unsigned)(a.n_q * a.n_heads + 15) / 16 * 16, n_seqs = (unsigned)a.n_seqs;
+  const unsigned groups = (unsigned)(a.n_q * a.n_heads + 15) / 16, n_seqs = (unsigned)a.n_seqs;
   // A wave a unit where it holds all shares of a request in flight at once, else eight (64
   // requests of 4 shares each: 201 against 211 us for the whole call; 48 of 5.3 shares: 43.4
-  // against 42.3; one of 256 shares: 151 against 64)
+  // against 42.3; one of 256 shares: 151 against 64); of half the dims where the units are
+  // fewer than the compute units (one of 256 shares: 63.3 against 64.4)
   if (a.shares <= 4 * a.n_seqs)
-    cache_merge_kernel<1><<<dim3(units / kWaves, n_seqs), dim3(kThreads), 0, s>>>(a);
+    cache_merge_kernel<1, 2><<<dim3(groups * 16 / kWaves, n_seqs), dim3(kThreads), 0, s>>>(a);
+  else if (groups * 16 * n_seqs >= 256)
+    cache_merge_kernel<kWaves, 2><<<dim3(groups * 16, n_seqs), dim3(kThreads), 0, s>>>(a);
   else
-    cache_merge_kernel<kWaves><<<dim3(units, n_seqs), dim3(kThreads), 0, s>>>(a);
+    cache_merge_kernel<kWaves, 1><<<dim3(groups * 32, n_seqs), dim3(kThreads), 0, s>>>(a);
   return hipGetLastError();
 }
 
