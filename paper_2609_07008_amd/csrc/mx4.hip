@@ -49,11 +49,12 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(Mx4Args a, int segs
 //   z      through LDS, a step ahead and double-buffered, [slab][row][16 chunks], chunk c of
 //          row r at c ^ z_swz(r)
 // Loaded as fragments, 16 channels or rows a load, either would keep the address unit four
-// times as long (64 clocks a kilobyte): z from memory and no tile past 64 x 16 took 75 us
-// where 32 rows x 7168 -> 16384 now take 24 (weights from memory; 13 at the rate of a copy),
-// and 114 us where 200 x 4096 -> 7168 take 24 (8 at the rate of a large product).  What is
-// left is the conversion of the codes, once a row block, and what a compute unit takes in;
-// one row x 4096 -> 4096 takes 5.7 us, most of it launch and two trips to memory.
+// times as long (64 clocks a kilobyte).  Weights from memory: 32 rows x 7168 -> 16384 take 24
+// to 25 us (75 with z as fragments from memory; 13 at the rate of a copy), 200 x 4096 -> 7168
+// 24 (114; 8 at the rate of a large product), 1 x 4096 -> 4096 5.7, most of it launch and two
+// trips to memory.  What is left is the conversion of the codes, once a row block, and what a
+// compute unit takes in, 15 bytes a clock: twice the waves, z three steps ahead or its loads
+// in another order on each unit leave the times as they are.
 // A 16-byte LDS read is served to lanes 0-3, 12-15, 20-27 of a half wave at once, then to
 // its others: rows 0-3 and 12-15 at one chunk with rows 4-11 at the chunk behind the next
 // four (lane / 16 of the fragment).  With this they lie in all 64 banks.
