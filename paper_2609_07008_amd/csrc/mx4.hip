@@ -65,6 +65,13 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
+// Loads before it are issued before those after it: wait_loads counts on z before the codes
+// of the step after.
+__device__ __forceinline__ void in_order() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 template <int W, int CW, int NB, int MB>
 struct WbCfg {
   static constexpr int KW = W / CW, CL = 8 / KW;      // slabs of a step, classes of a wave
@@ -170,9 +177,9 @@ __global__ __launch_bounds__(64 * W, (WbCfg<W, CW, NB, MB>::WAVES_SIMD)) void wb
     if (t + 1 < steps)
 #pragma unroll
       for (int i = 0; i < C::ZI; ++i) load_z(t + 1, i);
-    __builtin_amdgcn_sched_barrier(0);
+    in_order();
     load_codes(x, t + C::CA);
-    __builtin_amdgcn_sched_barrier(0);
+    in_order();
     const bool whole = (t * KW + kw) * 4 + 3 <= last_group;   // else groups past the end are zero on both sides
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -196,9 +203,9 @@ __global__ __launch_bounds__(64 * W, (WbCfg<W, CW, NB, MB>::WAVES_SIMD)) void wb
   load_codes(even, 0);
 #pragma unroll
   for (int i = 0; i < C::ZI; ++i) load_z(0, i);
-  __builtin_amdgcn_sched_barrier(0);
+  in_order();
   if (C::CA == 2) load_codes(odd, 1);
-  __builtin_amdgcn_sched_barrier(0);
+  in_order();
   for (int t = 0; t < steps; t += 2) {
     step(t, even, acc[0]);
     if (t + 1 < steps) step(t + 1, C::CA == 2 ? odd : even, acc[C::CL - 1]);
