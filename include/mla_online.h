@@ -616,8 +616,8 @@ typedef struct mla_page {
  * step is captured once and replayed as positions and pages change.  The result
  * does not depend on timing: a call gives the same bits again.  The split of a
  * request's keys, and with it the order of its sums, depends on the whole batch.
- * A NaN in a key makes every row NaN that sees it, and may make NaN the rows of
- * the same call and request that come before it.
+ * A NaN in a key makes every row NaN that sees it, and no other: a token's result
+ * does not depend on what keys behind its position hold.
  * n_seqs, n_q, H and the pages' totals fix the workspace.
  * Errors: NULL, SHAPE, UNSUPPORTED, WORKSPACE, HIP.  Kernels only. */
 #define MLA_CACHE_MAX_HEAD_ROWS 16384

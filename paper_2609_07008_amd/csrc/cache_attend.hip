@@ -479,19 +479,46 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
             }
       };
       // Chunk j of a group; lanes of the upper groups take neighbours
-      // swapped, so that a store meets all banks.
-      auto store_chunk = [&](const Codes& x, int buf, int i, int j) {
+      // swapped, so that a store meets all banks.  With a key's first chunk its byte turns into
+      // the scale in place: kept in both forms, one is a copy that waits for its load (231 us
+      // where 205 are, 64 requests of 16k).
+      auto store_chunk = [&](Codes& x, int buf, int i, int j) {
         const uint32_t c = grp >> 1 ? x.c[i][j ^ 1] : x.c[i][j];
-        *(bf16x8 MLA_LDS*)(L + ((buf + sat) ^ (j * 16)) + i * (8 / GW) * C::KBL) = mx4_values(c, mx4_scale(x.s[i]));
+        if (j == 0) x.s[i] = __float_as_uint(mx4_scale(x.s[i]));
+        *(bf16x8 MLA_LDS*)(L + ((buf + sat) ^ (j * 16)) + i * (8 / GW) * C::KBL) = mx4_values(c, __uint_as_float(x.s[i]));
       };
-      auto store_keys = [&](const Codes& x, int buf, int i0) {
+      auto store_keys = [&](Codes& x, int buf, int i0) {
 #pragma unroll
         for (int i = i0; i < NI; ++i)
 #pragma unroll
           for (int j = 0; j < 4; ++j) store_chunk(x, buf, i, j);
       };
+      // A weight of 0 times a value that is NaN or infinite (from scale byte 253 on one may be)
+      // would be NaN in rows that do not see its key: once the scores are taken, such values
+      // become 0.  Rows that see the key have its NaN or infinity from the score.
+      auto has_odd = [&](const Codes& x) {   // of the lane's keys
+        uint32_t top = x.s[0];
+#pragma unroll
+        for (int i = 1; i < NI; ++i) top = top > x.s[i] ? top : x.s[i];
+        return top >= __float_as_uint(mx4_scale(253));
+      };
+      auto drop_odd = [&](int buf) {
+#pragma unroll 1
+        for (int i = 0; i < NI; ++i)
+#pragma unroll 1
+          for (int j = 0; j < 4; ++j) {
+            u32x4 MLA_LDS* at = (u32x4 MLA_LDS*)(L + ((buf + sat) ^ (j * 16)) + i * (8 / GW) * C::KBL);
+            u32x4 v = *at;
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              v[c] &= ((v[c] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((v[c] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
+            *at = v;
+          }
+        asm volatile("" ::: "memory");
+      };
       Tile t = cur.next(a);
       Codes next{};
+      int odd = 0;             // bit 0: the tile to multiply holds such values, bit 1: the one behind it
       int t_max = INT32_MIN;   // the last position of the block's rows
       {
         Codes first;
@@ -511,10 +538,12 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
         lds_barrier();   // the queries have landed
         clear(first, seen_keys(t0, t_max));
         store_keys(first, 0, 0);
+        odd = has_odd(first) ? 1 : 0;
         lds_barrier();   // tile 0 is stored; the queries have left the second tile's place
         if (u0 + 1 < u1) {
           clear(next, seen_keys(t, t_max));
           store_keys(next, C::LAT, 0);
+          odd |= has_odd(next) ? 2 : 0;
         }
       }
       if (u0 + 2 < u1) {
@@ -541,6 +570,7 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
           const bf16x4 vh = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((MLA_LDS bf16x4*)(vp + 2 * C::KBL));
           return __builtin_shufflevector(vl, vh, 0, 1, 2, 3, 4, 5, 6, 7);
         };
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd & 1) != 0, 0)) drop_odd(buf);
         constexpr int VD = 3;
         bf16x8 vt[VD], p[2][NB];
         float mk[C::KW][NB];
@@ -597,7 +627,11 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
           if (f >= ND) store_chunk(next, buf, (f - ND) / 4, f % 4);
         }
         __builtin_amdgcn_s_setprio(0);
-        if (u + 2 < u1) store_keys(next, buf, NI / 2);
+        odd >>= 1;
+        if (u + 2 < u1) {
+          store_keys(next, buf, NI / 2);
+          odd |= has_odd(next) ? 2 : 0;
+        }
         if (u + 3 < u1) {
           t = cur.next(a);
           load_codes(next, t);
