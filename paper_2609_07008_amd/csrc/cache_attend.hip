@@ -406,13 +406,24 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
         }
         const float ref = m_run == -INFINITY ? 0.f : m_run;   // nothing seen yet: every weight is 0
         if (lg == 0) *(float MLA_LDS*)(L + C::M_OFF + ((pb * C::KW + kw) * BM + row) * 4) = m_run;
+        // From 2^23 on a rounded product of score and scale, as the reference is one, is off by more
+        // than half a unit: against the product as it is, weights would pass 2^9 and then the
+        // range.  There the products are rounded like the reference.
+        float scale = a.scale_log2;
+        if (fabsf(ref) >= 8388608.f) {
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[kb][i] *= scale;
+          scale = 1.f;
+        }
         float l = 0.f, r = 0.f;
         u32x2 b[KB];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
           float w[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], a.scale_log2, -ref));
+          for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], scale, -ref));
           l += (w[0] + w[1]) + (w[2] + w[3]);
           b[kb] = u32x2{pack_bf16x2(w[0], w[1]), pack_bf16x2(w[2], w[3])};
           r += (bf16_lo(b[kb][0]) + bf16_hi(b[kb][0])) + (bf16_lo(b[kb][1]) + bf16_hi(b[kb][1]));
