@@ -60,13 +60,15 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(Mx4Args a, int segs
 // four (lane / 16 of the fragment).  With this they lie in all 64 banks.
 __device__ __forceinline__ int z_swz(int r) { return (r & 3) | (r & 8 ? 12 : 0); }
 
+// All but the last N loads of this wave have landed and its LDS accesses are done, then all
+// waves meet: behind it a load may overwrite what any wave has read before.
 template <int N>
-__device__ __forceinline__ void wait_loads() {
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+__device__ __forceinline__ void meet() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// Loads before it are issued before those after it: wait_loads counts on z before the codes
-// of the step after.
+// Loads before it are issued before those after it: meet counts on z before the codes of the
+// step after.
 __device__ __forceinline__ void in_order() {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
@@ -160,9 +162,7 @@ __global__ __launch_bounds__(64 * W, (WbCfg<W, CW, NB, MB>::WAVES_SIMD)) void wb
   unsigned char MLA_LDS* own = L + C::C_OFF + wave * NB * 1024;
   auto step = [&](int t, Codes& x, f32x4 (&sum)[NB][MB]) {
     // z of this step has landed; the next step's codes may be on their way
-    wait_loads<(C::CA - 1) * 2 * NB>();
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
+    meet<(C::CA - 1) * 2 * NB>();
     float scale[NB];
     u32x4 code[NB];
 #pragma unroll
