@@ -329,7 +329,7 @@ def shared_wb(z, w_b, y, stream=None):
 
 # The calls below take tensors on the current device and check what the C ABI cannot see
 # (types, shapes, strides, the device); a refusal raises MlaError like the library's own.
-WB_MX4_MAX_ROWS = 1024   # MLA_WB_MX4_MAX_ROWS
+WB_MAX_D_IN, WB_MX4_MAX_ROWS, WB_MX4_MAX_D_OUT = 16384, 1024, 1 << 24   # MLA_WB_MAX_D_IN, MLA_WB_MX4_MAX_ROWS, MLA_WB_MX4_MAX_D_OUT
 CACHE_ROW_BYTES = 400   # a row of the paged 4-bit cache: 256 code bytes, 16 scales, 64 bf16
 
 

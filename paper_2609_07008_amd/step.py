@@ -138,6 +138,12 @@ class DecodeStep:
         npg, d_model = int(geom.n_proj_groups), int(geom.d_model)
         if npg < 1 or heads % npg or d_model < 1 or d_model % (32 * npg) or d_model % 64:
             raise mla.MlaError(2, f"{heads} heads, d_model {d_model}, {npg} projection groups")
+        if d_model > mla.WB_MAX_D_IN:
+            raise mla.MlaError(3, f"d_model {d_model}; the 4-bit W_b takes up to {mla.WB_MAX_D_IN}")
+        if not 1 <= int(d_out) <= mla.WB_MX4_MAX_D_OUT:
+            raise mla.MlaError(2 if d_out < 1 else 3, f"d_out {d_out}; the 4-bit W_b writes 1 to {mla.WB_MX4_MAX_D_OUT}")
+        if y_dtype not in (torch.bfloat16, torch.float32):
+            raise mla.MlaError(2, f"y_dtype {y_dtype}, expected torch.bfloat16 or torch.float32")
         fields = ("d_latent", "d_rope", "d_model", "n_proj_groups", "softmax_scale", "rope_base")
         self.all_global = SimpleNamespace(n_heads=heads, n_groups=heads, **{f: getattr(geom, f) for f in fields})
         self.info = mla.plan_query(self.all_global, [(0, self.n_rows, 0)], 0, self.n_rows)
