@@ -370,6 +370,11 @@ def _tensor(name, t, dev, dtype, shape=None, rows=False):
         _refuse(f"{name} is not contiguous")
 
 
+def check_tensor(name, t, dtype):
+    """Refuses what is not a contiguous tensor of dtype on the current device."""
+    _tensor(name, t, _device(), dtype)
+
+
 def _row_stride(t) -> int:
     """Elements between rows; of a single row (whose stride is arbitrary) its width rounded up."""
     return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 8) * 8

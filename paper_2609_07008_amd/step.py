@@ -154,6 +154,7 @@ class DecodeStep:
         self.out_o = torch.empty((n_seqs, n_q, heads, d_c), dtype=torch.bfloat16, device=dev)
         self.out_lse = torch.empty((n_seqs, n_q, heads), dtype=torch.float32, device=dev) if with_lse else None
         self.glob_head = np.zeros((heads,), dtype=np.int32)
+        self.w_o_size = heads * d_c * (d_model // npg)   # [n_pg, H / n_pg * d_latent, d_model / n_pg]
         self.all_rows = torch.arange(self.n_rows, dtype=torch.int32, device=dev)
         self.n_prot = torch.full((1,), self.n_rows, dtype=torch.int32, device=dev)
         self.z = torch.empty((self.n_rows, int(geom.d_model)), dtype=torch.bfloat16, device=dev)
@@ -167,6 +168,9 @@ class DecodeStep:
                          workspace=self.ws, stream=stream)
 
     def oproj(self, w_o, stream=None):
+        mla.check_tensor("w_o", w_o, torch.bfloat16)
+        if w_o.numel() != self.w_o_size:
+            raise mla.MlaError(2, f"w_o is {tuple(w_o.shape)}, expected {self.w_o_size} values")
         mla.sliced_oproj_add_planned(self.all_global, self.info, self.out_o, None, self.glob_head, self.all_rows,
                                      self.n_prot, w_o, self.z, self.z, stream)
 

@@ -34,3 +34,35 @@ def test_refused_where_it_is_made(mla, over, monkeypatch):
 def test_made_at_the_edges(mla, over):
     st = _step(**over)
     assert tuple(st.y.shape) == (2, over.get("d_out", 64))
+
+
+BF16 = torch.bfloat16
+W_O = (1, 16 * 512, 256)
+
+
+@pytest.mark.parametrize("w_o", [None, torch.zeros(W_O), torch.zeros((1, 16 * 512, 128), dtype=BF16), torch.zeros((1, 8 * 512, 256), dtype=BF16),
+                                 torch.zeros((1, 16 * 512, 512), dtype=BF16)[..., :256], torch.zeros(0, dtype=BF16)])
+def test_weight_of_the_o_proj(mla, w_o, monkeypatch):
+    """Its address alone reaches the library: type, size and layout are checked here."""
+    st = _step()
+    monkeypatch.setattr(mla, "_device", lambda: -1)      # host tensors count as on the current device
+    monkeypatch.setattr(mla, "sliced_oproj_add_planned", lambda *a: pytest.fail("reached the library"))
+    with pytest.raises(mla.MlaError) as e:
+        st.oproj(w_o)
+    assert "w_o" in str(e.value)
+
+
+def test_weight_of_the_o_proj_on_another_device(mla, monkeypatch):
+    st = _step()
+    monkeypatch.setattr(mla, "_device", lambda: 0)
+    with pytest.raises(mla.MlaError):
+        st.oproj(torch.zeros(W_O, dtype=BF16))
+
+
+@pytest.mark.parametrize("shape", [W_O, (16 * 512, 256), (16, 512, 256)])
+def test_weight_of_the_o_proj_in_any_shape_of_its_size(mla, shape, monkeypatch):
+    st, got = _step(), []
+    monkeypatch.setattr(mla, "_device", lambda: -1)
+    monkeypatch.setattr(mla, "sliced_oproj_add_planned", lambda *a: got.append(a))
+    st.oproj(torch.zeros(shape, dtype=BF16))
+    assert len(got) == 1
