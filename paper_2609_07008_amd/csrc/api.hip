@@ -77,11 +77,6 @@ mla_status check_geom(const mla_geom* g, bool for_oproj) {
   return MLA_OK;
 }
 
-void rope_theta_rev(const mla_geom* g, double* th) {
-  const double two_pi = 6.283185307179586476925286766559;
-  for (int j = 0; j < g->d_rope / 2; ++j) th[j] = std::pow(g->rope_base, -2.0 * j / g->d_rope) / two_pi;
-}
-
 }  // namespace mla
 
 namespace {
@@ -90,7 +85,6 @@ using mla::aligned16;
 using mla::check_geom;
 using mla::fail;
 using mla::hip_fail;
-using mla::rope_theta_rev;
 
 // width of one head output: the latent, plus the RoPE dims when the value is rotary
 int32_t head_dv(const mla_geom* g) { return g->d_latent + (g->value_rope ? g->d_rope : 0); }
@@ -209,6 +203,12 @@ void segment_tables(const mla_geom* g, const mla_segment* segs, int32_t n_segs, 
     if (!offline) cum += (int64_t)G * T->info[i].length * T->info[i].n_chunks;
   }
   T->global_parts = cum;
+}
+
+// RoPE frequencies in revolutions: base^(-2j/d_r) / (2 pi)
+void rope_theta_rev(const mla_geom* g, double* th) {
+  const double two_pi = 6.283185307179586476925286766559;
+  for (int j = 0; j < g->d_rope / 2; ++j) th[j] = std::pow(g->rope_base, -2.0 * j / g->d_rope) / two_pi;
 }
 
 // offline: the producer's plan (Alg. 1) -- every segment sees only itself, and

@@ -14,7 +14,4 @@ inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 
 
 mla_status check_geom(const mla_geom* g, bool for_oproj);
 
-// RoPE frequencies in revolutions: base^(-2j/d_r) / (2 pi)
-void rope_theta_rev(const mla_geom* g, double* th);
-
 }  // namespace mla
