@@ -97,7 +97,7 @@ mla_status check_mx4(int64_t n_rows, int32_t n_cols, const void* x, int64_t x_st
 // How mla_cache_attend splits its work, and its workspace
 struct AttendSplit {
   int32_t block, n_blocks, shares;
-  int64_t off_ml, off_o;
+  int64_t off_long, off_ml, off_o;
   size_t total;
 };
 
@@ -115,13 +115,13 @@ mla_status attend_split(const mla_geom* geom, int32_t n_seqs, int32_t n_q, int32
     return fail(MLA_ERR_UNSUPPORTED, "n_q * n_heads = %lld; built: up to %d", (long long)rows, MLA_CACHE_MAX_HEAD_ROWS);
   if ((int64_t)n_seqs * max_pages > INT32_MAX / (page_rows / mla::kCacheTile))
     return fail(MLA_ERR_UNSUPPORTED, "n_seqs * max_pages = %lld: too many tiles", (long long)n_seqs * max_pages);
-  constexpr int32_t kUnits = 256;
   S->block = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
   S->n_blocks = (int32_t)((rows + S->block - 1) / S->block);
-  S->shares = std::max(1, kUnits / S->n_blocks);
+  S->shares = std::max(1, mla::kMaxShares / S->n_blocks);
   auto up = [](int64_t x) { return (x + 255) / 256 * 256; };
   const int64_t part_rows = (int64_t)2 * S->shares * S->n_blocks * S->block;
-  S->off_ml = up(((int64_t)n_seqs + 1) * 4);
+  S->off_long = up(((int64_t)n_seqs + 1) * 4);
+  S->off_ml = S->off_long + up(mla::kMaxShares / mla::kLongShares * 4);
   S->off_o = S->off_ml + up(part_rows * 4 * 4);
   S->total = (size_t)(S->off_o + part_rows * 512 * 4);
   return MLA_OK;
@@ -240,6 +240,7 @@ mla_status mla_cache_attend(const mla_geom* geom, int32_t n_seqs, int32_t n_q, c
   a.out_o = reinterpret_cast<uint16_t*>(out_o);
   a.out_lse = out_lse;
   a.tile_base = reinterpret_cast<int32_t*>(W);
+  a.long_seq = reinterpret_cast<int32_t*>(W + S.off_long);
   a.part_ml = reinterpret_cast<float*>(W + S.off_ml);
   a.part_o = reinterpret_cast<float*>(W + S.off_o);
   a.n_seqs = n_seqs;

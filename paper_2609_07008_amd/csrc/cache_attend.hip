@@ -24,7 +24,7 @@
 //
 // Work is split by tiles, not by requests: the batch's tiles, in order, form `shares`
 // equal runs, one a workgroup (and head-row block).  A request inside one run is written
-// at once; one that crosses runs leaves sums to cache_merge_kernel.
+// at once; one that crosses runs leaves sums to the joining kernels.
 //
 // Measured, whole calls with the joining: 64 requests of ~16k keys (18,474 tiles), 64 heads
 // 200 to 212 us, 2.5 us a tile and compute unit; a tile's products keep the matrix cores
@@ -40,9 +40,11 @@
 namespace mla {
 namespace {
 
-constexpr int kWaves = 8, kThreads = kWaves * 64;   // of cache_merge_kernel
+constexpr int kWaves = 8, kThreads = kWaves * 64;   // of the joining kernels
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kLong = kLongShares;   // see cache_merge_mixed_kernel
 
 template <int NB>
 struct CaCfg {
@@ -233,6 +235,7 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
       if (lane >= o) inc += v;
     }
     if (lane == 63) sums[wave] = inc;
+    if (blockIdx.x == 0 && tid < kMaxShares / kLong) a.long_seq[tid] = -1;
     __syncthreads();
     int before = 0;
     total = 0;
@@ -243,11 +246,18 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
       total += v;
     }
     int base = before + inc - mine;
-    const int lo = Runs(a, total).first(share);   // total is the same in all lanes
+    const Runs runs(a, total);   // total is the same in all lanes
+    const int lo = runs.first(share);
     const bool writes = blockIdx.x == 0;
     for (int b = b0; b < b1; ++b) {
       const int n = per == 1 ? mine : tiles_of(a, b);
-      if (writes) a.tile_base[b] = base;
+      if (writes) {
+        a.tile_base[b] = base;
+        if (n > kLong && n > (int64_t)(kLong - 1) * runs.q) {
+          const int s0 = runs.share(base), s1 = runs.share(base + n - 1);
+          if (s1 - s0 >= kLong) a.long_seq[(s0 + kLong - 1) / kLong] = b;   // at the first kLong-th share that it has
+        }
+      }
       if (lo >= base && lo < base + n) {
         sums[16] = b;
         sums[17] = base;
@@ -712,17 +722,18 @@ __global__ __launch_bounds__(CaCfg<NB>::THREADS, CaCfg<NB>::WAVES / 4) void cach
   }
 }
 
-// Joins the sums of requests that several shares hold (and writes those without a tile).
-// A wave takes 16 head-rows and 16 kFrags dims, the fragments that the sums are kept in,
-// and every G-th share; G waves of a workgroup join their sums through LDS.
+template <int kFrags>
+using Joined = f32x4[kFrags + 1][64];   // a wave's sums in LDS
+
+// Joins the sums of requests that several shares hold (and writes those without a tile).  A
+// unit is 16 head-rows and 16 kFrags dims, the fragments that the sums are kept in; a wave
+// takes every G-th share of it, and G waves of a workgroup join their sums through LDS.
+// Requests of more than `most` shares are left out.
 template <int G, int kFrags>
-__global__ __launch_bounds__(kThreads) void cache_merge_kernel(CacheAttendArgs a) {
-  constexpr int kUnits = kWaves / G;   // units of a workgroup
-  __shared__ __attribute__((aligned(16))) f32x4 acc[G == 1 ? 1 : kWaves][kFrags + 1][64];
+__device__ __forceinline__ void join_unit(const CacheAttendArgs& a, int b, int unit, int most, Joined<kFrags>* acc) {
   const int R = a.n_q * a.n_heads;
   const int lane = threadIdx.x & 63, lg = lane >> 4, lc = lane & 15;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int b = blockIdx.y, unit = blockIdx.x * kUnits + wave / G, sub = wave % G;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sub = wave % G;
   const int group = unit / (32 / kFrags), frag = unit % (32 / kFrags) * kFrags;   // 16 head-rows; first fragment
   const int base = a.tile_base[b], n = a.tile_base[b + 1] - base;
   const int row = group * 16 + lc;
@@ -735,7 +746,7 @@ __global__ __launch_bounds__(kThreads) void cache_merge_kernel(CacheAttendArgs a
   if (n > 0) {
     const Runs runs(a, a.tile_base[a.n_seqs]);
     const int s0 = runs.share(base), s1 = runs.share(base + n - 1);
-    if (s0 == s1) return;
+    if (s0 == s1 || s1 - s0 >= most) return;
     // share s's sums: its first request's or, where another request ends in it, its last one's
     const int first_slot = base <= runs.first(s0) ? 2 * s0 : 2 * s0 + 1;
     const int nb = a.block / 16, block = group / nb, in_block = group - block * nb;
@@ -795,6 +806,29 @@ __global__ __launch_bounds__(kThreads) void cache_merge_kernel(CacheAttendArgs a
     a.out_lse[at] = l == 0.f ? -INFINITY : (m + __log2f(l)) * 0.6931471805599453f;
 }
 
+// All waves of a workgroup on one unit
+template <int kFrags>
+__global__ __launch_bounds__(kThreads) void cache_merge_kernel(CacheAttendArgs a) {
+  __shared__ __attribute__((aligned(16))) Joined<kFrags> acc[kWaves];
+  join_unit<kWaves, kFrags>(a, blockIdx.y, blockIdx.x, INT32_MAX, acc);
+}
+
+// A row of workgroups a request, a wave a unit of it, for requests of up to `most` shares; in
+// the rows behind, all waves of a workgroup on a unit of a longer one, of which there is one at
+// most for every kLong-th share (the attention's kernel says which).
+constexpr int kMixFrags = 2, kMixUnits = 32 / kMixFrags;   // units of 16 head-rows
+__global__ __launch_bounds__(kThreads) void cache_merge_mixed_kernel(CacheAttendArgs a, int most) {
+  __shared__ __attribute__((aligned(16))) Joined<kMixFrags> acc[kWaves];
+  if ((int)blockIdx.y < a.n_seqs) {
+    join_unit<1, kMixFrags>(a, blockIdx.y, blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), most, acc);
+    return;
+  }
+  const int units = gridDim.x * kWaves, at = ((int)blockIdx.y - a.n_seqs) * gridDim.x + blockIdx.x, k = at / units;
+  if (k * kLong >= a.shares) return;
+  const int b = __builtin_amdgcn_readfirstlane(a.long_seq[k]);
+  if (b >= 0) join_unit<kWaves, kMixFrags>(a, b, at % units, INT32_MAX, acc);
+}
+
 }  // namespace
 
 hipError_t launch_cache_attend(const CacheAttendArgs& a, hipStream_t s) {
@@ -810,14 +844,22 @@ hipError_t launch_cache_attend(const CacheAttendArgs& a, hipStream_t s) {
   const unsigned groups = (unsigned)(a.n_q * a.n_heads + 15) / 16, n_seqs = (unsigned)a.n_seqs;
   // A wave a unit where it holds all shares of a request in flight at once, else eight (64
   // requests of 4 shares each: 201 against 211 us for the whole call; 48 of 5.3 shares: 43.4
-  // against 42.3; one of 256 shares: 151 against 64); of half the dims where the units are
-  // fewer than the compute units (one of 256 shares: 63.3 against 64.4)
-  if (a.shares <= 4 * a.n_seqs)
-    cache_merge_kernel<1, 2><<<dim3(groups * 16 / kWaves, n_seqs), dim3(kThreads), 0, s>>>(a);
-  else if (groups * 16 * n_seqs >= 256)
-    cache_merge_kernel<kWaves, 2><<<dim3(groups * 16, n_seqs), dim3(kThreads), 0, s>>>(a);
-  else
-    cache_merge_kernel<kWaves, 1><<<dim3(groups * 32, n_seqs), dim3(kThreads), 0, s>>>(a);
+  // against 42.3; one of 256 shares: 151 against 64).  How the shares fall to the requests is
+  // known on the device alone: with up to four on average, rows of workgroups behind the
+  // requests' take those of more than kLong (one of 264k keys among 63 of 400 keys: 87 us, 166
+  // with a wave a unit; with kLong 8 and 16 it is the same within a twentieth, and more
+  // workgroups find no work in other batches).  Where the grid holds no row more, a wave a unit.
+  // Of half the dims where the units are fewer than the compute units (one of 256 shares: 63.3
+  // against 64.4).
+  if (a.shares <= 4 * a.n_seqs) {
+    const unsigned rows = a.shares > kLong ? (unsigned)(a.shares + kLong - 1) / kLong * kWaves : 0;
+    const bool fits = n_seqs + rows <= 65535;
+    cache_merge_mixed_kernel<<<dim3(groups * kMixUnits / kWaves, n_seqs + (fits ? rows : 0)), dim3(kThreads), 0, s>>>(a, fits ? kLong : INT32_MAX);
+  } else if (groups * 16 * n_seqs >= 256) {
+    cache_merge_kernel<2><<<dim3(groups * 16, n_seqs), dim3(kThreads), 0, s>>>(a);
+  } else {
+    cache_merge_kernel<1><<<dim3(groups * 32, n_seqs), dim3(kThreads), 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 

@@ -108,6 +108,9 @@ struct CacheRowsArgs {
 hipError_t launch_cache_append(const CacheRowsArgs& a, hipStream_t s);
 hipError_t launch_cache_gather(const CacheRowsArgs& a, hipStream_t s);
 
+constexpr int kMaxShares = 256;   // of the attention's work: a workgroup a compute unit
+constexpr int kLongShares = 32;   // a request that more shares than this hold is joined by whole workgroups
+
 struct CacheAttendArgs {
   const unsigned char* cache;
   const uint16_t* q;          // [n_seqs, n_q, n_heads, 576] bf16
@@ -119,6 +122,7 @@ struct CacheAttendArgs {
   float* part_o;              // [2 shares, n_blocks, block / 16, 32, 64, 4]: sums of a request that several shares hold, as 16-dim fragments
   float* part_ml;             // [2 shares, n_blocks, block, 4]: reference (log2 units), row sums of the weights and of their bf16 values
   int32_t* tile_base;         // [n_seqs + 1]: tiles before each request
+  int32_t* long_seq;          // [kMaxShares / kLongShares], k: the request of more than kLongShares shares whose first share of an index kLongShares divides is kLongShares k, or -1
   int32_t n_seqs, n_q, n_heads;
   int32_t max_pages, page_rows, cache_pages;
   int32_t page_tiles;         // page_rows in tiles
