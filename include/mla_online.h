@@ -493,7 +493,8 @@ mla_status mla_shared_wb(int64_t n_rows, int32_t d_in, int32_t d_out, const void
  * values; a value is an e2m1 code (sign, and 0 0.5 1 1.5 2 3 4 6) times its
  * group's scale.  Codes are two a byte, the even value in the low nibble; a scale
  * is one byte e that stands for 2^(e - 127), and e = 255 makes its group NaN.
- * What a code stands for is exact in bf16.
+ * What a code stands for is exact in bf16, and infinite where it passes the type's
+ * range: values of 1.75 x 2^127 and more come back so.
  *
  * mla_mx4_quantize: bf16 values to codes and scales.  The scale is
  * 2^(floor(log2 max|x|) - 2), one power more where max|x| is 7 times it or more;
@@ -518,8 +519,11 @@ mla_status mla_mx4_dequantize(int64_t n_rows, int32_t n_cols, const void* codes,
                               int64_t x_stride, void* stream);
 
 /* y = W_b z as mla_shared_wb, with W_b in mx4, for the rows of a decode step or a
- * chunk of new tokens: at most MLA_WB_MX4_MAX_ROWS (more rows are bound by the
- * matrix cores, not by the weight: dequantize once and call mla_shared_wb).
+ * chunk of new tokens: at most MLA_WB_MX4_MAX_ROWS.  Many rows are bound by the
+ * matrix cores, not by the weight: above about 500, mla_mx4_dequantize and
+ * mla_shared_wb together take less time (512 x 4096 -> 4096 26 us against 35, 1024
+ * 53 against 43; 400 x 4096 -> 7168 46 against 48, 512 50 against 48), and with the
+ * dequantized weight kept, mla_shared_wb does from about 200 to 400 rows on.
  * Products and sums as in mla_shared_wb (bf16 MFMA, fp32 sums), in an order that
  * depends on d_in alone: a row of z gives the same bits in any call.
  *   n_rows, d_in, d_out  as for mla_shared_wb (d_in up to MLA_WB_MAX_D_IN, d_out up
@@ -604,7 +608,9 @@ typedef struct mla_page {
  *   pages      device [n_seqs, max_pages], 16-byte aligned: the requests' pages in
  *              any order; a key at position p is seen iff p <= t, so rows allocated
  *              but not yet written need no mark (their contents do not matter)
- *   seq_pages  device int32 [n_seqs]: entries in use (clamped to [0, max_pages])
+ *   seq_pages  device int32 [n_seqs]: entries in use (clamped to [0, max_pages]); 0
+ *              for a padded request: entries are read and scored whether or not a
+ *              token sees a key of theirs
  *   cache_pages, page_rows, cache   as for mla_cache_append
  *   out_o      device bf16 [n_seqs, n_q, H, d_latent], 16-byte aligned: 0 where a
  *              token sees no key
@@ -618,7 +624,14 @@ typedef struct mla_page {
  * request's keys, and with it the order of its sums, depends on the whole batch.
  * A NaN in a key makes every row NaN that sees it, and no other: a token's result
  * does not depend on what keys behind its position hold.
- * n_seqs, n_q, H and the pages' totals fix the workspace.
+ * Precision: scores and sums in 32 bits, the RoPE part of the turned query in two
+ * bf16 terms, softmax weights in bf16 (half a step of each, as wide as the output's
+ * own rounding) for the product with the values, whose sum is divided by the sum of
+ * the same weights.  Next to 64 bits that is 0.0017 to 0.0021 of the output's size,
+ * of which its rounding to bf16 alone is 0.0017.
+ * n_seqs, n_q and H fix the workspace: 17 MB for up to 16 head-rows n_q H, 34 MB up
+ * to 32 and up to 68 MB above, for the sums of requests that workgroups share,
+ * and four bytes a request.
  * Errors: NULL, SHAPE, UNSUPPORTED, WORKSPACE, HIP.  Kernels only. */
 #define MLA_CACHE_MAX_HEAD_ROWS 16384
 mla_status mla_cache_attend_query(const mla_geom* geom, int32_t n_seqs, int32_t n_q, int32_t max_pages, int32_t page_rows,

@@ -26,13 +26,18 @@
 // equal runs, one a workgroup (and head-row block).  A request inside one run is written
 // at once; one that crosses runs leaves sums to the joining kernels.
 //
-// Measured, whole calls with the joining: 64 requests of ~16k keys (18,474 tiles), 64 heads
-// 200 to 212 us, 2.5 us a tile and compute unit; a tile's products keep the matrix cores
+// Measured, whole calls with the joining, by card: 64 requests of ~16k keys (18,474 tiles), 64
+// heads 200 to 215 us, 2.5 us a tile and compute unit; a tile's products keep the matrix cores
 // busy 2300 of its 5000 clocks, its LDS traffic takes 2600, its vector instructions 2100: the
-// two kinds of waves hide each other only in part.  16 requests of ~8k, 256 head-rows 85 us;
-// one of 264k, 64 heads 65 us.  48 of ~6k, 16 heads 41 us, of which 8 are the start (three
-// dependent reads from memory before the first tile) and 5 the joining: there the
-// conversion bounds a tile, and eight value waves against four take 41.4 against 43.5.
+// two kinds of waves hide each other only in part (207 us; without the latent's score products
+// and their reads 174, without the value products 186, without softmax or conversion 203 to 206,
+// all keys from one page 190 of 215).  16 requests of ~8k, 256 head-rows 85 to 89 us; one of
+// 264k, 64 heads 63 to 66.  48 of ~6k, 16 heads 41 to 43, and 46 to 47 where other calls have
+// used the last-level cache in between; 8 of it are the start (three dependent reads from
+// memory before the first tile) and 5 the joining.  No part alone bounds a tile there (without
+// conversion 40.5 of 41.3, score products 39.2, value products 38.5): what is left is the way
+// through one from barrier to barrier, and eight value waves against four take 41.4 against
+// 43.5.
 #include "mx4.h"
 
 #include <algorithm>
