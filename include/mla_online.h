@@ -523,7 +523,7 @@ mla_status mla_mx4_dequantize(int64_t n_rows, int32_t n_cols, const void* codes,
  * matrix cores, not by the weight: above about 500, mla_mx4_dequantize and
  * mla_shared_wb together take less time (512 x 4096 -> 4096 26 us against 35, 1024
  * 53 against 43; 400 x 4096 -> 7168 46 against 48, 512 50 against 48), and with the
- * dequantized weight kept, mla_shared_wb does from about 200 to 400 rows on.
+ * dequantized weight kept, mla_shared_wb does from 200 to 600 rows on, by shape.
  * Products and sums as in mla_shared_wb (bf16 MFMA, fp32 sums), in an order that
  * depends on d_in alone: a row of z gives the same bits in any call.
  *   n_rows, d_in, d_out  as for mla_shared_wb (d_in up to MLA_WB_MAX_D_IN, d_out up

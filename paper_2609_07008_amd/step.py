@@ -180,7 +180,9 @@ class DecodeStep:
     def run(self, kv, slots, q, pos, pages, seq_pages, cache, w_o, wb_codes, wb_scales, turn=None, stream=None):
         """kv [n_rows, D] bfloat16, slots [n_rows] int32, q [n_seqs, n_q, H, D], pos [n_seqs,
         n_q] int32; turn [n_rows] int32: each row's position in its page's RoPE frame (pos
-        where the frame is 0).  Returns y [n_rows, d_out]."""
+        where the frame is 0).  Returns y [n_rows, d_out].  Every call checks its own
+        arguments: where one refuses, those before it have run, and the append of the same
+        rows may be repeated."""
         self.append(kv, slots, cache, pos.view(-1) if turn is None else turn, stream)
         self.attend(q, pos, pages, seq_pages, cache, stream)
         self.oproj(w_o, stream)
