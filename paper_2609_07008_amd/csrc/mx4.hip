@@ -295,7 +295,7 @@ hipError_t launch_wb_mx4(const WbMx4Args& a, hipStream_t s) {
   // take 24 us in 64 x 128 (224 workgroups) and 28 in 64 x 64 (448), 128 rows 25 and 18.
   // Of all tiles at 1 to 200 rows and 512 to 16384 channels, the rule's is the fastest or, at
   // d_in = 1024 and 4096, within 6 % of it; at 512 and 16384 within 14 % (1 x 16384 -> 16384 39.6
-  // us, in 16 x 32 34.9), at 128 within 0.7 us.
+  // us, in 16 x 32 34.9), at 128 within 0.9 us.
   struct Tile {
     int rows, channels;
     hipError_t (*launch)(const WbMx4Args&, hipStream_t);
