@@ -17,7 +17,8 @@
  *      added) on protected rows (RestoreAndReplace, eq:factorization).
  * Beside the step the library exports the offline producer of the artifact
  * (Alg. 1), the protected token-row set (eq:protected), the shared second
- * projection y = W_b z and the adaptive MoE fanout (eq:moe).
+ * projection y = W_b z, the adaptive MoE fanout (eq:moe), and an MoE layer's router
+ * and experts.
  *
  * Conventions (all entry points):
  *  - Host arrays are read during the call only.  Device arrays are owned by the
@@ -33,7 +34,7 @@
  *    slot waits for the copy that last read it, so a third back-to-back call
  *    may block the host until the first call's copy has run.  Every other
  *    call only enqueues kernels and never blocks.
- *  - HIP graph capture: the merge, o-proj, W_b, MoE, 4-bit and cache calls and the
+ *  - HIP graph capture: the merge, o-proj, W_b, MoE, 4-bit, 8-bit and cache calls and the
  *    planned protected-set, attend and o-proj calls enqueue kernels only (no memset
  *    or memcpy nodes) and may be captured.  The calls that upload a plan return
  *    MLA_ERR_UNSUPPORTED on a capturing stream, before enqueueing anything: their staging buffer is
@@ -641,6 +642,145 @@ mla_status mla_cache_attend(const mla_geom* geom, int32_t n_seqs, int32_t n_q, c
                             const mla_page* pages, const int32_t* seq_pages, int32_t max_pages, int64_t cache_pages,
                             int32_t page_rows, const void* cache, void* out_o, float* out_lse, void* workspace,
                             size_t ws_bytes, void* stream);
+
+/* ----------------------------------------------------------------------------
+ * mla_moe_route -- the experts of every token row from the router's logits l, ready
+ * for mla_moe_experts_i8.  Scores s are the softmax of the row or the sigmoid of each
+ * logit; c = s + bias chooses (a bias for balance changes who is chosen, not the
+ * weights):
+ *   1. the experts lie in n_groups groups of consecutive ones; a group scores the sum
+ *      of its group_best largest c; the top_groups best groups stay (equal scores: the
+ *      lower group);
+ *   2. of their experts the top_k with the largest c, in that order (equal c: the lower
+ *      index).  Without a bias the order is that of the logits;
+ *   3. weights w_j = s of rank j, divided by their sum if `renormalize` (where the sum is
+ *      0 they stay 0), times `scale`;
+ *   4. the adaptive fanout K = min{k in [min_k, top_k] : sum_{j<=k} s_j >= tau sum_j s_j}
+ *      (eq:moe), top_k where no k qualifies or the sum is not positive.  tau > 1 (or
+ *      min_k = top_k) keeps all.
+ * Choices and fanouts are those of scores in 64 bits, so that neighbours in rank a
+ * rounding apart come out in their order; weights are within 2^-20 of their value.
+ * A NaN never ranks before a number; a row with a NaN or a +infinity has NaN softmax
+ * scores (its order stays that of the logits), a row of -infinity alone has scores 0.
+ * An expert with bias -infinity is chosen only where nothing else is left.
+ *
+ *   n_rows, n_experts   N token rows, E experts (top_k <= E <= 1024)
+ *   logits        device [N, E] f32 or bf16 (logits_dtype), rows logits_stride elements
+ *                 apart (at least E), aligned to their type
+ *   bias          device f32 [E] or NULL
+ *   cfg           host; n_groups divides E (at most 64 groups), top_groups groups hold
+ *                 top_k experts, group_best 1 or 2, 1 <= min_k <= top_k <= 8
+ *   expert_idx    device int32 [N, top_k], written
+ *   expert_w      device f32 [N, top_k], written
+ *   fanout        device int32 [N] or NULL (all top_k), written
+ *   expert_count  device int32 [E] or NULL: written with the rows that execute each
+ *                 expert (rank < K)
+ * Device arrays 4-byte aligned.  Errors: NULL, SHAPE, UNSUPPORTED, HIP.  Kernels only:
+ * may be captured.
+ * ------------------------------------------------------------------------- */
+typedef enum mla_scoring { MLA_SOFTMAX = 0, MLA_SIGMOID = 1 } mla_scoring;
+
+typedef struct mla_route_cfg {
+  int32_t scoring;       /* mla_scoring                                        */
+  int32_t n_groups;      /* 1: no groups                                       */
+  int32_t top_groups;    /* groups that a row may use                          */
+  int32_t group_best;    /* largest c summed for a group's score: 1 or 2       */
+  int32_t top_k;
+  int32_t min_k;         /* least fanout                                       */
+  int32_t renormalize;   /* nonzero: weights are divided by their sum          */
+  float scale;           /* factor of the weights (finite)                     */
+  float tau;             /* the fanout threshold (not NaN)                     */
+} mla_route_cfg;
+
+mla_status mla_moe_route(int64_t n_rows, int32_t n_experts, const void* logits, int32_t logits_dtype, int64_t logits_stride,
+                         const float* bias, const mla_route_cfg* cfg, int32_t* expert_idx, float* expert_w, int32_t* fanout,
+                         int32_t* expert_count, void* stream);
+
+/* ----------------------------------------------------------------------------
+ * Rows in 8-bit integers: a row x (a token, or an output channel's weights) is codes
+ * q = round(127 x / max|x|), ties to even, and the scale max|x| / 127; a code stands for
+ * q * scale.  Codes do not depend on the machine.  A row of zeros has scale 0; a row with
+ * a NaN or an infinity has scale NaN and codes 0.  A scale below 2^-126 (max|x| below
+ * 1.5e-36) has fewer bits than others, as f32 has there.
+ *
+ * mla_i8_quantize: bf16 rows to codes and scales.  mla_i8_dequantize: back to bf16.
+ *   n_rows, n_cols  N rows (>= 0) of n_cols values (a multiple of 16, at most
+ *                   MLA_I8_MAX_COLS)
+ *   x               device bf16 [N, n_cols], rows x_stride elements apart (a multiple of 8,
+ *                   at least n_cols), 16-byte aligned
+ *   codes           device int8 [N, n_cols], 16-byte aligned
+ *   scales          device f32 [N]
+ * Errors: NULL, SHAPE, UNSUPPORTED, HIP.  Kernels only: may be captured.
+ * ------------------------------------------------------------------------- */
+#define MLA_I8_MAX_COLS 16384
+mla_status mla_i8_quantize(int64_t n_rows, int32_t n_cols, const void* x, int64_t x_stride, void* codes, float* scales, void* stream);
+
+mla_status mla_i8_dequantize(int64_t n_rows, int32_t n_cols, const void* codes, const float* scales, void* x, int64_t x_stride,
+                             void* stream);
+
+/* y = W_b z as mla_shared_wb, both sides in 8 bits: a row of z has a scale, and so has an
+ * output channel.  The sum of a product of codes is exact in i32 (d_in at most 16384);
+ * y = (sum * w_scale) * z_scale in f32, rounded once more to a bf16 y.  Any number of rows;
+ * a row of z gives the same bits in any call.
+ *   n_rows, d_in, d_out  as for mla_shared_wb (d_out up to MLA_WB_I8_MAX_D_OUT)
+ *   z_codes, z_scales    device int8 [N, d_in] (16-byte aligned), f32 [N]
+ *   w_codes, w_scales    device int8 [d_out, d_in] (16-byte aligned), f32 [d_out]
+ *   out_dtype, y         as for mla_shared_wb
+ * Errors: NULL, SHAPE, UNSUPPORTED, HIP.  Kernels only: may be captured. */
+#define MLA_WB_I8_MAX_D_OUT 16777216
+mla_status mla_shared_wb_i8(int64_t n_rows, int32_t d_in, int32_t d_out, const void* z_codes, const float* z_scales,
+                            const void* w_codes, const float* w_scales, int32_t out_dtype, void* y, void* stream);
+
+/* ----------------------------------------------------------------------------
+ * mla_moe_experts_i8 -- the experts of a mixture-of-experts layer in 8-bit integers, for
+ * every token row the first fanout of its experts (mla_moe_route, or mla_moe_fanout's
+ * ranks):
+ *   y_n = sum_{j < K_n} w_nj W_down[e] h_nj,   e = expert_idx[n, j] - first_expert,
+ *   h_nj = silu(W_gate[e] x_n) * (W_up[e] x_n),   silu(g) = g / (1 + exp(-g))
+ * x is quantized a row as mla_i8_quantize does, h is rounded to bf16 and then quantized a
+ * row; sums of products are exact in i32 and scaled as in mla_shared_wb_i8; the pairs of
+ * a token are summed in f32 in rank order.  A row's result does not depend on the other
+ * rows, and a call gives the same bits again.
+ *
+ * A device may hold a share of the experts, [first_expert, first_expert + n_experts):
+ * pairs of others add nothing (y of the devices is then summed by the caller; MLA_F32
+ * keeps such sums unrounded), and neither do indexes outside the layer (-1: a padded
+ * row, y = 0).  An expert may be given twice in a row and counts twice.
+ *   layer        host: d_model, d_ffn multiples of 64 up to MLA_I8_MAX_COLS; n_experts
+ *                here (1 .. 1024); first_expert >= 0; top_k columns of expert_idx (1 .. 16:
+ *                a caller may append experts that every row uses)
+ *   n_rows       N (>= 0); N * top_k at most MLA_EXPERTS_MAX_PAIRS
+ *   x            device bf16 [N, d_model], rows x_stride elements apart (a multiple of 8, at
+ *                least d_model), 16-byte aligned
+ *   expert_idx, expert_w   device int32, f32 [N, top_k]
+ *   fanout       device int32 [N] or NULL: experts of each row (values past top_k: all,
+ *                below 1: none)
+ *   w_gate_up, s_gate_up   device int8 [n_experts, 2 d_ffn, d_model] (d_ffn rows of the gate,
+ *                then d_ffn of up), f32 [n_experts, 2 d_ffn]; 16-byte aligned
+ *   w_down, s_down         device int8 [n_experts, d_model, d_ffn], f32 [n_experts, d_model];
+ *                16-byte aligned
+ *   out_dtype, y           MLA_BF16 or MLA_F32; device [N, d_model], 16-byte aligned, every
+ *                row written
+ *   workspace    device, 256-byte aligned, mla_moe_experts_i8_query bytes; overwritten (calls
+ *                that may overlap need one each)
+ * Everything that changes from call to call is read on the device.  Errors: NULL, SHAPE,
+ * UNSUPPORTED, WORKSPACE, HIP.  Kernels only: may be captured.
+ * ------------------------------------------------------------------------- */
+#define MLA_EXPERTS_MAX_PAIRS 16777216
+typedef struct mla_moe_layer {
+  int32_t d_model;
+  int32_t d_ffn;
+  int32_t n_experts;
+  int32_t first_expert;
+  int32_t top_k;
+} mla_moe_layer;
+
+mla_status mla_moe_experts_i8_query(const mla_moe_layer* layer, int64_t n_rows, int32_t out_dtype, size_t* ws_bytes);
+
+mla_status mla_moe_experts_i8(const mla_moe_layer* layer, int64_t n_rows, const void* x, int64_t x_stride, const int32_t* expert_idx,
+                              const float* expert_w, const int32_t* fanout, const void* w_gate_up, const float* s_gate_up,
+                              const void* w_down, const float* s_down, int32_t out_dtype, void* y, void* workspace, size_t ws_bytes,
+                              void* stream);
 
 /* Static description of a status code. */
 const char* mla_status_str(mla_status s);

@@ -22,5 +22,8 @@ struct MoeArgs {
 };
 
 hipError_t launch_moe_fanout(const MoeArgs& a, hipStream_t s);
+// adds to expert_count (zeroed before) the rows that execute each expert, from expert_idx and
+// fanout (null: all top_k ranks)
+hipError_t launch_moe_count(const MoeArgs& a, hipStream_t s);
 
 }  // namespace mla

@@ -387,7 +387,7 @@ __global__ __launch_bounds__(256) void moe_count_kernel(MoeArgs a) {
   for (int i = threadIdx.x; i < E; i += 256) hist[i] = 0;
   __syncthreads();
   for (int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x; r < a.n_rows; r += (int64_t)gridDim.x * 256) {
-    const int K = a.fanout[r];
+    const int K = a.fanout != nullptr ? a.fanout[r] : TK;
     for (int j = 0; j < TK; ++j) {
       const int32_t e = a.expert_idx[r * TK + j];
       if (j < K && (uint32_t)e < (uint32_t)E) atomicAdd(&hist[e], 1u);
@@ -433,12 +433,13 @@ hipError_t launch_moe_fanout(const MoeArgs& a, hipStream_t s) {
   else if (E <= 512) moe_fanout_wave_kernel<8><<<grid(1), blk, 0, s>>>(a);
   else moe_fanout_wave_kernel<16><<<grid(1), blk, 0, s>>>(a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (a.expert_count != nullptr) {
-    const unsigned cblocks = (unsigned)std::min<int64_t>((a.n_rows + 1023) / 1024, 256);
-    moe_count_kernel<<<dim3(cblocks), dim3(256), 0, s>>>(a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  return hipSuccess;
+  return a.expert_count != nullptr ? launch_moe_count(a, s) : hipSuccess;
+}
+
+hipError_t launch_moe_count(const MoeArgs& a, hipStream_t s) {
+  const unsigned cblocks = (unsigned)std::min<int64_t>((a.n_rows + 1023) / 1024, 256);
+  moe_count_kernel<<<dim3(cblocks), dim3(256), 0, s>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace mla

@@ -26,7 +26,8 @@ EXPORTS = ("mla_online_attend_query", "mla_online_attend", "mla_segment_merge", 
            "mla_protected_rows_planned_query", "mla_protected_rows_planned",
            "mla_moe_fanout", "mla_shared_wb", "mla_mx4_quantize", "mla_mx4_dequantize", "mla_shared_wb_mx4",
            "mla_cache_append", "mla_cache_gather", "mla_cache_attend_query", "mla_cache_attend",
-           "mla_probe_mfma_bf16", "mla_status_str", "mla_last_error_detail",
+           "mla_moe_route", "mla_i8_quantize", "mla_i8_dequantize", "mla_shared_wb_i8", "mla_moe_experts_i8_query",
+           "mla_moe_experts_i8", "mla_probe_mfma_bf16", "mla_status_str", "mla_last_error_detail",
            "mla_version")
 
 
@@ -61,6 +62,17 @@ class ProtectCfg(ctypes.Structure):
                 ("budget", ctypes.c_double)]
 
 
+class RouteCfg(ctypes.Structure):
+    _fields_ = [("scoring", ctypes.c_int32), ("n_groups", ctypes.c_int32), ("top_groups", ctypes.c_int32),
+                ("group_best", ctypes.c_int32), ("top_k", ctypes.c_int32), ("min_k", ctypes.c_int32),
+                ("renormalize", ctypes.c_int32), ("scale", ctypes.c_float), ("tau", ctypes.c_float)]
+
+
+class MoeLayer(ctypes.Structure):
+    _fields_ = [("d_model", ctypes.c_int32), ("d_ffn", ctypes.c_int32), ("n_experts", ctypes.c_int32),
+                ("first_expert", ctypes.c_int32), ("top_k", ctypes.c_int32)]
+
+
 def _load(path: str = LIB_PATH):
     if not os.path.exists(path):
         raise ImportError(f"{path} is not built; run `python -m paper_2609_07008_amd.build`")
@@ -93,6 +105,13 @@ def _load(path: str = LIB_PATH):
     lib.mla_cache_gather.argtypes = [GP, I64, P, I64, I32, P, P, I64, P]
     lib.mla_cache_attend_query.argtypes = [GP, I32, I32, I32, I32, ctypes.POINTER(SZ)]
     lib.mla_cache_attend.argtypes = [GP, I32, I32, P, P, P, P, I32, I64, I32, P, P, P, P, SZ, P]
+    lib.mla_moe_route.argtypes = [I64, I32, P, I32, I64, P, ctypes.POINTER(RouteCfg), P, P, P, P, P]
+    lib.mla_i8_quantize.argtypes = [I64, I32, P, I64, P, P, P]
+    lib.mla_i8_dequantize.argtypes = [I64, I32, P, P, P, I64, P]
+    lib.mla_shared_wb_i8.argtypes = [I64, I32, I32, P, P, P, P, I32, P, P]
+    LP = ctypes.POINTER(MoeLayer)
+    lib.mla_moe_experts_i8_query.argtypes = [LP, I64, I32, ctypes.POINTER(SZ)]
+    lib.mla_moe_experts_i8.argtypes = [LP, I64, P, I64, P, P, P, P, P, P, P, I32, P, P, SZ, P]
     lib.mla_probe_mfma_bf16.argtypes = [I32, ctypes.POINTER(ctypes.c_double), P, P]
     for f in ("mla_online_attend_query", "mla_online_attend", "mla_segment_merge", "mla_sliced_oproj_add",
               "mla_online_plan_query", "mla_online_plan", "mla_online_attend_planned",
@@ -100,7 +119,8 @@ def _load(path: str = LIB_PATH):
               "mla_offline_produce", "mla_protected_rows_query", "mla_protected_rows",
               "mla_protected_rows_planned_query", "mla_protected_rows_planned", "mla_moe_fanout", "mla_shared_wb",
               "mla_mx4_quantize", "mla_mx4_dequantize", "mla_shared_wb_mx4", "mla_cache_append", "mla_cache_gather",
-              "mla_cache_attend_query", "mla_cache_attend", "mla_probe_mfma_bf16"):
+              "mla_cache_attend_query", "mla_cache_attend", "mla_moe_route", "mla_i8_quantize", "mla_i8_dequantize",
+              "mla_shared_wb_i8", "mla_moe_experts_i8_query", "mla_moe_experts_i8", "mla_probe_mfma_bf16"):
         getattr(lib, f).restype = ctypes.c_int
     lib.mla_status_str.argtypes = [ctypes.c_int]
     lib.mla_status_str.restype = ctypes.c_char_p
@@ -495,6 +515,122 @@ def cache_attend(geom, q, pos, pages, seq_pages, cache, page_rows: int, out_o, o
     _check(LIB.mla_cache_attend(ctypes.byref(g), b, n_q, _addr(q), _addr(pos), _addr(pages), _addr(seq_pages), pages.shape[1],
                                 n_pages, page_rows, _addr(cache), _addr(out_o), _addr(out_lse), _addr(workspace),
                                 workspace.numel(), _queue(stream, dev)))
+
+
+SCORINGS = {"softmax": 0, "sigmoid": 1}   # MLA_SOFTMAX, MLA_SIGMOID
+
+
+def moe_route(logits, expert_idx, expert_w, fanout=None, expert_count=None, bias=None, scoring: str = "softmax", n_groups: int = 1,
+              top_groups: int = 1, group_best: int = 1, renormalize: bool = True, scale: float = 1.0, min_k: int = 1,
+              tau: float = 2.0, stream=None):
+    """The experts of token rows (mla_moe_route): logits [N, E] float32 or bfloat16 with
+    contiguous rows, bias [E] float32 or None, into expert_idx [N, top_k] int32, expert_w
+    [N, top_k] float32 and, if given, fanout [N] and expert_count [E] int32."""
+    dev = _device()
+    bf16 = isinstance(logits, torch.Tensor) and logits.dtype == torch.bfloat16
+    _tensor("logits", logits, dev, torch.bfloat16 if bf16 else torch.float32, rows=True)
+    n, e = logits.shape
+    _tensor("expert_idx", expert_idx, dev, torch.int32)
+    if expert_idx.dim() != 2 or expert_idx.shape[0] != n:
+        _refuse(f"expert_idx is {tuple(expert_idx.shape)}, expected [{n}, top_k]")
+    k = expert_idx.shape[1]
+    _tensor("expert_w", expert_w, dev, torch.float32, (n, k))
+    if fanout is not None:
+        _tensor("fanout", fanout, dev, torch.int32, (n,))
+    if expert_count is not None:
+        _tensor("expert_count", expert_count, dev, torch.int32, (e,))
+    if bias is not None:
+        _tensor("bias", bias, dev, torch.float32, (e,))
+    if scoring not in SCORINGS:
+        _refuse(f"scoring {scoring!r}, expected one of {sorted(SCORINGS)}")
+    cfg = RouteCfg(SCORINGS[scoring], n_groups, top_groups, group_best, k, min_k, bool(renormalize), scale, tau)
+    _check(LIB.mla_moe_route(n, e, _addr(logits), MLA_BF16 if bf16 else MLA_F32, logits.stride(0) if n > 1 else e, _addr(bias),
+                             ctypes.byref(cfg), _addr(expert_idx), _addr(expert_w), _addr(fanout), _addr(expert_count),
+                             _queue(stream, dev)))
+
+
+def i8_quantize(x, codes, scales, stream=None):
+    """bf16 rows into 8-bit codes and a scale each (mla_i8_quantize): x [N, C] bfloat16
+    with contiguous rows, codes [N, C] int8 and scales [N] float32, written."""
+    dev = _device()
+    _tensor("x", x, dev, torch.bfloat16, rows=True)
+    n, c = x.shape
+    _tensor("codes", codes, dev, torch.int8, (n, c))
+    _tensor("scales", scales, dev, torch.float32, (n,))
+    _check(LIB.mla_i8_quantize(n, c, _addr(x), _row_stride(x), _addr(codes), _addr(scales), _queue(stream, dev)))
+
+
+def i8_dequantize(codes, scales, x, stream=None):
+    """The values of codes [N, C] int8 and scales [N] float32 into x [N, C] bfloat16 with
+    contiguous rows (mla_i8_dequantize)."""
+    dev = _device()
+    _tensor("x", x, dev, torch.bfloat16, rows=True)
+    n, c = x.shape
+    _tensor("codes", codes, dev, torch.int8, (n, c))
+    _tensor("scales", scales, dev, torch.float32, (n,))
+    _check(LIB.mla_i8_dequantize(n, c, _addr(codes), _addr(scales), _addr(x), _row_stride(x), _queue(stream, dev)))
+
+
+def shared_wb_i8(z_codes, z_scales, w_codes, w_scales, y, stream=None):
+    """y = W_b z in 8 bits (mla_shared_wb_i8): z_codes [N, d_in] and w_codes [d_out, d_in]
+    int8, z_scales [N] and w_scales [d_out] float32, y [N, d_out] float32 or bfloat16."""
+    dev = _device()
+    _tensor("z_codes", z_codes, dev, torch.int8)
+    _tensor("w_codes", w_codes, dev, torch.int8)
+    if z_codes.dim() != 2 or w_codes.dim() != 2 or w_codes.shape[1] != z_codes.shape[1]:
+        _refuse(f"z_codes is {tuple(z_codes.shape)}, w_codes {tuple(w_codes.shape)}")
+    n, d_in = z_codes.shape
+    d_out = w_codes.shape[0]
+    _tensor("z_scales", z_scales, dev, torch.float32, (n,))
+    _tensor("w_scales", w_scales, dev, torch.float32, (d_out,))
+    bf16 = isinstance(y, torch.Tensor) and y.dtype == torch.bfloat16
+    _tensor("y", y, dev, torch.bfloat16 if bf16 else torch.float32, (n, d_out))
+    _check(LIB.mla_shared_wb_i8(n, d_in, d_out, _addr(z_codes), _addr(z_scales), _addr(w_codes), _addr(w_scales),
+                                MLA_BF16 if bf16 else MLA_F32, _addr(y), _queue(stream, dev)))
+
+
+def moe_experts_i8_query(n_rows: int, d_model: int, d_ffn: int, n_experts: int, top_k: int, y_dtype=torch.bfloat16) -> int:
+    """Host-only: workspace bytes of mla_moe_experts_i8."""
+    if y_dtype not in (torch.bfloat16, torch.float32):
+        _refuse(f"y_dtype {y_dtype}, expected torch.bfloat16 or torch.float32")
+    layer = MoeLayer(int(d_model), int(d_ffn), int(n_experts), 0, int(top_k))
+    ws = ctypes.c_size_t()
+    _check(LIB.mla_moe_experts_i8_query(ctypes.byref(layer), int(n_rows), MLA_BF16 if y_dtype == torch.bfloat16 else MLA_F32,
+                                        ctypes.byref(ws)))
+    return ws.value
+
+
+def moe_experts_i8(x, expert_idx, expert_w, w_gate_up, s_gate_up, w_down, s_down, y, workspace, fanout=None, first_expert: int = 0,
+                   stream=None):
+    """The experts of an MoE layer in 8 bits (mla_moe_experts_i8): x [N, d_model] bfloat16
+    with contiguous rows, expert_idx [N, top_k] int32, expert_w [N, top_k] float32, fanout [N]
+    int32 or None; w_gate_up [E, 2 d_ffn, d_model] and w_down [E, d_model, d_ffn] int8 of the
+    experts [first_expert, first_expert + E) with s_gate_up [E, 2 d_ffn] and s_down [E,
+    d_model] float32; y [N, d_model] bfloat16 or float32."""
+    dev = _device()
+    _tensor("x", x, dev, torch.bfloat16, rows=True)
+    n, d = x.shape
+    _tensor("expert_idx", expert_idx, dev, torch.int32)
+    if expert_idx.dim() != 2 or expert_idx.shape[0] != n:
+        _refuse(f"expert_idx is {tuple(expert_idx.shape)}, expected [{n}, top_k]")
+    k = expert_idx.shape[1]
+    _tensor("expert_w", expert_w, dev, torch.float32, (n, k))
+    if fanout is not None:
+        _tensor("fanout", fanout, dev, torch.int32, (n,))
+    _tensor("w_down", w_down, dev, torch.int8)
+    if w_down.dim() != 3 or w_down.shape[1] != d:
+        _refuse(f"w_down is {tuple(w_down.shape)}, expected [E, {d}, d_ffn]")
+    e, _, f = w_down.shape
+    _tensor("w_gate_up", w_gate_up, dev, torch.int8, (e, 2 * f, d))
+    _tensor("s_gate_up", s_gate_up, dev, torch.float32, (e, 2 * f))
+    _tensor("s_down", s_down, dev, torch.float32, (e, d))
+    bf16 = isinstance(y, torch.Tensor) and y.dtype == torch.bfloat16
+    _tensor("y", y, dev, torch.bfloat16 if bf16 else torch.float32, (n, d))
+    _tensor("workspace", workspace, dev, torch.uint8)
+    layer = MoeLayer(d, f, e, first_expert, k)
+    _check(LIB.mla_moe_experts_i8(ctypes.byref(layer), n, _addr(x), _row_stride(x), _addr(expert_idx), _addr(expert_w), _addr(fanout),
+                                  _addr(w_gate_up), _addr(s_gate_up), _addr(w_down), _addr(s_down), MLA_BF16 if bf16 else MLA_F32,
+                                  _addr(y), _addr(workspace), workspace.numel(), _queue(stream, dev)))
 
 
 def probe_mfma_bf16(iters, sink, stream=None) -> float:

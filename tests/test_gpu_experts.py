@@ -1,0 +1,172 @@
+"""GPU tests of the experts in 8 bits (mla_moe_experts_i8) against the 64-bit definition; the bound of the reference, and half
+a step 2^-8 of a bf16 output."""
+import numpy as np
+import pytest
+
+import moe_reference as R
+
+pytestmark = pytest.mark.gpu
+
+
+class Layer:
+    def __init__(self, d, f, e, seed, first=0):
+        import torch
+        gen = torch.Generator().manual_seed(seed)
+        self.d, self.f, self.e, self.first = d, f, e, first
+        codes = lambda *s: torch.randn(s, generator=gen).mul(32).round().clamp(-127, 127).to(torch.int8).cuda()
+        scales = lambda *s: (0.02 / 32 * torch.exp2(0.3 * torch.randn(s, generator=gen))).cuda()
+        self.w_gu, self.s_gu, self.w_down, self.s_down = codes(e, 2 * f, d), scales(e, 2 * f), codes(e, d, f), scales(e, d)
+
+    def run(self, x, idx, w, fanout=None, out="f32", ws=None, y=None):
+        import torch
+        from paper_2609_07008_amd import mla
+        dt = torch.bfloat16 if out == "bf16" else torch.float32
+        if y is None:
+            y = torch.full((x.shape[0], self.d), float("nan"), dtype=dt, device="cuda")
+        if ws is None:
+            ws = torch.full((mla.moe_experts_i8_query(x.shape[0], self.d, self.f, self.e, idx.shape[1], dt),), 0xA5, dtype=torch.uint8, device="cuda")
+        mla.moe_experts_i8(x, idx, w, self.w_gu, self.s_gu, self.w_down, self.s_down, y, ws, fanout=fanout, first_expert=self.first)
+        return y
+
+    def want(self, x, idx, w, fanout=None):
+        host = lambda t: t.cpu().numpy()
+        return R.experts(x.float().cpu().numpy().astype(np.float64), host(idx), host(w).astype(np.float64), None if fanout is None else host(fanout),
+                         host(self.w_gu), host(self.s_gu), host(self.w_down), host(self.s_down), self.first)
+
+    def check(self, x, idx, w, fanout=None, out="f32"):
+        y = self.run(x, idx, w, fanout, out).float().cpu().numpy().astype(np.float64)
+        want, off = self.want(x, idx, w, fanout)
+        if out == "bf16":
+            off = off * (1 + 2.0 ** -8) + np.abs(want) * 2.0 ** -8
+        assert (np.abs(y - want) <= off).all(), (np.abs(y - want) - off).max()
+
+
+def _tokens(n, d, experts, k, seed, skew=0.5, stride=None):
+    import torch
+    gen = torch.Generator().manual_seed(seed)
+    x = torch.randn((n, stride or d), generator=gen).mul(torch.exp2(torch.randn((n, 1), generator=gen))).to(torch.bfloat16).cuda()[:, :d]
+    score = torch.randn((n, experts), generator=gen) + skew * torch.randn((1, experts), generator=gen)
+    idx = score.topk(k, dim=1).indices.to(torch.int32).cuda()
+    w = torch.rand((n, k), generator=gen).cuda()
+    fanout = torch.randint(0, k + 2, (n,), generator=gen, dtype=torch.int32).cuda()
+    return x, idx, w, fanout
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("n,d,f,e,k", [(1, 64, 64, 1, 1), (1, 512, 192, 8, 2), (3, 192, 64, 4, 3), (7, 128, 320, 64, 6), (17, 320, 128, 4, 2), (33, 64, 192, 2, 1),
+                                       (64, 256, 256, 16, 6), (97, 576, 64, 3, 3), (200, 128, 128, 2, 2), (300, 64, 448, 4, 2), (130, 1088, 64, 300, 8)])
+def test_random(n, d, f, e, k, out):
+    x, idx, w, fanout = _tokens(n, d, e, k, n + d + f)
+    layer = Layer(d, f, e, e)
+    layer.check(x, idx, w, None, out)
+    layer.check(x, idx, w, fanout, out)
+
+
+def test_widest():
+    """d_model and d_ffn of 16384: the largest sums."""
+    x, idx, w, _ = _tokens(2, 16384, 2, 1, 3)
+    Layer(16384, 64, 2, 1).check(x, idx, w)
+    x, idx, w, _ = _tokens(2, 64, 2, 2, 4)
+    Layer(64, 16384, 2, 2).check(x, idx, w)
+
+
+def test_share_and_padding():
+    """Experts [5, 8) of 16; indexes outside the layer; every value of fanout."""
+    import torch
+    x, idx, w, fanout = _tokens(90, 192, 16, 5, 8, stride=200)
+    idx[80:85] = -1
+    idx[85, 2], idx[86, 0], idx[87, 1] = 2 ** 31 - 1, -2 ** 31, 16
+    fanout[:4] = torch.tensor([-5, 0, 100, 2 ** 31 - 1], dtype=torch.int32)
+    layer = Layer(192, 128, 3, 7, first=5)
+    layer.check(x, idx, w, fanout)
+    layer.check(x, idx, w, None)
+    y = layer.run(x, idx, w)
+    gone = ~((idx >= 5) & (idx < 8)).any(1)
+    assert int(gone.sum()) > 5 and bool((y[gone] == 0).all())
+    y = layer.run(x, torch.full_like(idx, -1), w)
+    assert bool((y == 0).all())
+
+
+def test_shares_add_up():
+    """Two devices' shares: each pair is in one of them."""
+    import torch
+    x, idx, w, _ = _tokens(40, 128, 12, 4, 9)
+    whole = Layer(128, 64, 12, 5)
+    parts = []
+    for lo, hi in ((0, 7), (7, 12)):
+        p = Layer(64, 64, 1, 0, first=lo)
+        p.d, p.e = 128, hi - lo
+        p.w_gu, p.s_gu, p.w_down, p.s_down = (t[lo:hi].contiguous() for t in (whole.w_gu, whole.s_gu, whole.w_down, whole.s_down))
+        parts.append(p.run(x, idx, w))
+    y = whole.run(x, idx, w)
+    # the pairs' terms are the same; adding them up takes a product and an addition each, both at most half a step 2^-24 of
+    # the sum of their magnitudes (which the shares' own sums, having cancelled, do not show): 4 + 4 in the whole, as many
+    # over the shares, and the addition of the shares
+    terms = sum(whole.run(x, idx[:, j:j + 1].contiguous(), w[:, j:j + 1].contiguous()).abs() for j in range(4))
+    assert bool(((parts[0] + parts[1] - y).abs() <= 17 * 2.0 ** -24 * terms).all())
+
+
+def test_an_expert_twice_and_all_rows_at_one():
+    import torch
+    x, idx, w, _ = _tokens(150, 128, 8, 3, 10)
+    idx[:, 1] = idx[:, 0]
+    layer = Layer(128, 64, 8, 3)
+    layer.check(x, idx, w)
+    layer.check(x, torch.full_like(idx, 6), w, None, "bf16")
+
+
+def test_rows_do_not_meet():
+    """A row's bits alone, in a batch, and again; a row of NaN, zeros and infinities beside others."""
+    import torch
+    x, idx, w, _ = _tokens(260, 256, 8, 3, 11)
+    layer = Layer(256, 128, 8, 4)
+    y = layer.run(x, idx, w)
+    assert torch.equal(layer.run(x, idx, w), y)
+    for r in (0, 100, 259):
+        assert torch.equal(layer.run(x[r:r + 1].contiguous(), idx[r:r + 1].contiguous(), w[r:r + 1].contiguous()), y[r:r + 1])
+    x2 = x.clone()
+    x2[5, 7], x2[6] = float("nan"), 0.0
+    x2[7, 0] = float("inf")
+    y2 = layer.run(x2, idx, w)
+    assert bool(y2[5].isnan().all()) and bool((y2[6] == 0).all()) and bool(y2[7].isnan().all())
+    rest = torch.ones(260, dtype=torch.bool)
+    rest[5:8] = False
+    assert torch.equal(y2[rest], y[rest])
+
+
+def test_weights_and_unused_parts():
+    """Weights of NaN past the fanout, zero and negative weights; the workspace's old contents do not matter."""
+    import torch
+    from paper_2609_07008_amd import mla
+    x, idx, w, _ = _tokens(50, 128, 8, 4, 12)
+    fanout = torch.full((50,), 2, dtype=torch.int32, device="cuda")
+    w[:, 2:] = float("nan")
+    w[:, 1] = -w[:, 1]
+    w[3] = 0.0
+    layer = Layer(128, 128, 8, 6)
+    layer.check(x, idx, torch.nan_to_num(w), fanout)
+    y = layer.run(x, idx, w, fanout)
+    ws = torch.full((mla.moe_experts_i8_query(50, 128, 128, 8, 4, torch.float32),), 0xFF, dtype=torch.uint8, device="cuda")
+    assert torch.equal(layer.run(x, idx, w, fanout, ws=ws), y) and bool(y.isfinite().all())
+
+
+def test_no_rows():
+    import torch
+    x, idx, w, _ = _tokens(2, 64, 2, 1, 13)
+    layer = Layer(64, 64, 2, 8)
+    assert layer.run(x[:0], idx[:0], w[:0]).shape == (0, 64)
+
+
+def test_thousands_of_pairs():
+    """Enough pairs for every way of counting and placing them: against the pairs' own rows, computed one batch of 100 at a time."""
+    import torch
+    n = 9001
+    x, idx, w, fanout = _tokens(n, 64, 37, 4, 14, skew=2.0)
+    layer = Layer(64, 64, 37, 9)
+    y = layer.run(x, idx, w, fanout)
+    for lo in (0, 4000, n - 100):
+        part = slice(lo, lo + 100)
+        assert torch.equal(layer.run(x[part].contiguous(), idx[part].contiguous(), w[part].contiguous(), fanout[part].contiguous()), y[part])
+    some = torch.randperm(n, generator=torch.Generator().manual_seed(1))[:60].cuda()
+    want, off = layer.want(x[some], idx[some], w[some], fanout[some])
+    assert (np.abs(y[some].cpu().numpy() - want) <= off).all()

@@ -1,0 +1,148 @@
+"""GPU tests of the router (mla_moe_route) against 64-bit definitions: experts, fanouts and counts equal, weights within
+2^-20 (scores take an exponential of 2 steps, a sum, a quotient and the products, of 2^-24 each)."""
+import numpy as np
+import pytest
+
+import moe_reference as R
+
+pytestmark = pytest.mark.gpu
+
+
+def _route(x, k, bias=None, bf16=False, pad=0, fanout=True, count=True, **kw):
+    import torch
+    from paper_2609_07008_amd import mla
+    n, e = x.shape
+    wide = torch.full((n, e + pad), float("nan"))
+    wide[:, :e] = torch.from_numpy(np.asarray(x, dtype=np.float32))
+    logits = wide.cuda().to(torch.bfloat16 if bf16 else torch.float32)[:, :e]
+    idx = torch.full((n, k), -7, dtype=torch.int32, device="cuda")
+    w = torch.full((n, k), -7.0, device="cuda")
+    fan = torch.full((n,), -7, dtype=torch.int32, device="cuda") if fanout else None
+    cnt = torch.full((e,), -7, dtype=torch.int32, device="cuda") if count else None
+    b = None if bias is None else torch.from_numpy(np.asarray(bias, dtype=np.float32)).cuda()
+    mla.moe_route(logits, idx, w, fan, cnt, bias=b, **kw)
+    torch.cuda.synchronize()
+    return logits.double().cpu().numpy(), idx.cpu().numpy(), w.cpu().numpy(), None if fan is None else fan.cpu().numpy(), \
+        None if cnt is None else cnt.cpu().numpy()
+
+
+def check(x, k, bias=None, bf16=False, pad=0, **kw):
+    seen, idx, w, fan, cnt = _route(x, k, bias, bf16, pad, **kw)
+    b = None if bias is None else np.asarray(bias, dtype=np.float32).astype(np.float64)
+    ri, rw, rf = R.route(seen, k, b, **kw)
+    assert np.array_equal(idx, ri)
+    bad = np.isnan(rw)
+    assert np.array_equal(np.isnan(w), bad)
+    assert (np.abs(w - rw)[~bad] <= 2.0 ** -20 * np.abs(rw)[~bad] + 1e-44).all()
+    assert np.array_equal(fan, rf)
+    taken = np.arange(k)[None, :] < rf[:, None]
+    assert np.array_equal(cnt, np.bincount(ri[taken], minlength=x.shape[1]))
+
+
+def _logits(n, e, seed):
+    rng = np.random.default_rng(seed)
+    return rng.standard_normal((n, e)) * rng.uniform(0.3, 4.0, (n, 1)), rng
+
+
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("with_bias", [False, True])
+@pytest.mark.parametrize("e", [1, 2, 7, 16, 20, 48, 64, 100, 128, 160, 192, 224, 256, 300, 512, 1000, 1024])
+def test_random(e, with_bias, scoring):
+    x, rng = _logits(531, e, e)
+    bias = rng.standard_normal(e) * (0.1 if scoring == "sigmoid" else 0.3 / e) if with_bias else None
+    check(x, min(e, 6), bias, bf16=e % 3 == 0, pad=e % 5, scoring=scoring, min_k=min(e, 3), tau=0.9)
+
+
+@pytest.mark.parametrize("e,g,kept,best,k", [(256, 8, 4, 2, 8), (256, 8, 1, 2, 8), (256, 8, 8, 2, 8), (256, 4, 3, 1, 6), (256, 16, 5, 2, 8), (256, 2, 1, 1, 3),
+                                             (256, 32, 3, 2, 8), (256, 64, 8, 2, 8), (64, 8, 2, 2, 8), (64, 16, 3, 1, 5), (128, 16, 2, 2, 8), (192, 16, 4, 2, 8),
+                                             (160, 8, 3, 1, 6), (60, 5, 2, 2, 6), (96, 3, 2, 2, 8), (8, 8, 3, 2, 3), (1024, 64, 9, 2, 8), (1000, 10, 3, 2, 7)])
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+def test_groups(scoring, e, g, kept, best, k):
+    x, rng = _logits(403, e, e + g)
+    for bias in (rng.standard_normal(e) * (0.2 if scoring == "sigmoid" else 0.3 / e), None):
+        check(x, k, bias, scoring=scoring, n_groups=g, top_groups=kept, group_best=best, scale=2.5, min_k=1, tau=0.8)
+
+
+@pytest.mark.parametrize("k", [1, 2, 3, 4, 5, 7, 8])
+@pytest.mark.parametrize("renorm", [False, True])
+def test_top_k_and_weights(k, renorm):
+    x, rng = _logits(300, 256, k)
+    check(x, k, rng.standard_normal(256) * 0.1, scoring="sigmoid", renormalize=renorm, scale=16.0, min_k=k, tau=0.5)
+    check(x[:7], k, None, scoring="softmax", renormalize=renorm, min_k=1, tau=-1.0)
+
+
+def test_rows_of_equal_scores():
+    """Equal logits, few distinct ones, and equal group scores: the lower index."""
+    rng = np.random.default_rng(3)
+    x = np.concatenate([np.zeros((40, 256)), rng.integers(-2, 3, (200, 256)) / 2, np.tile(rng.integers(0, 4, (50, 32)), (1, 8))])
+    for kw in (dict(scoring="softmax"), dict(scoring="sigmoid"), dict(scoring="sigmoid", n_groups=8, top_groups=3, group_best=2),
+               dict(scoring="softmax", n_groups=16, top_groups=2)):
+        check(x, 8, None, bf16=True, min_k=8, tau=2.0, **kw)
+        check(x, 8, np.tile(rng.integers(0, 2, 64) / 8, 4), min_k=8, tau=2.0, **kw)
+
+
+@pytest.mark.parametrize("e", [64, 256, 1024])
+def test_scores_a_rounding_apart(e):
+    """Biases that bring every c within some 1e-8 of one another: 64 bits decide."""
+    rng = np.random.default_rng(e)
+    x = np.float32(rng.standard_normal((1, e)) * 2)
+    for scoring in ("sigmoid", "softmax"):
+        s = 1 / (1 + np.exp(-x.astype(np.float64))) if scoring == "sigmoid" else np.exp(x.astype(np.float64)) / np.exp(x.astype(np.float64)).sum()
+        bias = np.float32(0.75 - s[0])
+        check(np.repeat(x, 70, 0), 8, bias, scoring=scoring, min_k=8)
+        check(np.repeat(x, 70, 0), 8, bias, scoring=scoring, n_groups=8, top_groups=2, group_best=2, min_k=8)
+        # only some of them
+        bias = np.where(rng.random(e) < 0.05, bias, bias - np.float32(0.3))
+        check(np.repeat(x, 9, 0), 8, bias, scoring=scoring, min_k=8)
+
+
+def test_fanout_next_to_tau():
+    """tau the nearest float of a row's own share: 64 bits decide on which side it lies."""
+    x, _ = _logits(64, 256, 4)
+    x = np.float32(x)
+    for scoring in ("softmax", "sigmoid"):
+        _, w, _ = R.route(x.astype(np.float64), 6, scoring=scoring)
+        for r in range(24):
+            check(x, 6, scoring=scoring, min_k=1, tau=float(np.float32(w[r, : 1 + r % 5].sum())))
+
+
+def test_odd_values():
+    """NaN, infinities and large logits; rows of -infinity; disabled experts."""
+    x, rng = _logits(600, 256, 8)
+    odd = np.array([np.inf, -np.inf, np.nan, 1e30, -1e30, 88.0, -100.0, 0.0])
+    for r in range(300):
+        x[r, rng.choice(256, r % 9, replace=False)] = odd[: r % 9][::-1]
+    x[300:340] = -np.inf
+    x[340:360] = np.nan
+    x[360:380] = np.inf
+    x[380:420, 5:] = -np.inf
+    x[420:440] *= 1e4
+    x[440:460] = -1e4 + x[440:460]
+    off = np.where(rng.random(256) < 0.9, -np.inf, 0.01 * rng.standard_normal(256))
+    for scoring in ("softmax", "sigmoid"):
+        for bias in (None, 0.1 * rng.standard_normal(256), off):
+            for groups in (dict(), dict(n_groups=8, top_groups=4, group_best=2)):
+                check(x, 8, bias, scoring=scoring, min_k=2, tau=0.7, **groups)
+
+
+def test_no_rows_and_no_extras():
+    import torch
+    from paper_2609_07008_amd import mla
+    _, _, _, _, cnt = _route(np.zeros((0, 32)), 4)
+    assert not cnt.any()
+    x, _ = _logits(33, 48, 2)
+    _, i0, w0, f0, _ = _route(x, 5, min_k=2, tau=0.6)
+    _, i1, w1, f1, c1 = _route(x, 5, min_k=2, tau=0.6, fanout=False, count=False)
+    assert f1 is None and c1 is None and np.array_equal(i0, i1) and np.array_equal(w0.view(np.int32), w1.view(np.int32))
+    # without a fanout every rank counts
+    logits = torch.from_numpy(np.float32(x)).cuda()
+    idx, w = torch.zeros((33, 5), dtype=torch.int32, device="cuda"), torch.zeros((33, 5), device="cuda")
+    cnt = torch.zeros(48, dtype=torch.int32, device="cuda")
+    mla.moe_route(logits, idx, w, None, cnt, min_k=2, tau=0.6)
+    assert int(cnt.sum()) == 33 * 5 and np.array_equal(cnt.cpu().numpy(), np.bincount(i0.ravel(), minlength=48))
+
+
+def test_many_rows():
+    x, rng = _logits(30011, 256, 77)
+    check(np.float32(x), 6, 0.1 * rng.standard_normal(256), scoring="sigmoid", n_groups=8, top_groups=4, group_best=2, min_k=3, tau=0.9)
+    check(np.float32(x), 8, None, bf16=True, scoring="softmax", min_k=3, tau=0.9)
