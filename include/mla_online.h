@@ -749,7 +749,7 @@ mla_status mla_shared_wb_i8(int64_t n_rows, int32_t d_in, int32_t d_out, const v
  *   layer        host: d_model, d_ffn multiples of 64 up to MLA_I8_MAX_COLS; n_experts
  *                here (1 .. 1024); first_expert >= 0; top_k columns of expert_idx (1 .. 16:
  *                a caller may append experts that every row uses)
- *   n_rows       N (>= 0); N * top_k at most MLA_EXPERTS_MAX_PAIRS
+ *   n_rows       N (>= 0); taken 65536 at a time, which bounds the workspace
  *   x            device bf16 [N, d_model], rows x_stride elements apart (a multiple of 8, at
  *                least d_model), 16-byte aligned
  *   expert_idx, expert_w   device int32, f32 [N, top_k]
@@ -766,7 +766,6 @@ mla_status mla_shared_wb_i8(int64_t n_rows, int32_t d_in, int32_t d_out, const v
  * Everything that changes from call to call is read on the device.  Errors: NULL, SHAPE,
  * UNSUPPORTED, WORKSPACE, HIP.  Kernels only: may be captured.
  * ------------------------------------------------------------------------- */
-#define MLA_EXPERTS_MAX_PAIRS 16777216
 typedef struct mla_moe_layer {
   int32_t d_model;
   int32_t d_ffn;

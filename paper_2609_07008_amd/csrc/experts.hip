@@ -1,12 +1,12 @@
 // The experts of a mixture-of-experts layer in 8-bit integers:
 //   y_n = sum_{j < K_n} w_nj W_down[e] h_nj,  h_nj = silu(W_gate[e] x_n) * (W_up[e] x_n),  e = expert_idx[n, j]
-// Pairs (n, j) are put in expert order; x is quantized a row; the products run over blocks of
-// rows of one expert; h is rounded to bf16, a layer's activation, and quantized a row; the
-// pairs of a token are joined in rank order.  Within an expert the order of the pairs hangs on
-// atomics, but rows do not meet and the products are exact in i32: the result does not.
-#include "i8.h"
-
-#include <algorithm>
+// Pairs (n, j) are put in expert order; x is quantized a row; the products run over tiles of
+// rows of one expert (i8_tiles.h); h is rounded to bf16, a layer's activation, and quantized a
+// row; the pairs of a token are joined in rank order, in f32.  Within an expert the order of the
+// pairs hangs on LDS atomics, but rows do not meet and the products are exact in i32: the result
+// does not.
+#include "i8_rows.h"
+#include "i8_tiles.h"
 
 namespace mla {
 namespace {
@@ -19,145 +19,245 @@ __device__ __forceinline__ int pair_expert(const ExpertsArgs& a, int32_t p) {
   return a.fanout != nullptr && j >= a.fanout[n] ? -1 : (int)e;
 }
 
-__global__ __launch_bounds__(256) void experts_zero_kernel(ExpertsArgs a) {
-  for (int i = threadIdx.x; i < a.n_experts; i += 256) a.counts[i] = 0;
-}
-
-__global__ __launch_bounds__(256) void experts_count_kernel(ExpertsArgs a) {
-  __shared__ int hist[kExpertsMax];
-  for (int i = threadIdx.x; i < a.n_experts; i += 256) hist[i] = 0;
-  __syncthreads();
-  const int64_t n_pairs = a.n_rows * a.top_k;
-  for (int64_t p = (int64_t)blockIdx.x * 256 + threadIdx.x; p < n_pairs; p += (int64_t)gridDim.x * 256) {
-    const int e = pair_expert(a, (int32_t)p);
-    if (e >= 0) atomicAdd(&hist[e], 1);
+// counts of all experts, one a thread of the first n_experts (1024 threads) -> the place of
+// each expert's first pair, in `place`; with `out`, the tiles and totals into memory
+__device__ void scan_counts(const ExpertsArgs& a, int c, int* place, int* wave_sums, bool out) {
+  const int e = threadIdx.x, lane = e & 63, wave = e >> 6;
+  const int b = (c + a.tile_rows - 1) / a.tile_rows;
+  int rows = c, blocks = b;   // inclusive sums
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int x = __shfl_up(rows, d, 64), y = __shfl_up(blocks, d, 64);
+    if (lane >= d) {
+      rows += x;
+      blocks += y;
+    }
+  }
+  if (lane == 63) {
+    wave_sums[2 * wave] = rows;
+    wave_sums[2 * wave + 1] = blocks;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < a.n_experts; i += 256)
-    if (hist[i]) atomicAdd(&a.counts[i], hist[i]);
-}
-
-// counts -> each expert's first place (its cursor), the tiles, the totals
-__global__ __launch_bounds__(1024) void experts_scan_kernel(ExpertsArgs a) {
-  __shared__ int rows[kExpertsMax], blocks[kExpertsMax];
-  const int e = threadIdx.x;
-  const int c = e < a.n_experts ? a.counts[e] : 0, b = (c + a.tile_rows - 1) / a.tile_rows;
-  rows[e] = c;
-  blocks[e] = b;
-  __syncthreads();
-  for (int d = 1; d < kExpertsMax; d *= 2) {
-    const int x = e >= d ? rows[e - d] : 0, y = e >= d ? blocks[e - d] : 0;
-    __syncthreads();
-    rows[e] += x;
-    blocks[e] += y;
-    __syncthreads();
+  for (int w = 0; w < wave; ++w) {
+    rows += wave_sums[2 * w];
+    blocks += wave_sums[2 * w + 1];
   }
-  if (e < a.n_experts) {
-    const int row = rows[e] - c, t0 = blocks[e] - b;
-    a.counts[a.n_experts + e] = row;
-    for (int i = 0; i < b; ++i) a.tiles[t0 + i] = ExpertTile{e, row + i * a.tile_rows, std::min(a.tile_rows, c - i * a.tile_rows), 0};
+  if (e < a.n_experts) place[e] = rows - c;
+  if (!out) return;
+  if (e == 1023) {
+    a.head[0] = rows;
+    a.head[1] = blocks;
   }
-  if (e == kExpertsMax - 1) {
-    a.head[0] = rows[e];
-    a.head[1] = blocks[e];
+  if (b > 0) a.tiles[blocks - b] = ExpertTile{e, blocks - b, rows - c, c};
+  // the other tiles of an expert by all lanes of its wave: one expert may have most of them
+  for (uint64_t more = __ballot(b > 1); more != 0; more &= more - 1) {
+    const int l = __builtin_ctzll(more);
+    const int n = __shfl(b, l, 64), first = __shfl(blocks - b, l, 64), row0 = __shfl(rows - c, l, 64), count = __shfl(c, l, 64);
+    for (int i = 1 + lane; i < n; i += 64) a.tiles[first + i] = ExpertTile{(e & ~63) + l, first, row0, count};
   }
 }
 
-__global__ __launch_bounds__(256) void experts_place_kernel(ExpertsArgs a) {
-  __shared__ int hist[kExpertsMax];
-  for (int i = threadIdx.x; i < a.n_experts; i += 256) hist[i] = 0;
+constexpr int kOneBlockPairs = 8192;   // pairs that one workgroup counts and places
+
+// Workgroups [0, blocks): the pairs of each expert, counted a share each; a single one places
+// them as well.  The others quantize rows of x.
+template <int NV>
+__global__ __launch_bounds__(1024) void experts_start_kernel(ExpertsArgs a, int blocks) {
+  __shared__ int hist[kExpertsMax], sums[32];
+  if ((int)blockIdx.x >= blocks) {
+    quantize_rows<256, NV>(I8Args{a.x, a.xq, a.xs, a.n_rows, a.x_stride, a.d_model, nullptr}, a.n_rows,
+                           ((int64_t)blockIdx.x - blocks) * 4 + threadIdx.x / 256, ((int64_t)gridDim.x - blocks) * 4, hist);
+    return;
+  }
+  for (int i = threadIdx.x; i < a.n_experts; i += 1024) hist[i] = 0;
   __syncthreads();
-  const int64_t n_pairs = a.n_rows * a.top_k, per = (n_pairs + gridDim.x - 1) / gridDim.x;
+  const int64_t n_pairs = a.n_rows * a.top_k, per = (n_pairs + blocks - 1) / blocks;
   const int64_t lo = blockIdx.x * per, hi = std::min(lo + per, n_pairs);
-  for (int64_t p = lo + threadIdx.x; p < hi; p += 256) {
+  for (int64_t p = lo + threadIdx.x; p < hi; p += 1024) {
     const int e = pair_expert(a, (int32_t)p);
     if (e >= 0) atomicAdd(&hist[e], 1);
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < a.n_experts; i += 256)
-    if (hist[i]) hist[i] = atomicAdd(&a.counts[a.n_experts + i], hist[i]);
+  if (blocks > 1) {
+    for (int i = threadIdx.x; i < a.n_experts; i += 1024) a.hist[blockIdx.x * a.n_experts + i] = hist[i];
+    return;
+  }
+  const int c = (int)threadIdx.x < a.n_experts ? hist[threadIdx.x] : 0;
+  scan_counts(a, c, hist, sums, true);
   __syncthreads();
-  for (int64_t p = lo + threadIdx.x; p < hi; p += 256) {
+  for (int64_t p = lo + threadIdx.x; p < hi; p += 1024) {
     const int e = pair_expert(a, (int32_t)p);
     if (e >= 0) a.pairs[atomicAdd(&hist[e], 1)] = (int32_t)p;
   }
 }
 
+// every workgroup adds up the counts of all, and so knows where its own pairs go
+__global__ __launch_bounds__(1024) void experts_place_kernel(ExpertsArgs a) {
+  __shared__ int place[kExpertsMax], sums[32];
+  int total = 0, before = 0;
+  if ((int)threadIdx.x < a.n_experts) {
+    const int* h = a.hist + threadIdx.x;
+#pragma unroll 8
+    for (int b = 0; b < (int)gridDim.x; ++b) {
+      const int c = h[b * a.n_experts];
+      total += c;
+      before += b < (int)blockIdx.x ? c : 0;
+    }
+  }
+  scan_counts(a, total, place, sums, blockIdx.x == 0);
+  if ((int)threadIdx.x < a.n_experts) place[threadIdx.x] += before;
+  __syncthreads();
+  const int64_t n_pairs = a.n_rows * a.top_k, per = (n_pairs + gridDim.x - 1) / gridDim.x;
+  const int64_t lo = blockIdx.x * per, hi = std::min(lo + per, n_pairs);
+  for (int64_t p = lo + threadIdx.x; p < hi; p += 1024) {
+    const int e = pair_expert(a, (int32_t)p);
+    if (e >= 0) a.pairs[atomicAdd(&place[e], 1)] = (int32_t)p;
+  }
+}
+
+constexpr int kExpertsGroup = 8;   // row tiles per column tile in the walk of an expert
+
+// The expert tile and column tile of a workgroup.  The tiles that exist are known on the device
+// alone: XCD x takes a contiguous range of them, an expert's tiles column by column over 8 row
+// tiles, which share the weights in its L2.
+struct Place {
+  int expert, row, rows, col;   // first place of the tile's rows, rows of it (1 .. BM)
+  bool any;
+};
+__device__ __forceinline__ Place my_tile(const ExpertsArgs& a, int cols) {
+  Place p{};
+  const int total = a.head[1] * cols, per = (total + 7) / 8;
+  const int t = (int)(blockIdx.x % 8) * per + (int)(blockIdx.x / 8);
+  if ((int)(blockIdx.x / 8) >= per || t >= total) return p;
+  const ExpertTile e = a.tiles[t / cols];
+  const int mt = (e.count + a.tile_rows - 1) / a.tile_rows;
+  const int r = t - e.first_tile * cols;
+  const int group = r / (kExpertsGroup * cols), rem = r % (kExpertsGroup * cols), gm = std::min(kExpertsGroup, mt - group * kExpertsGroup);
+  const int m = group * kExpertsGroup + rem % gm;
+  p.col = rem / gm;
+  p.expert = e.expert;
+  p.row = e.row0 + m * a.tile_rows;
+  p.rows = std::min(a.tile_rows, e.count - m * a.tile_rows);
+  p.any = true;
+  return p;
+}
+
 __device__ __forceinline__ float silu(float g) { return g / (1.0f + __expf(-g)); }
 
-// 64 rows x 32 channels of h, 16 rows a wave, fragments from memory
-__global__ __launch_bounds__(256) void experts_gate_up_kernel(ExpertsArgs a) {
-  if ((int)blockIdx.x >= a.head[1]) return;
-  const ExpertTile t = a.tiles[blockIdx.x];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lg = lane >> 4, lc = lane & 15;
-  const int f0 = blockIdx.y * 32;
-  for (int r0 = wave * 16; r0 < t.count; r0 += 64) {
-    const int r = r0 + lc, rc = t.row + std::min(r, t.count - 1);
-    const int64_t n = a.pairs[rc] / a.top_k;
-    const int8_t* x = a.xq + n * a.d_model + lg * 16;
-    const int8_t* w = a.w_gu + ((int64_t)t.expert * 2 * a.d_ffn + f0 + lc) * a.d_model + lg * 16;
-    const int64_t up = (int64_t)a.d_ffn * a.d_model, b16 = 16 * (int64_t)a.d_model;
-    i32x4 acc[4] = {};
-    for (int k = 0; k < a.d_model; k += 64) {
-      const i32x4 fx = *(const i32x4*)(x + k);
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(*(const i32x4*)(w + (j >> 1) * up + (j & 1) * b16 + k), fx, acc[j], 0, 0, 0);
+// h of 32 MI rows x BN / 2 channels: of a wave's BN / 4 columns the first half are gate
+// channels, the second the same channels of up.
+template <int MI, int BN, int NST>
+__global__ __launch_bounds__(I8_WAVES * 64, 2) void experts_gate_up_kernel(ExpertsArgs a) {
+  using Tile = I8Tile<MI, BN, NST>;
+  constexpr int NI = Tile::NI, BM = Tile::BM, W = BN / 8;   // channels of a wave
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[Tile::LDS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Place at = my_tile(a, (a.d_ffn + BN / 2 - 1) / (BN / 2));
+  if (!at.any) return;
+  const int f0 = at.col * (BN / 2), d = a.d_model, f = a.d_ffn;
+  const int8_t* w = a.w_gu + (int64_t)at.expert * 2 * f * d;
+  Tile tile;
+  // rows and channels past the end are clamped to the last one (their results are not stored)
+  tile.aim(wave, lane, [&](bool is_a, int r0, int r, const unsigned char*& src, uint32_t& off) {
+    if (is_a) {
+      src = (const unsigned char*)a.xq;
+      off = (uint32_t)(a.pairs[at.row + std::min(r, at.rows - 1)] / a.top_k) * (uint32_t)d;
+    } else {
+      auto row = [&](int q) { return (q / W & 1) * f + std::min(f0 + q / (2 * W) * W + q % W, f - 1); };
+      src = (const unsigned char*)w + (int64_t)row(r0) * d;
+      off = (uint32_t)((row(r) - row(r0)) * d);
     }
-    if (r >= t.count) continue;
-    const float xs = a.xs[n];
-    const float* s = a.s_gu + (int64_t)t.expert * 2 * a.d_ffn + f0;
+  });
+  tile.product(lds, wave, lane, d);
+  const int wm = wave >> 2, wn = wave & 3, lg = lane >> 4, lc = lane & 15;
+  const float* s = a.s_gu + (int64_t)at.expert * 2 * f;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+  for (int j = 0; j < NI / 2; ++j) {
+    const int c = f0 + wn * W + j * 16 + lg * 4;
+    if (c >= f) continue;   // whole fours: d_ffn is a multiple of 64
+    const f32x4 sg = *(const f32x4*)(s + c), su = *(const f32x4*)(s + f + c);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int f = 16 * j + lg * 4 + e;
-        const float g = (float)acc[j][e] * s[f] * xs, u = (float)acc[2 + j][e] * s[a.d_ffn + f] * xs;
-        ((__bf16*)a.h)[(int64_t)rc * a.d_ffn + f0 + f] = (__bf16)(silu(g) * u);
-      }
+    for (int i = 0; i < MI; ++i) {
+      const int r = wm * (BM / 2) + i * 16 + lc;
+      if (r >= at.rows) continue;
+      const float xs = a.xs[a.pairs[at.row + r] / a.top_k];
+      float h[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        h[e] = silu((float)tile.acc[i][j][e] * sg[e] * xs) * ((float)tile.acc[i][j + NI / 2][e] * su[e] * xs);
+      *(u32x2*)(a.h + (int64_t)(at.row + r) * f + c) = u32x2{pack_bf16x2(h[0], h[1]), pack_bf16x2(h[2], h[3])};
+    }
   }
 }
 
-__global__ __launch_bounds__(256) void experts_down_kernel(ExpertsArgs a) {
-  if ((int)blockIdx.x >= a.head[1]) return;
-  const ExpertTile t = a.tiles[blockIdx.x];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lg = lane >> 4, lc = lane & 15;
-  const int c0 = blockIdx.y * 64;
-  for (int r0 = wave * 16; r0 < t.count; r0 += 64) {
-    const int r = r0 + lc, rc = t.row + std::min(r, t.count - 1);
-    const int8_t* h = a.hq + (int64_t)rc * a.d_ffn + lg * 16;
-    const int8_t* w = a.w_down + ((int64_t)t.expert * a.d_model + c0 + lc) * a.d_ffn + lg * 16;
-    i32x4 acc[4] = {};
-    for (int k = 0; k < a.d_ffn; k += 64) {
-      const i32x4 fh = *(const i32x4*)(h + k);
+// W_down h of 32 MI rows x BN channels; rows leave through LDS, whole lines of each pair's part
+template <int MI, int BN, int NST>
+__global__ __launch_bounds__(I8_WAVES * 64, 2) void experts_down_kernel(ExpertsArgs a) {
+  using Tile = I8Tile<MI, BN, NST>;
+  constexpr int NI = Tile::NI, BM = Tile::BM;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[Tile::LDS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Place at = my_tile(a, (a.d_model + BN - 1) / BN);
+  if (!at.any) return;
+  const int n0 = at.col * BN, d = a.d_model, f = a.d_ffn;
+  Tile tile;
+  tile.aim(wave, lane, [&](bool is_a, int r0, int r, const unsigned char*& src, uint32_t& off) {
+    const int last = is_a ? at.rows - 1 : d - 1 - n0, first = std::min(r0, last);
+    src = (const unsigned char*)(is_a ? a.hq + (int64_t)(at.row + first) * f : a.w_down + ((int64_t)at.expert * d + n0 + first) * f);
+    off = (uint32_t)((std::min(r, last) - first) * f);
+  });
+  tile.product(lds, wave, lane, f);
+  const int wm = wave >> 2, wn = wave & 3, lg = lane >> 4, lc = lane & 15;
+  constexpr int ROW = BN, CH = ROW / 16, RPI = 64 / CH, SW = CH < 8 ? CH - 1 : 7;   // bytes of a wave's row of BN / 4
+  unsigned char MLA_LDS* sw = (unsigned char MLA_LDS*)lds + wave * (2 * 16 * ROW);
+  f32x4 ws[NI];
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(*(const i32x4*)(w + (int64_t)j * 16 * a.d_ffn + k), fh, acc[j], 0, 0, 0);
+  for (int j = 0; j < NI; ++j) {
+    const int c = n0 + wn * (BN / 4) + j * 16 + lg * 4;
+    ws[j] = *(const f32x4*)(a.s_down + (int64_t)at.expert * d + (c < d ? c : 0));
+  }
+  const int rl = lane / CH, cl = lane % CH, n = n0 + wn * (BN / 4) + cl * 4;
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    unsigned char MLA_LDS* sb = sw + (i & 1) * (16 * ROW);
+    const float hs = a.hs[at.row + std::min(wm * (BM / 2) + i * 16 + lc, at.rows - 1)];
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      f32x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = (float)tile.acc[i][j][e] * ws[j][e] * hs;
+      *(f32x4 MLA_LDS*)(sb + lc * ROW + (((j * 4 + lg) ^ (lc & SW)) * 16)) = v;
     }
-    if (r >= t.count) continue;
-    const float hs = a.hs[rc];
-    const float* s = a.s_down + (int64_t)t.expert * a.d_model + c0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int c = 16 * j + lg * 4 + e;
-        a.part[(int64_t)a.pairs[rc] * a.d_model + c0 + c] = (float)acc[j][e] * s[c] * hs;
-      }
+    for (int p = 0; p < 16 / RPI; ++p) {
+      const int r = p * RPI + rl, m = wm * (BM / 2) + i * 16 + r;
+      const f32x4 v = *(const f32x4 MLA_LDS*)(sb + r * ROW + ((cl ^ (r & SW)) * 16));
+      if (m < at.rows && n < d) *(f32x4*)(a.part + (int64_t)a.pairs[at.row + m] * d + n) = v;
+    }
   }
 }
 
+// y of a token: its pairs' parts in rank order, four channels a thread
 template <bool OUT_BF16>
 __global__ __launch_bounds__(256) void experts_join_kernel(ExpertsArgs a) {
-  const int64_t units = a.n_rows * (a.d_model / 4);
+  const int quads = a.d_model / 4;
+  const int64_t units = a.n_rows * quads;
   for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
-    const int64_t n = u / (a.d_model / 4);
-    const int c = (int)(u - n * (a.d_model / 4)) * 4;
+    const int64_t n = u / quads;
+    const int c = (int)(u - n * quads) * 4;
     f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    for (int j = 0; j < a.top_k; ++j) {
-      const int32_t p = (int32_t)(n * a.top_k + j);
-      if (pair_expert(a, p) < 0) continue;
-      y += a.ew[p] * *(const f32x4*)(a.part + (int64_t)p * a.d_model + c);
+    for (int j0 = 0; j0 < a.top_k; j0 += 8) {   // eight parts under way at once
+      f32x4 v[8];
+      float w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int32_t p = (int32_t)(n * a.top_k + std::min(j0 + j, a.top_k - 1));
+        const bool here = j0 + j < a.top_k && pair_expert(a, p) >= 0;
+        w[j] = here ? a.ew[p] : 0.f;
+        v[j] = here ? *(const f32x4*)(a.part + (int64_t)p * a.d_model + c) : f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y += w[j] * v[j];
     }
     if (OUT_BF16)
       *(u32x2*)((uint16_t*)a.y + n * a.d_model + c) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
@@ -166,27 +266,78 @@ __global__ __launch_bounds__(256) void experts_join_kernel(ExpertsArgs a) {
   }
 }
 
-}  // namespace
+template <int MI, int BN, int NST>
+hipError_t launch_gate_up(const ExpertsArgs& a, hipStream_t s) {
+  const int64_t total = experts_max_tiles(a.n_rows * a.top_k, a.n_experts, 32 * MI) * ((a.d_ffn + BN / 2 - 1) / (BN / 2));
+  experts_gate_up_kernel<MI, BN, NST><<<dim3((unsigned)(8 * ((total + 7) / 8))), dim3(I8_WAVES * 64), 0, s>>>(a);
+  return hipGetLastError();
+}
 
-int32_t experts_tile_rows(int64_t n_pairs, int32_t n_experts) { return 64; }
+template <int MI, int BN, int NST>
+hipError_t launch_down(const ExpertsArgs& a, hipStream_t s) {
+  const int64_t total = experts_max_tiles(a.n_rows * a.top_k, a.n_experts, 32 * MI) * ((a.d_model + BN - 1) / BN);
+  experts_down_kernel<MI, BN, NST><<<dim3((unsigned)(8 * ((total + 7) / 8))), dim3(I8_WAVES * 64), 0, s>>>(a);
+  return hipGetLastError();
+}
 
-hipError_t launch_experts(const ExpertsArgs& a, hipStream_t s) {
-  hipError_t e;
+hipError_t launch_start(const ExpertsArgs& a, hipStream_t s) {
   const int64_t n_pairs = a.n_rows * a.top_k;
-  experts_zero_kernel<<<dim3(1), dim3(256), 0, s>>>(a);
-  if ((e = launch_i8_quantize(I8Args{a.x, a.xq, a.xs, a.n_rows, a.x_stride, a.d_model, nullptr}, s)) != hipSuccess) return e;
-  const unsigned blocks = (unsigned)std::min<int64_t>((n_pairs + 1023) / 1024, 256);
-  experts_count_kernel<<<dim3(blocks), dim3(256), 0, s>>>(a);
-  experts_scan_kernel<<<dim3(1), dim3(kExpertsMax), 0, s>>>(a);
-  experts_place_kernel<<<dim3(blocks), dim3(256), 0, s>>>(a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  experts_gate_up_kernel<<<dim3((unsigned)a.max_tiles, (unsigned)(a.d_ffn / 32)), dim3(256), 0, s>>>(a);
-  if ((e = launch_i8_quantize(I8Args{a.h, a.hq, a.hs, n_pairs, a.d_ffn, a.d_ffn, a.head}, s)) != hipSuccess) return e;
-  experts_down_kernel<<<dim3((unsigned)a.max_tiles, (unsigned)(a.d_model / 64)), dim3(256), 0, s>>>(a);
+  const int blocks = n_pairs <= kOneBlockPairs ? 1 : (int)std::min<int64_t>((n_pairs + 2047) / 2048, kDispatchBlocks);
+  const dim3 grid((unsigned)(blocks + (a.n_rows + 3) / 4)), blk(1024);
+  if (a.d_model <= 4096) experts_start_kernel<2><<<grid, blk, 0, s>>>(a, blocks);
+  else if (a.d_model <= 8192) experts_start_kernel<4><<<grid, blk, 0, s>>>(a, blocks);
+  else experts_start_kernel<8><<<grid, blk, 0, s>>>(a, blocks);
+  if (blocks > 1) experts_place_kernel<<<dim3((unsigned)blocks), blk, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_chunk(const ExpertsArgs& a, hipStream_t s) {
+  hipError_t e = launch_start(a, s);
+  if (e != hipSuccess) return e;
+  switch (a.tile_rows) {
+    case 32: e = launch_gate_up<1, 128, 7>(a, s); break;
+    case 64: e = launch_gate_up<2, 256, 3>(a, s); break;
+    case 128: e = launch_gate_up<4, 256, 3>(a, s); break;
+    case 192: e = launch_gate_up<6, 256, 2>(a, s); break;
+    default: e = launch_gate_up<8, 256, 2>(a, s); break;
+  }
+  if (e != hipSuccess) return e;
+  e = launch_i8_quantize(I8Args{a.h, a.hq, a.hs, a.n_rows * a.top_k, a.d_ffn, a.d_ffn, a.head}, s);
+  if (e != hipSuccess) return e;
+  switch (a.tile_rows) {
+    case 32: e = launch_down<1, 128, 7>(a, s); break;
+    case 64: e = launch_down<2, 256, 3>(a, s); break;
+    case 128: e = launch_down<4, 256, 3>(a, s); break;
+    case 192: e = launch_down<6, 256, 2>(a, s); break;
+    default: e = launch_down<8, 256, 2>(a, s); break;
+  }
+  if (e != hipSuccess) return e;
   const unsigned join = (unsigned)std::min<int64_t>((a.n_rows * (a.d_model / 4) + 255) / 256, 1 << 16);
   if (a.y_bf16) experts_join_kernel<true><<<dim3(join), dim3(256), 0, s>>>(a);
   else experts_join_kernel<false><<<dim3(join), dim3(256), 0, s>>>(a);
   return hipGetLastError();
+}
+
+}  // namespace
+
+int32_t experts_tile_rows(int64_t n_pairs, int32_t n_experts) {
+  const int64_t avg = n_pairs / n_experts;
+  return avg <= 16 ? 32 : avg <= 64 ? 64 : avg <= 160 ? 128 : 256;
+}
+
+hipError_t launch_experts(const ExpertsArgs& all, hipStream_t s) {
+  for (int64_t r = 0; r < all.n_rows; r += kExpertsChunk) {
+    ExpertsArgs a = all;
+    a.n_rows = std::min<int64_t>(all.n_rows - r, kExpertsChunk);
+    a.x += r * a.x_stride;
+    a.idx += r * a.top_k;
+    a.ew += r * a.top_k;
+    if (a.fanout != nullptr) a.fanout += r;
+    a.y = (unsigned char*)a.y + r * a.d_model * (a.y_bf16 ? 2 : 4);
+    const hipError_t e = launch_chunk(a, s);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace mla

@@ -39,12 +39,16 @@ struct WbI8Args {
 
 hipError_t launch_wb_i8(const WbI8Args& a, hipStream_t s);
 
-// One block of rows of an expert: rows [row, row + count) of the pairs in expert order
+constexpr int kExpertsChunk = 65536;    // rows taken at a time: what the workspace holds
+constexpr int kDispatchBlocks = 128;    // workgroups that count and place pairs, at most
+
+// One block of rows of an expert.  Its pairs lie at places [row0, row0 + count) of the expert
+// order and make ceil(count / tile rows) tiles from first_tile on, all with this entry.
 struct ExpertTile {
   int32_t expert;
-  int32_t row;
+  int32_t first_tile;
+  int32_t row0;
   int32_t count;
-  int32_t pad;
 };
 
 struct ExpertsArgs {
@@ -61,23 +65,25 @@ struct ExpertsArgs {
   int64_t n_rows;
   int64_t x_stride;
   int32_t d_model, d_ffn, n_experts, first, top_k, y_bf16;
-  // the workspace
-  int32_t* counts;           // [n_experts] pairs of each expert (atomics), then its cursors [n_experts]
+  // the workspace, for min(n_rows, kExpertsChunk) rows
+  int32_t* hist;             // [kDispatchBlocks, n_experts] pairs of each expert in each block's share
   int32_t* head;             // [4]: pairs, tiles
   ExpertTile* tiles;         // [max_tiles]
-  int32_t* pairs;            // [N top_k]: pair n * top_k + j at each place of the expert order
-  int8_t* xq;                // [N, d_model]
-  float* xs;                 // [N]
-  uint16_t* h;               // [N top_k, d_ffn] bf16
-  int8_t* hq;                // [N top_k, d_ffn]
-  float* hs;                 // [N top_k]
-  float* part;               // [N top_k, d_model]: W_down h of each pair
-  int32_t max_tiles;
+  int32_t* pairs;            // [rows top_k]: pair n * top_k + j at each place of the expert order
+  int8_t* xq;                // [rows, d_model]
+  float* xs;                 // [rows]
+  uint16_t* h;               // [rows top_k, d_ffn] bf16
+  int8_t* hq;                // [rows top_k, d_ffn]
+  float* hs;                 // [rows top_k]
+  float* part;               // [rows top_k, d_model]: W_down h of each pair
   int32_t tile_rows;
 };
 
-// rows of a tile, by the largest number of pairs that an expert has on average
+// rows of a tile (32 .. 256), by the pairs that an expert has on average
 int32_t experts_tile_rows(int64_t n_pairs, int32_t n_experts);
+inline int64_t experts_max_tiles(int64_t n_pairs, int32_t n_experts, int32_t tile_rows) {
+  return n_pairs / tile_rows + (n_experts < n_pairs ? n_experts : n_pairs);
+}
 hipError_t launch_experts(const ExpertsArgs& a, hipStream_t s);
 
 }  // namespace mla

@@ -3,93 +3,17 @@
 // A row x of bf16 is held as codes q = round(127 x / max|x|) and the scale max|x| / 127.  The
 // sum of a product of codes is a whole number below 127^2 * 16384 < 2^31 and is exact in i32,
 // so a product does not depend on its order, tile or split: every form gives the same bits.
-#include "i8.h"
-
-#include <algorithm>
+#include "i8_rows.h"
+#include "i8_tiles.h"
 
 namespace mla {
 namespace {
 
-__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
-
-// Codes of a row whose largest magnitude is `top` (bf16 bits without the sign, finite).  The
-// quotient n / A of n = 127 x 2^-e and A = top 2^-e is taken as one Newton step on v_rcp: its
-// error is far below 2^-18, the least distance of such a quotient (8 by 8 bits) from a tie, and
-// a quotient that is a tie has at most 8 bits and comes out exact, so rint rounds as the exact
-// quotient does.  The scaling keeps n in range: e is top's exponent, and no less than -100.
-struct I8Coder {
-  float mul, a, inv;
-  __device__ __forceinline__ explicit I8Coder(uint32_t top) {
-    const int e = std::max((int)(top >> 7), 27) - 127;
-    const float two = __uint_as_float((uint32_t)(127 - e) << 23);   // 2^-e; 2^-128 is subnormal and top < 2^128, e <= 127
-    const float t = __uint_as_float(top << 16);
-    mul = e == 127 ? 127.0f * 0x1p-127f : 127.0f * two;
-    a = e == 127 ? t * 0x1p-127f : t * two;
-    inv = a > 0.0f ? __builtin_amdgcn_rcpf(a) : 0.0f;
-  }
-  __device__ __forceinline__ int code(float x) const {
-    const float n = x * mul, t0 = n * inv;
-    return (int)__builtin_rintf(__builtin_fmaf(__builtin_fmaf(-t0, a, n), inv, t0));
-  }
-};
-
-__device__ __forceinline__ u32x2 codes8(const I8Coder& c, u32x4 v) {
-  u32x2 q;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int c0 = c.code(bf16_lo(v[2 * i])), c1 = c.code(bf16_hi(v[2 * i]));
-    const int c2 = c.code(bf16_lo(v[2 * i + 1])), c3 = c.code(bf16_hi(v[2 * i + 1]));
-    q[i] = (uint32_t)(c0 & 255) | (uint32_t)(c1 & 255) << 8 | (uint32_t)(c2 & 255) << 16 | (uint32_t)c3 << 24;
-  }
-  return q;
-}
-
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) v = umax(v, (uint32_t)__shfl_xor((int)v, d, 64));
-  return v;
-}
-
-// A row by T threads (a wave, or a workgroup of 256), read once and kept in registers: 3 bytes
-// moved a value.
 template <int T, int NV>
 __global__ __launch_bounds__(256) void i8_quantize_kernel(I8Args a) {
-  __shared__ uint32_t part[2][4];   // of this turn and the last: one barrier a row
-  const int t = threadIdx.x % T;
+  __shared__ int part[8];
   const int64_t n = a.n_dev != nullptr ? std::min<int64_t>(*a.n_dev, a.n_rows) : a.n_rows;
-  int turn = 0;
-  for (int64_t r0 = (int64_t)blockIdx.x * (256 / T); r0 < n; r0 += (int64_t)gridDim.x * (256 / T), turn ^= 1) {
-    const int64_t r = r0 + threadIdx.x / T;
-    const bool there = r < n;
-    const uint16_t* x = (const uint16_t*)a.x + (there ? r : r0) * a.x_stride;
-    u32x4 v[NV];
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * T + t) * 8;
-      v[i] = c < a.n_cols ? *(const u32x4*)(x + c) : u32x4{0, 0, 0, 0};
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) m = umax(m, umax(v[i][k] & 0x7fffu, (v[i][k] >> 16) & 0x7fffu));
-    m = wave_max(m);
-    if (T == 256) {
-      if ((threadIdx.x & 63) == 0) part[turn][threadIdx.x >> 6] = m;
-      __syncthreads();
-      m = umax(umax(part[turn][0], part[turn][1]), umax(part[turn][2], part[turn][3]));
-    }
-    if (!there) continue;
-    const bool finite = m < 0x7f80u;
-    const I8Coder coder(finite ? m : 0);
-    int8_t* q = (int8_t*)a.codes + r * a.n_cols;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (i * T + t) * 8;
-      if (c < a.n_cols) *(u32x2*)(q + c) = finite ? codes8(coder, v[i]) : u32x2{0, 0};
-    }
-    if (t == 0) a.scales[r] = finite ? __uint_as_float(m << 16) / 127.0f : __uint_as_float(0x7fc00000u);
-  }
+  quantize_rows<T, NV>(a, n, (int64_t)blockIdx.x * (256 / T) + threadIdx.x / T, (int64_t)gridDim.x * (256 / T), part);
 }
 
 __global__ __launch_bounds__(256) void i8_dequantize_kernel(I8Args a, int segs) {
@@ -111,39 +35,218 @@ __global__ __launch_bounds__(256) void i8_dequantize_kernel(I8Args a, int segs) 
   }
 }
 
-// 64 rows x 64 channels a workgroup, 16 rows a wave, fragments from memory
-template <bool OUT_BF16>
-__global__ __launch_bounds__(256) void wb_i8_kernel(WbI8Args a, int n_tiles) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lg = lane >> 4, lc = lane & 15;
-  const int64_t m = (int64_t)(blockIdx.x / n_tiles) * 64 + wave * 16 + lc;
-  const int n0 = (int)(blockIdx.x % n_tiles) * 64;
-  const int8_t* z = a.z + std::min<int64_t>(m, a.n_rows - 1) * a.d_in + lg * 16;
-  const int8_t* w[4];
-  i32x4 acc[4];
+constexpr int kWbGroup = 8;                              // row panels per column panel in the tile walk
+constexpr int64_t kI8FewRows = 32, kI8FewBlocks = 512;   // largest requests of the few-row kernel
+
+// y = W_b z in tiles (i8_tiles.h).  Workgroups go to the 8 XCDs round-robin, so XCD x takes a
+// contiguous range of tiles, and inside it tiles walk 8 row panels per column panel.  The output
+// leaves through LDS as whole 128-byte lines.
+template <bool OUT_BF16, int MI, int BN, int NST>
+__global__ __launch_bounds__(I8_WAVES * 64, 2) void wb_i8_tile_kernel(WbI8Args a, int m_tiles, int n_tiles, bool stream_out) {
+  using Tile = I8Tile<MI, BN, NST>;
+  constexpr int NI = Tile::NI, BM = Tile::BM;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[Tile::LDS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int total = m_tiles * n_tiles, per = (total + 7) / 8;
+  const int t = (int)(blockIdx.x % 8) * per + (int)(blockIdx.x / 8);
+  if ((int)(blockIdx.x / 8) >= per || t >= total) return;
+  const int group = t / (kWbGroup * n_tiles), rem = t % (kWbGroup * n_tiles);
+  const int gm = std::min(kWbGroup, m_tiles - group * kWbGroup);
+  const int mt = group * kWbGroup + rem % gm, nt = rem / gm;
+  const int64_t m0 = (int64_t)mt * BM;
+  const int n0 = nt * BN;
+
+  Tile tile;
+  // rows past the end are clamped to the last one (their results are not stored)
+  tile.aim(wave, lane, [&](bool is_a, int r0, int r, const unsigned char*& src, uint32_t& off) {
+    const int64_t rows = is_a ? a.n_rows - m0 : (int64_t)a.d_out - n0;   // from the tile's first to the last
+    const int64_t first = std::min<int64_t>(r0, rows - 1);
+    src = (const unsigned char*)(is_a ? a.z : a.w) + ((is_a ? m0 : n0) + first) * a.d_in;
+    off = (uint32_t)((std::min<int64_t>(r, rows - 1) - first) * a.d_in);
+  });
+  tile.product(lds, wave, lane, a.d_in);
+
+  // 16 rows x BN / 4 channels a wave at a time: scaled and written in the sums' layout (row lc,
+  // channels lg * 4 .. + 3 of each block; 16-byte chunk c of row r at c ^ (r & SW)), read back
+  // row-contiguous
+  const int wm = wave >> 2, wn = wave & 3, lg = lane >> 4, lc = lane & 15;
+  constexpr int ES = OUT_BF16 ? 2 : 4, ROW = BN / 4 * ES;   // element and row bytes
+  constexpr int CH = ROW / 16, RPI = 64 / CH;               // 16-byte chunks a row, rows a store
+  constexpr int SW = CH < 8 ? CH - 1 : 7;
+  unsigned char MLA_LDS* sw = (unsigned char MLA_LDS*)lds + wave * (2 * 16 * ROW);
+  f32x4 ws[NI];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    w[j] = a.w + (int64_t)std::min(n0 + 16 * j + lc, a.d_out - 1) * a.d_in + lg * 16;
-    acc[j] = i32x4{0, 0, 0, 0};
-  }
-  for (int k = 0; k < a.d_in; k += 64) {
-    const i32x4 fz = *(const i32x4*)(z + k);
+  for (int j = 0; j < NI; ++j)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(*(const i32x4*)(w[j] + k), fz, acc[j], 0, 0, 0);
+    for (int e = 0; e < 4; ++e) ws[j][e] = a.w_scale[std::min(n0 + wn * (BN / 4) + j * 16 + lg * 4 + e, a.d_out - 1)];
+  float zs[MI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i) zs[i] = a.z_scale[std::min<int64_t>(m0 + wm * (BM / 2) + i * 16 + lc, a.n_rows - 1)];
+  const bool vec = (a.d_out & (16 / ES - 1)) == 0;   // whole chunks: y is 16-byte aligned
+  const int rl = lane / CH, cl = lane % CH;
+  const int n = n0 + wn * (BN / 4) + cl * (16 / ES);
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    unsigned char MLA_LDS* sb = sw + (i & 1) * (16 * ROW);
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      f32x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = (float)tile.acc[i][j][e] * ws[j][e] * zs[i];
+      if (OUT_BF16)
+        *(u32x2 MLA_LDS*)(sb + lc * ROW + (((j * 2 + (lg >> 1)) ^ (lc & SW)) * 16) + (lg & 1) * 8) =
+            u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+      else
+        *(f32x4 MLA_LDS*)(sb + lc * ROW + (((j * 4 + lg) ^ (lc & SW)) * 16)) = v;
+    }
+#pragma unroll
+    for (int p = 0; p < 16 / RPI; ++p) {
+      const int r = p * RPI + rl;
+      const u32x4 v = *(const u32x4 MLA_LDS*)(sb + r * ROW + ((cl ^ (r & SW)) * 16));
+      const int64_t m = m0 + wm * (BM / 2) + i * 16 + r;
+      if (m >= a.n_rows) continue;
+      const int64_t at = m * a.d_out + n;
+      if (vec && n + 16 / ES <= a.d_out) {
+        u32x4* q = (u32x4*)((unsigned char*)a.y + at * ES);
+        if (stream_out) __builtin_nontemporal_store(v, q); else *q = v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16 / ES; ++e) {
+          if (n + e >= a.d_out) continue;
+          if (OUT_BF16)
+            ((uint16_t*)a.y)[at + e] = (uint16_t)(v[e / 2] >> (16 * (e & 1)));
+          else
+            ((uint32_t*)a.y)[at + e] = v[e];
+        }
+      }
+    }
   }
+}
+
+// Few rows: the weight is read once, so what counts is how much of it is in flight.  A workgroup
+// takes 16 output channels and up to 16 MB rows (all of them); its 8 waves bring 1024 of K at a
+// time, a kilobyte of one weight or z row a direct load, into NST stages, and wave b < MB runs
+// the MFMAs of row block b.  Chunk c of row r sits at c ^ (r & 15).
+template <bool OUT_BF16, int MB, int NST>
+__global__ __launch_bounds__(I8_WAVES * 64) void wb_i8_rows_kernel(WbI8Args a) {
+  constexpr int ROWB = 1024, ROWS = 16 + 16 * MB, STAGE = ROWS * ROWB;
+  constexpr int LPW = ROWS / I8_WAVES;           // 1 KB direct loads per wave and stage
+  static_assert(ROWS % I8_WAVES == 0, "a load takes a row");
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[NST * STAGE];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lg = lane >> 4, lc = lane & 15;
+  const int n0 = (int)blockIdx.x * 16;
+  // rows past the end repeat the last one; their results are not stored
+  const unsigned char* src[LPW];
+#pragma unroll
+  for (int j = 0; j < LPW; ++j) {
+    const int r = wave * LPW + j;
+    src[j] = (const unsigned char*)(r < 16 ? a.w + (int64_t)std::min(n0 + r, a.d_out - 1) * a.d_in
+                                           : a.z + std::min<int64_t>(r - 16, a.n_rows - 1) * a.d_in);
+  }
+  auto load = [&](int s, int st) {   // past the end of K: the last chunk again, not used
+#pragma unroll
+    for (int j = 0; j < LPW; ++j) {
+      const int r = wave * LPW + j;
+      const uint32_t at = std::min((uint32_t)(s * ROWB + (lane ^ (r & 15)) * 16), (uint32_t)(a.d_in - 16));
+      dma16(src[j], at, (const unsigned char MLA_LDS*)(lds + st + r * ROWB));
+    }
+  };
+  i32x4 acc = {0, 0, 0, 0};
+  const unsigned char MLA_LDS* L = (const unsigned char MLA_LDS*)lds;
+  const int nk = a.d_in / 64, ns = (a.d_in + ROWB - 1) / ROWB;
+#pragma unroll
+  for (int p = 0; p < NST - 1; ++p) load(p, p * STAGE);
+  int st = 0;
+  for (int s = 0; s < ns; ++s) {
+    // stage s has landed, and every wave has read stage s - 1, whose buffer is next
+    dma_barrier<(NST - 2) * LPW>();
+    load(s + NST - 1, st == 0 ? (NST - 1) * STAGE : st - STAGE);
+    if (wave < MB) {
+      const unsigned char MLA_LDS* pw = L + st + lc * ROWB;
+      const unsigned char MLA_LDS* pz = L + st + (16 + wave * 16 + lc) * ROWB;
+      const int left = nk - s * (ROWB / 64);
+      constexpr int N = ROWB / 64, AHEAD = 4;   // fragments read ahead of their MFMA
+      i32x4 fw[N], fz[N];
+      auto frag = [&](int k) {
+        const int o = ((k * 4 + lg) ^ lc) * 16;
+        fw[k] = *(const i32x4 MLA_LDS*)(pw + o);
+        fz[k] = *(const i32x4 MLA_LDS*)(pz + o);
+      };
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) frag(k);
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        if (k + AHEAD < N) frag(k + AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
+        if (k < left) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[k], fz[k], acc, 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    st = st == (NST - 1) * STAGE ? 0 : st + STAGE;
+  }
+  dma_barrier<0>();   // the loads past the end have landed
+  if (wave >= MB) return;
+  const int64_t m = wave * 16 + lc;
   if (m >= a.n_rows) return;
   const float zs = a.z_scale[m];
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int n = n0 + 16 * j + lg * 4 + e;
-      if (n >= a.d_out) continue;
-      const float v = (float)acc[j][e] * a.w_scale[n] * zs;
-      if (OUT_BF16)
-        ((__bf16*)a.y)[m * a.d_out + n] = (__bf16)v;
-      else
-        ((float*)a.y)[m * a.d_out + n] = v;
+  for (int e = 0; e < 4; ++e) {
+    const int n = n0 + lg * 4 + e;
+    if (n >= a.d_out) continue;
+    const float v = (float)acc[e] * a.w_scale[n] * zs;
+    if (OUT_BF16)
+      ((__bf16*)a.y)[m * a.d_out + n] = (__bf16)v;
+    else
+      ((float*)a.y)[m * a.d_out + n] = v;
+  }
+}
+
+template <bool OUT_BF16, int MI, int BN, int NST>
+hipError_t launch_tiles(const WbI8Args& a, hipStream_t s) {
+  const int m_tiles = (int)((a.n_rows + 32 * MI - 1) / (32 * MI));
+  const int n_tiles = (a.d_out + BN - 1) / BN;
+  const int total = m_tiles * n_tiles;
+  // an output beyond the L2s' 32 MB cannot stay there: stored past them, it leaves them to the panels
+  const bool stream_out = a.n_rows * a.d_out * (OUT_BF16 ? 2 : 4) > (int64_t)32 << 20;
+  wb_i8_tile_kernel<OUT_BF16, MI, BN, NST><<<dim3((unsigned)(8 * ((total + 7) / 8))), dim3(I8_WAVES * 64), 0, s>>>(a, m_tiles, n_tiles, stream_out);
+  return hipGetLastError();
+}
+
+template <bool OUT_BF16>
+hipError_t launch_out(const WbI8Args& a, hipStream_t s) {
+  const int64_t few_blocks = ((int64_t)a.d_out + 15) / 16;
+  if (a.n_rows <= kI8FewRows && few_blocks <= kI8FewBlocks) {
+    if (a.n_rows <= 16) wb_i8_rows_kernel<OUT_BF16, 1, 4><<<dim3((unsigned)few_blocks), dim3(I8_WAVES * 64), 0, s>>>(a);
+    else wb_i8_rows_kernel<OUT_BF16, 2, 3><<<dim3((unsigned)few_blocks), dim3(I8_WAVES * 64), 0, s>>>(a);
+    return hipGetLastError();
+  }
+  // the tile whose rounds over the 256 compute units cost least
+  int best = 8;
+  int64_t cost = INT64_MAX;
+  auto tile = [&](int id, int mi, int bn, int w) {
+    const int64_t tiles = (a.n_rows + 32 * mi - 1) / (32 * mi) * ((a.d_out + bn - 1) / bn);
+    const int64_t c = (tiles + 255) / 256 * w;
+    if (c < cost) {
+      cost = c;
+      best = id;
     }
+  };
+  for (int mi = 8; mi >= 2; --mi) tile(mi, mi, 256, 3 * (mi + 3));
+  for (int mi = 4; mi >= 1; --mi) tile(10 + mi, mi, 128, mi + 7);
+  switch (best) {
+    case 2: return launch_tiles<OUT_BF16, 2, 256, 3>(a, s);
+    case 3: return launch_tiles<OUT_BF16, 3, 256, 3>(a, s);
+    case 4: return launch_tiles<OUT_BF16, 4, 256, 3>(a, s);
+    case 5: return launch_tiles<OUT_BF16, 5, 256, 3>(a, s);
+    case 6: return launch_tiles<OUT_BF16, 6, 256, 2>(a, s);
+    case 7: return launch_tiles<OUT_BF16, 7, 256, 2>(a, s);
+    case 11: return launch_tiles<OUT_BF16, 1, 128, 7>(a, s);
+    case 12: return launch_tiles<OUT_BF16, 2, 128, 6>(a, s);
+    case 13: return launch_tiles<OUT_BF16, 3, 128, 5>(a, s);
+    case 14: return launch_tiles<OUT_BF16, 4, 128, 4>(a, s);
+    default: return launch_tiles<OUT_BF16, 8, 256, 2>(a, s);
+  }
 }
 
 }  // namespace
@@ -167,11 +270,7 @@ hipError_t launch_i8_dequantize(const I8Args& a, hipStream_t s) {
 }
 
 hipError_t launch_wb_i8(const WbI8Args& a, hipStream_t s) {
-  const int n_tiles = (a.d_out + 63) / 64;
-  const dim3 grid((unsigned)((a.n_rows + 63) / 64 * n_tiles));
-  if (a.y_bf16) wb_i8_kernel<true><<<grid, dim3(256), 0, s>>>(a, n_tiles);
-  else wb_i8_kernel<false><<<grid, dim3(256), 0, s>>>(a, n_tiles);
-  return hipGetLastError();
+  return a.y_bf16 ? launch_out<true>(a, s) : launch_out<false>(a, s);
 }
 
 }  // namespace mla

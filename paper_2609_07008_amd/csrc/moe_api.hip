@@ -31,8 +31,8 @@ mla_status check_i8(int64_t n_rows, int32_t n_cols, const void* x, int64_t x_str
 
 // Where the tables and intermediates of mla_moe_experts_i8 lie in its workspace
 struct ExpertsSplit {
-  int32_t tile_rows, max_tiles;
-  int64_t off_counts, off_head, off_tiles, off_pairs, off_xq, off_xs, off_h, off_hq, off_hs, off_part;
+  int32_t tile_rows;
+  int64_t off_hist, off_head, off_tiles, off_pairs, off_xq, off_xs, off_h, off_hq, off_hs, off_part;
   size_t total;
 };
 
@@ -51,23 +51,21 @@ mla_status experts_split(const mla_moe_layer* L, int64_t n_rows, int32_t out_dty
   if (L->top_k > mla::kExpertsMaxPairs)
     return fail(MLA_ERR_UNSUPPORTED, "top_k = %d; built: up to %d", L->top_k, mla::kExpertsMaxPairs);
   if (out_dtype != MLA_BF16 && out_dtype != MLA_F32) return fail(MLA_ERR_SHAPE, "out_dtype %d", out_dtype);
-  if (n_rows > MLA_EXPERTS_MAX_PAIRS / L->top_k)
-    return fail(MLA_ERR_UNSUPPORTED, "n_rows * top_k = %lld * %d; built: up to %d", (long long)n_rows, L->top_k, MLA_EXPERTS_MAX_PAIRS);
-  const int64_t pairs = n_rows * L->top_k, d = L->d_model, f = L->d_ffn;
+  if (n_rows > INT64_MAX / 8 / L->top_k / L->d_model) return fail(MLA_ERR_SHAPE, "n_rows * top_k * d_model overflows");
+  const int64_t rows = std::min<int64_t>(n_rows, mla::kExpertsChunk), pairs = rows * L->top_k, d = L->d_model, f = L->d_ffn;
   S->tile_rows = mla::experts_tile_rows(pairs, L->n_experts);
-  S->max_tiles = (int32_t)(pairs / S->tile_rows + std::min<int64_t>(L->n_experts, pairs));
   int64_t at = 0;
   auto take = [&at](int64_t bytes) {
     const int64_t was = at;
     at += (bytes + 255) / 256 * 256;
     return was;
   };
-  S->off_counts = take((int64_t)2 * L->n_experts * 4);
+  S->off_hist = take((int64_t)mla::kDispatchBlocks * L->n_experts * 4);
   S->off_head = take(16);
-  S->off_tiles = take((int64_t)S->max_tiles * (int64_t)sizeof(mla::ExpertTile));
+  S->off_tiles = take(mla::experts_max_tiles(pairs, L->n_experts, S->tile_rows) * (int64_t)sizeof(mla::ExpertTile));
   S->off_pairs = take(pairs * 4);
-  S->off_xq = take(n_rows * d);
-  S->off_xs = take(n_rows * 4);
+  S->off_xq = take(rows * d);
+  S->off_xs = take(rows * 4);
   S->off_hq = take(pairs * f);
   S->off_hs = take(pairs * 4);
   // h is read for the last time before the first of the parts is written
@@ -228,7 +226,7 @@ mla_status mla_moe_experts_i8(const mla_moe_layer* layer, int64_t n_rows, const 
   a.first = layer->first_expert;
   a.top_k = layer->top_k;
   a.y_bf16 = out_dtype == MLA_BF16;
-  a.counts = reinterpret_cast<int32_t*>(W + S.off_counts);
+  a.hist = reinterpret_cast<int32_t*>(W + S.off_hist);
   a.head = reinterpret_cast<int32_t*>(W + S.off_head);
   a.tiles = reinterpret_cast<mla::ExpertTile*>(W + S.off_tiles);
   a.pairs = reinterpret_cast<int32_t*>(W + S.off_pairs);
@@ -238,7 +236,6 @@ mla_status mla_moe_experts_i8(const mla_moe_layer* layer, int64_t n_rows, const 
   a.hq = reinterpret_cast<int8_t*>(W + S.off_hq);
   a.hs = reinterpret_cast<float*>(W + S.off_hs);
   a.part = reinterpret_cast<float*>(W + S.off_part);
-  a.max_tiles = S.max_tiles;
   a.tile_rows = S.tile_rows;
   const hipError_t e = mla::launch_experts(a, reinterpret_cast<hipStream_t>(stream));
   return e == hipSuccess ? MLA_OK : hip_fail(e, "experts' kernels");
