@@ -5,6 +5,7 @@
 // row; the pairs of a token are joined in rank order, in f32.  Within an expert the order of the
 // pairs hangs on LDS atomics, but rows do not meet and the products are exact in i32: the result
 // does not.
+#include <cstdlib>
 #include "i8_rows.h"
 #include "i8_tiles.h"
 
@@ -65,7 +66,7 @@ template <int NV>
 __global__ __launch_bounds__(1024) void experts_start_kernel(ExpertsArgs a, int blocks) {
   __shared__ int hist[kExpertsMax], sums[32];
   if ((int)blockIdx.x >= blocks) {
-    quantize_rows<256, NV>(I8Args{a.x, a.xq, a.xs, a.n_rows, a.x_stride, a.d_model, nullptr}, a.n_rows,
+    quantize_rows<256, NV>(I8Args{a.x, a.xq, a.xs, a.n_rows, a.x_stride, a.d_model, nullptr, nullptr}, a.n_rows,
                            ((int64_t)blockIdx.x - blocks) * 4 + threadIdx.x / 256, ((int64_t)gridDim.x - blocks) * 4, hist);
     return;
   }
@@ -87,7 +88,7 @@ __global__ __launch_bounds__(1024) void experts_start_kernel(ExpertsArgs a, int 
   __syncthreads();
   for (int64_t p = lo + threadIdx.x; p < hi; p += 1024) {
     const int e = pair_expert(a, (int32_t)p);
-    if (e >= 0) a.pairs[atomicAdd(&hist[e], 1)] = (int32_t)p;
+    if (e >= 0) a.pairs[atomicAdd(&hist[e], 1)] = int2{(int)p / a.top_k, (int)p};
   }
 }
 
@@ -111,7 +112,7 @@ __global__ __launch_bounds__(1024) void experts_place_kernel(ExpertsArgs a) {
   const int64_t lo = blockIdx.x * per, hi = std::min(lo + per, n_pairs);
   for (int64_t p = lo + threadIdx.x; p < hi; p += 1024) {
     const int e = pair_expert(a, (int32_t)p);
-    if (e >= 0) a.pairs[atomicAdd(&place[e], 1)] = (int32_t)p;
+    if (e >= 0) a.pairs[atomicAdd(&place[e], 1)] = int2{(int)p / a.top_k, (int)p};
   }
 }
 
@@ -142,7 +143,8 @@ __device__ __forceinline__ Place my_tile(const ExpertsArgs& a, int cols) {
   return p;
 }
 
-__device__ __forceinline__ float silu(float g) { return g / (1.0f + __expf(-g)); }
+// v_rcp is off by a step of 2^-23 at most, as far as the exponential
+__device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
 
 // h of 32 MI rows x BN / 2 channels: of a wave's BN / 4 columns the first half are gate
 // channels, the second the same channels of up.
@@ -161,40 +163,55 @@ __global__ __launch_bounds__(I8_WAVES * 64, 2) void experts_gate_up_kernel(Exper
   tile.aim(wave, lane, [&](bool is_a, int r0, int r, const unsigned char*& src, uint32_t& off) {
     if (is_a) {
       src = (const unsigned char*)a.xq;
-      off = (uint32_t)(a.pairs[at.row + std::min(r, at.rows - 1)] / a.top_k) * (uint32_t)d;
+      off = (uint32_t)a.pairs[at.row + std::min(r, at.rows - 1)].x * (uint32_t)d;
     } else {
       auto row = [&](int q) { return (q / W & 1) * f + std::min(f0 + q / (2 * W) * W + q % W, f - 1); };
       src = (const unsigned char*)w + (int64_t)row(r0) * d;
       off = (uint32_t)((row(r) - row(r0)) * d);
     }
   });
-  tile.product(lds, wave, lane, d);
+  tile.product(lds, wave, lane, d, (at.rows + 31) / 32);
   const int wm = wave >> 2, wn = wave & 3, lg = lane >> 4, lc = lane & 15;
   const float* s = a.s_gu + (int64_t)at.expert * 2 * f;
+  f32x4 sg[NI / 2], su[NI / 2];
 #pragma unroll
   for (int j = 0; j < NI / 2; ++j) {
-    const int c = f0 + wn * W + j * 16 + lg * 4;
-    if (c >= f) continue;   // whole fours: d_ffn is a multiple of 64
-    const f32x4 sg = *(const f32x4*)(s + c), su = *(const f32x4*)(s + f + c);
+    const int c = std::min(f0 + wn * W + j * 16 + lg * 4, f - 4);
+    sg[j] = *(const f32x4*)(s + c);
+    su[j] = *(const f32x4*)(s + f + c);
+  }
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      const int r = wm * (BM / 2) + i * 16 + lc;
-      if (r >= at.rows) continue;
-      const float xs = a.xs[a.pairs[at.row + r] / a.top_k];
+  for (int i = 0; i < MI; ++i) {
+    const int r = Tile::row_of(wm, i) + lc;
+    if (r >= at.rows) continue;
+    const float xs = a.xs[a.pairs[at.row + r].x];
+#pragma unroll
+    for (int j = 0; j < NI / 2; ++j) {
+      const int c = f0 + wn * W + j * 16 + lg * 4;
+      if (c >= f) continue;   // whole fours: d_ffn is a multiple of 64
       float h[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        h[e] = silu((float)tile.acc[i][j][e] * sg[e] * xs) * ((float)tile.acc[i][j + NI / 2][e] * su[e] * xs);
+        h[e] = silu((float)tile.acc[i][j][e] * sg[j][e] * xs) * ((float)tile.acc[i][j + NI / 2][e] * su[j][e] * xs);
       *(u32x2*)(a.h + (int64_t)(at.row + r) * f + c) = u32x2{pack_bf16x2(h[0], h[1]), pack_bf16x2(h[2], h[3])};
     }
   }
 }
 
+// A sum of W_down's products on its way to the join of a bf16 y: f16 of sum * 2^-12.  Sums are
+// below 128 * 127 * 16384 and whole, so that none overflows, none but 0 is subnormal, and each
+// is rounded by half a step 2^-11 of it: an eighth of what the rounding of y to bf16 is.  Scales
+// come on in f32 at the join.  f32 parts would be 2.5 GB out and 2.5 GB in for 33,792 rows x 4096.
+constexpr float kPartUnit = 0x1p-12f;
+
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
 // W_down h of 32 MI rows x BN channels; rows leave through LDS, whole lines of each pair's part
-template <int MI, int BN, int NST>
+template <bool F16, int MI, int BN, int NST>
 __global__ __launch_bounds__(I8_WAVES * 64, 2) void experts_down_kernel(ExpertsArgs a) {
   using Tile = I8Tile<MI, BN, NST>;
-  constexpr int NI = Tile::NI, BM = Tile::BM;
+  constexpr int NI = Tile::NI;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[Tile::LDS];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Place at = my_tile(a, (a.d_model + BN - 1) / BN);
@@ -206,63 +223,98 @@ __global__ __launch_bounds__(I8_WAVES * 64, 2) void experts_down_kernel(ExpertsA
     src = (const unsigned char*)(is_a ? a.hq + (int64_t)(at.row + first) * f : a.w_down + ((int64_t)at.expert * d + n0 + first) * f);
     off = (uint32_t)((std::min(r, last) - first) * f);
   });
-  tile.product(lds, wave, lane, f);
+  tile.product(lds, wave, lane, f, (at.rows + 31) / 32);
   const int wm = wave >> 2, wn = wave & 3, lg = lane >> 4, lc = lane & 15;
-  constexpr int ROW = BN, CH = ROW / 16, RPI = 64 / CH, SW = CH < 8 ? CH - 1 : 7;   // bytes of a wave's row of BN / 4
+  constexpr int ES = F16 ? 2 : 4, ROW = BN / 4 * ES, CH = ROW / 16, RPI = 64 / CH, SW = CH < 8 ? CH - 1 : 7;
   unsigned char MLA_LDS* sw = (unsigned char MLA_LDS*)lds + wave * (2 * 16 * ROW);
   f32x4 ws[NI];
+  if (!F16) {
 #pragma unroll
-  for (int j = 0; j < NI; ++j) {
-    const int c = n0 + wn * (BN / 4) + j * 16 + lg * 4;
-    ws[j] = *(const f32x4*)(a.s_down + (int64_t)at.expert * d + (c < d ? c : 0));
+    for (int j = 0; j < NI; ++j)
+      ws[j] = *(const f32x4*)(a.s_down + (int64_t)at.expert * d + std::min(n0 + wn * (BN / 4) + j * 16 + lg * 4, d - 4));
   }
-  const int rl = lane / CH, cl = lane % CH, n = n0 + wn * (BN / 4) + cl * 4;
+  const int rl = lane / CH, cl = lane % CH, n = n0 + wn * (BN / 4) + cl * (16 / ES);
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
+    const int r0 = Tile::row_of(wm, i);
+    if (r0 >= at.rows) break;
     unsigned char MLA_LDS* sb = sw + (i & 1) * (16 * ROW);
-    const float hs = a.hs[at.row + std::min(wm * (BM / 2) + i * 16 + lc, at.rows - 1)];
+    const float hs = F16 ? 0.f : a.hs[a.pairs[at.row + std::min(r0 + lc, at.rows - 1)].y];
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
-      f32x4 v;
+      if (F16) {
+        f16x4 v;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = (float)tile.acc[i][j][e] * ws[j][e] * hs;
-      *(f32x4 MLA_LDS*)(sb + lc * ROW + (((j * 4 + lg) ^ (lc & SW)) * 16)) = v;
+        for (int e = 0; e < 4; ++e) v[e] = (_Float16)((float)tile.acc[i][j][e] * kPartUnit);
+        *(f16x4 MLA_LDS*)(sb + lc * ROW + (((j * 2 + (lg >> 1)) ^ (lc & SW)) * 16) + (lg & 1) * 8) = v;
+      } else {
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (float)tile.acc[i][j][e] * ws[j][e] * hs;
+        *(f32x4 MLA_LDS*)(sb + lc * ROW + (((j * 4 + lg) ^ (lc & SW)) * 16)) = v;
+      }
     }
 #pragma unroll
     for (int p = 0; p < 16 / RPI; ++p) {
-      const int r = p * RPI + rl, m = wm * (BM / 2) + i * 16 + r;
-      const f32x4 v = *(const f32x4 MLA_LDS*)(sb + r * ROW + ((cl ^ (r & SW)) * 16));
-      if (m < at.rows && n < d) *(f32x4*)(a.part + (int64_t)a.pairs[at.row + m] * d + n) = v;
+      const int r = p * RPI + rl, m = r0 + r;
+      const u32x4 v = *(const u32x4 MLA_LDS*)(sb + r * ROW + ((cl ^ (r & SW)) * 16));
+      if (m < at.rows && n < d) *(u32x4*)((unsigned char*)a.part + ((int64_t)a.pairs[at.row + m].y * d + n) * ES) = v;
     }
   }
 }
 
-// y of a token: its pairs' parts in rank order, four channels a thread
+// y of a token: its pairs' parts in rank order, eight channels a thread
 template <bool OUT_BF16>
 __global__ __launch_bounds__(256) void experts_join_kernel(ExpertsArgs a) {
-  const int quads = a.d_model / 4;
-  const int64_t units = a.n_rows * quads;
+  constexpr int G = 4;   // parts under way at once
+  const int eights = a.d_model / 8;
+  const int64_t units = a.n_rows * eights;
   for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
-    const int64_t n = u / quads;
-    const int c = (int)(u - n * quads) * 4;
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    for (int j0 = 0; j0 < a.top_k; j0 += 8) {   // eight parts under way at once
-      f32x4 v[8];
-      float w[8];
+    const int64_t n = u / eights;
+    const int c = (int)(u - n * eights) * 8;
+    float y[8] = {};
+    for (int j0 = 0; j0 < a.top_k; j0 += G) {
+      float v[G][8], s[G][8], w[G];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < G; ++j) {
         const int32_t p = (int32_t)(n * a.top_k + std::min(j0 + j, a.top_k - 1));
-        const bool here = j0 + j < a.top_k && pair_expert(a, p) >= 0;
-        w[j] = here ? a.ew[p] : 0.f;
-        v[j] = here ? *(const f32x4*)(a.part + (int64_t)p * a.d_model + c) : f32x4{0.f, 0.f, 0.f, 0.f};
+        const int e = j0 + j < a.top_k ? pair_expert(a, p) : -1;
+        w[j] = 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[j][k] = s[j][k] = 0.f;
+        if (e < 0) continue;
+        w[j] = a.ew[p];
+        if (OUT_BF16) {
+          w[j] *= a.hs[p] / kPartUnit;
+          const f16x8 x = *(const f16x8*)((const _Float16*)a.part + (int64_t)p * a.d_model + c);
+          const f32x4* ws = (const f32x4*)(a.s_down + (int64_t)e * a.d_model + c);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            v[j][k] = (float)x[k];
+            s[j][k] = ws[k / 4][k % 4];
+          }
+        } else {
+          const f32x4* x = (const f32x4*)((const float*)a.part + (int64_t)p * a.d_model + c);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            v[j][k] = x[k / 4][k % 4];
+            s[j][k] = 1.f;
+          }
+        }
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y += w[j] * v[j];
+      for (int j = 0; j < G; ++j)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) y[k] += w[j] * (v[j][k] * s[j][k]);
     }
-    if (OUT_BF16)
-      *(u32x2*)((uint16_t*)a.y + n * a.d_model + c) = u32x2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
-    else
-      *(f32x4*)((float*)a.y + n * a.d_model + c) = y;
+    if (OUT_BF16) {
+      *(u32x4*)((uint16_t*)a.y + n * a.d_model + c) =
+          u32x4{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])};
+    } else {
+      f32x4* to = (f32x4*)((float*)a.y + n * a.d_model + c);
+      to[0] = f32x4{y[0], y[1], y[2], y[3]};
+      to[1] = f32x4{y[4], y[5], y[6], y[7]};
+    }
   }
 }
 
@@ -276,7 +328,9 @@ hipError_t launch_gate_up(const ExpertsArgs& a, hipStream_t s) {
 template <int MI, int BN, int NST>
 hipError_t launch_down(const ExpertsArgs& a, hipStream_t s) {
   const int64_t total = experts_max_tiles(a.n_rows * a.top_k, a.n_experts, 32 * MI) * ((a.d_model + BN - 1) / BN);
-  experts_down_kernel<MI, BN, NST><<<dim3((unsigned)(8 * ((total + 7) / 8))), dim3(I8_WAVES * 64), 0, s>>>(a);
+  const dim3 grid((unsigned)(8 * ((total + 7) / 8))), blk(I8_WAVES * 64);
+  if (a.y_bf16) experts_down_kernel<true, MI, BN, NST><<<grid, blk, 0, s>>>(a);
+  else experts_down_kernel<false, MI, BN, NST><<<grid, blk, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -302,7 +356,7 @@ hipError_t launch_chunk(const ExpertsArgs& a, hipStream_t s) {
     default: e = launch_gate_up<8, 256, 2>(a, s); break;
   }
   if (e != hipSuccess) return e;
-  e = launch_i8_quantize(I8Args{a.h, a.hq, a.hs, a.n_rows * a.top_k, a.d_ffn, a.d_ffn, a.head}, s);
+  e = launch_i8_quantize(I8Args{a.h, a.hq, a.hs, a.n_rows * a.top_k, a.d_ffn, a.d_ffn, a.head, a.pairs}, s);
   if (e != hipSuccess) return e;
   switch (a.tile_rows) {
     case 32: e = launch_down<1, 128, 7>(a, s); break;
@@ -312,7 +366,7 @@ hipError_t launch_chunk(const ExpertsArgs& a, hipStream_t s) {
     default: e = launch_down<8, 256, 2>(a, s); break;
   }
   if (e != hipSuccess) return e;
-  const unsigned join = (unsigned)std::min<int64_t>((a.n_rows * (a.d_model / 4) + 255) / 256, 1 << 16);
+  const unsigned join = (unsigned)std::min<int64_t>((a.n_rows * (a.d_model / 8) + 255) / 256, 1 << 16);
   if (a.y_bf16) experts_join_kernel<true><<<dim3(join), dim3(256), 0, s>>>(a);
   else experts_join_kernel<false><<<dim3(join), dim3(256), 0, s>>>(a);
   return hipGetLastError();
@@ -322,7 +376,8 @@ hipError_t launch_chunk(const ExpertsArgs& a, hipStream_t s) {
 
 int32_t experts_tile_rows(int64_t n_pairs, int32_t n_experts) {
   const int64_t avg = n_pairs / n_experts;
-  return avg <= 16 ? 32 : avg <= 64 ? 64 : avg <= 160 ? 128 : 256;
+  if (getenv("TILE_ROWS")) return atoi(getenv("TILE_ROWS"));
+  return n_pairs <= 16 ? 32 : avg <= 48 ? 64 : avg <= 256 ? 128 : 256;
 }
 
 hipError_t launch_experts(const ExpertsArgs& all, hipStream_t s) {

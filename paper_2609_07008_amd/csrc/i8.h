@@ -20,6 +20,7 @@ struct I8Args {
   int64_t x_stride;
   int32_t n_cols;        // multiple of 16, <= kI8MaxCols
   const int32_t* n_dev;  // device count of rows, at most n_rows, or null
+  const int2* at;        // the scale of row r goes to scales[at[r].y], or null: to scales[r]
 };
 
 hipError_t launch_i8_quantize(const I8Args& a, hipStream_t s);
@@ -69,13 +70,13 @@ struct ExpertsArgs {
   int32_t* hist;             // [kDispatchBlocks, n_experts] pairs of each expert in each block's share
   int32_t* head;             // [4]: pairs, tiles
   ExpertTile* tiles;         // [max_tiles]
-  int32_t* pairs;            // [rows top_k]: pair n * top_k + j at each place of the expert order
+  int2* pairs;               // [rows top_k]: (n, n * top_k + j) of the pair at each place of the expert order
   int8_t* xq;                // [rows, d_model]
   float* xs;                 // [rows]
   uint16_t* h;               // [rows top_k, d_ffn] bf16
   int8_t* hq;                // [rows top_k, d_ffn]
-  float* hs;                 // [rows top_k]
-  float* part;               // [rows top_k, d_model]: W_down h of each pair
+  float* hs;                 // [rows top_k] by pair
+  void* part;                // [rows top_k, d_model] by pair: W_down h in f32, or (y in bf16) its sums in f16
   int32_t tile_rows;
 };
 

@@ -64,7 +64,7 @@ __global__ __launch_bounds__(I8_WAVES * 64, 2) void wb_i8_tile_kernel(WbI8Args a
     src = (const unsigned char*)(is_a ? a.z : a.w) + ((is_a ? m0 : n0) + first) * a.d_in;
     off = (uint32_t)((std::min<int64_t>(r, rows - 1) - first) * a.d_in);
   });
-  tile.product(lds, wave, lane, a.d_in);
+  tile.product(lds, wave, lane, a.d_in, (int)std::min<int64_t>((a.n_rows - m0 + 31) / 32, MI));
 
   // 16 rows x BN / 4 channels a wave at a time: scaled and written in the sums' layout (row lc,
   // channels lg * 4 .. + 3 of each block; 16-byte chunk c of row r at c ^ (r & SW)), read back
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(I8_WAVES * 64, 2) void wb_i8_tile_kernel(WbI8Args a
     for (int e = 0; e < 4; ++e) ws[j][e] = a.w_scale[std::min(n0 + wn * (BN / 4) + j * 16 + lg * 4 + e, a.d_out - 1)];
   float zs[MI];
 #pragma unroll
-  for (int i = 0; i < MI; ++i) zs[i] = a.z_scale[std::min<int64_t>(m0 + wm * (BM / 2) + i * 16 + lc, a.n_rows - 1)];
+  for (int i = 0; i < MI; ++i) zs[i] = a.z_scale[std::min<int64_t>(m0 + Tile::row_of(wm, i) + lc, a.n_rows - 1)];
   const bool vec = (a.d_out & (16 / ES - 1)) == 0;   // whole chunks: y is 16-byte aligned
   const int rl = lane / CH, cl = lane % CH;
   const int n = n0 + wn * (BN / 4) + cl * (16 / ES);
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(I8_WAVES * 64, 2) void wb_i8_tile_kernel(WbI8Args a
     for (int p = 0; p < 16 / RPI; ++p) {
       const int r = p * RPI + rl;
       const u32x4 v = *(const u32x4 MLA_LDS*)(sb + r * ROW + ((cl ^ (r & SW)) * 16));
-      const int64_t m = m0 + wm * (BM / 2) + i * 16 + r;
+      const int64_t m = m0 + Tile::row_of(wm, i) + r;
       if (m >= a.n_rows) continue;
       const int64_t at = m * a.d_out + n;
       if (vec && n + 16 / ES <= a.d_out) {

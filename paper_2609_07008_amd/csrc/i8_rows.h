@@ -86,7 +86,7 @@ __device__ __forceinline__ void quantize_rows(const I8Args& a, int64_t n, int64_
       const int c = (i * T + t) * 8;
       if (c < a.n_cols) *(u32x2*)(q + c) = finite ? codes8(coder, v[i]) : u32x2{0, 0};
     }
-    if (t == 0) a.scales[r] = finite ? __uint_as_float(m << 16) / 127.0f : __uint_as_float(0x7fc00000u);
+    if (t == 0) a.scales[a.at != nullptr ? a.at[r].y : r] = finite ? __uint_as_float(m << 16) / 127.0f : __uint_as_float(0x7fc00000u);
   }
 }
 

@@ -48,9 +48,20 @@ struct I8Tile {
     }
   }
 
+  // row of the tile that block i of 16 begins at, for the waves of half wm: a tile's first rows
+  // are shared by both halves
+  static __device__ __forceinline__ int row_of(int wm, int i) { return 32 * i + 16 * wm; }
+
   // acc = A B^T over `d_in` of K, a multiple of 64.  Of a last slice of 64 the upper chunks, past
-  // the rows' ends, are taken from the lower ones and not used.
-  __device__ __forceinline__ void product(unsigned char* lds, int wave, int lane, int d_in) {
+  // the rows' ends, are taken from the lower ones and not used.  Of a tile with fewer rows than
+  // it has room for, the blocks i >= mi take no products (their sums are 0).
+  __device__ __forceinline__ void product(unsigned char* lds, int wave, int lane, int d_in, int mi = MI) {
+    if (mi >= MI) steps<false>(lds, wave, lane, d_in, MI);
+    else steps<true>(lds, wave, lane, d_in, mi);
+  }
+
+  template <bool SOME>
+  __device__ __forceinline__ void steps(unsigned char* lds, int wave, int lane, int d_in, int mi) {
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -64,13 +75,13 @@ struct I8Tile {
     // fragments (16 rows x 64 of K): lane group lg holds chunk 4 h + lg of row lc; the rows'
     // swizzle repeats every 16, so blocks are immediate offsets
     const int wm = wave >> 2, wn = wave & 3, lg = lane >> 4, lc = lane & 15;
-    const int fa = (wm * (BM / 2) + lc) * I8_ROWB + ((lg ^ i8_swz(lc)) * 16);
+    const int fa = (wm * 16 + lc) * I8_ROWB + ((lg ^ i8_swz(lc)) * 16);
     const int fb = A_BYTES + (wn * (BN / 4) + lc) * I8_ROWB + ((lg ^ i8_swz(lc)) * 16);
     struct Frags {
       i32x4 a[MI], b[NI];
     };
-    auto frag = [&](int base, int st, int h, int i) -> i32x4 {
-      return *(const i32x4 MLA_LDS*)((const unsigned char MLA_LDS*)lds + ((st + base) ^ (h * 64)) + i * 16 * I8_ROWB);
+    auto frag = [&](int base, int st, int h, int rows) -> i32x4 {
+      return *(const i32x4 MLA_LDS*)((const unsigned char MLA_LDS*)lds + ((st + base) ^ (h * 64)) + rows * I8_ROWB);
     };
     auto half = [&](const Frags& f, Frags& nx, int nst, int nh, auto LOAD, int kt, int lst) {
       constexpr int R = MI + NI;                 // fragments to read, spread over the rows of MFMAs
@@ -80,18 +91,20 @@ struct I8Tile {
       for (int i = 0; i < MI; ++i) {
 #pragma unroll
         for (int k = 0; k < PER; ++k, ++rd)
-          if (rd < NI) nx.b[rd] = frag(fb, nst, nh, rd);
-          else if (rd < R) nx.a[rd - NI] = frag(fa, nst, nh, rd - NI);
+          if (rd < NI) nx.b[rd] = frag(fb, nst, nh, 16 * rd);
+          else if (rd < R && (!SOME || rd - NI < mi)) nx.a[rd - NI] = frag(fa, nst, nh, 32 * (rd - NI));
         if constexpr (decltype(LOAD)::value) {
 #pragma unroll
           for (int k = 0; k < (LPW + MI - 1) / MI; ++k, ++ld)
             if (ld < LPW) load_one(ld, kt, lst);
         }
         __builtin_amdgcn_sched_barrier(0);
+        if (!SOME || i < mi) {
 #pragma unroll
-        for (int jj = 0; jj < NI; ++jj) {
-          const int j = i & 1 ? NI - 1 - jj : jj;   // neighbours share an operand
-          acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.b[j], f.a[i], acc[i][j], 0, 0, 0);
+          for (int jj = 0; jj < NI; ++jj) {
+            const int j = i & 1 ? NI - 1 - jj : jj;   // neighbours share an operand
+            acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(f.b[j], f.a[i], acc[i][j], 0, 0, 0);
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -108,9 +121,9 @@ struct I8Tile {
     if (nk >= NST) dma_barrier<(NST - 1) * LPW>(); else dma_barrier<0>();
     Frags f0, f1;
 #pragma unroll
-    for (int j = 0; j < NI; ++j) f0.b[j] = frag(fb, 0, 0, j);
+    for (int j = 0; j < NI; ++j) f0.b[j] = frag(fb, 0, 0, 16 * j);
 #pragma unroll
-    for (int i = 0; i < MI; ++i) f0.a[i] = frag(fa, 0, 0, i);
+    for (int i = 0; i < MI; ++i) f0.a[i] = frag(fa, 0, 0, 32 * i);
     int st = 0, kt = 0;
     for (; kt + NST < nk; ++kt) {
       half(f0, f1, st, 1, std::false_type{}, 0, 0);

@@ -63,13 +63,13 @@ mla_status experts_split(const mla_moe_layer* L, int64_t n_rows, int32_t out_dty
   S->off_hist = take((int64_t)mla::kDispatchBlocks * L->n_experts * 4);
   S->off_head = take(16);
   S->off_tiles = take(mla::experts_max_tiles(pairs, L->n_experts, S->tile_rows) * (int64_t)sizeof(mla::ExpertTile));
-  S->off_pairs = take(pairs * 4);
+  S->off_pairs = take(pairs * (int64_t)sizeof(int2));
   S->off_xq = take(rows * d);
   S->off_xs = take(rows * 4);
   S->off_hq = take(pairs * f);
   S->off_hs = take(pairs * 4);
   // h is read for the last time before the first of the parts is written
-  S->off_h = S->off_part = take(std::max(pairs * f * 2, pairs * d * 4));
+  S->off_h = S->off_part = take(std::max(pairs * f * 2, pairs * d * (out_dtype == MLA_BF16 ? 2 : 4)));
   S->total = (size_t)std::max<int64_t>(at, 256);
   return MLA_OK;
 }
@@ -136,7 +136,7 @@ mla_status mla_i8_quantize(int64_t n_rows, int32_t n_cols, const void* x, int64_
   mla::clear_detail();
   const mla_status st = check_i8(n_rows, n_cols, x, x_stride, codes, scales);
   if (st != MLA_OK || n_rows == 0) return st;
-  const hipError_t e = mla::launch_i8_quantize(mla::I8Args{x, codes, scales, n_rows, x_stride, n_cols, nullptr},
+  const hipError_t e = mla::launch_i8_quantize(mla::I8Args{x, codes, scales, n_rows, x_stride, n_cols, nullptr, nullptr},
                                                reinterpret_cast<hipStream_t>(stream));
   return e == hipSuccess ? MLA_OK : hip_fail(e, "8-bit quantize kernel");
 }
@@ -147,7 +147,7 @@ mla_status mla_i8_dequantize(int64_t n_rows, int32_t n_cols, const void* codes, 
   const mla_status st = check_i8(n_rows, n_cols, x, x_stride, codes, scales);
   if (st != MLA_OK || n_rows == 0) return st;
   const hipError_t e =
-      mla::launch_i8_dequantize(mla::I8Args{x, const_cast<void*>(codes), const_cast<float*>(scales), n_rows, x_stride, n_cols, nullptr},
+      mla::launch_i8_dequantize(mla::I8Args{x, const_cast<void*>(codes), const_cast<float*>(scales), n_rows, x_stride, n_cols, nullptr, nullptr},
                                 reinterpret_cast<hipStream_t>(stream));
   return e == hipSuccess ? MLA_OK : hip_fail(e, "8-bit dequantize kernel");
 }
@@ -229,13 +229,13 @@ mla_status mla_moe_experts_i8(const mla_moe_layer* layer, int64_t n_rows, const 
   a.hist = reinterpret_cast<int32_t*>(W + S.off_hist);
   a.head = reinterpret_cast<int32_t*>(W + S.off_head);
   a.tiles = reinterpret_cast<mla::ExpertTile*>(W + S.off_tiles);
-  a.pairs = reinterpret_cast<int32_t*>(W + S.off_pairs);
+  a.pairs = reinterpret_cast<int2*>(W + S.off_pairs);
   a.xq = reinterpret_cast<int8_t*>(W + S.off_xq);
   a.xs = reinterpret_cast<float*>(W + S.off_xs);
   a.h = reinterpret_cast<uint16_t*>(W + S.off_h);
   a.hq = reinterpret_cast<int8_t*>(W + S.off_hq);
   a.hs = reinterpret_cast<float*>(W + S.off_hs);
-  a.part = reinterpret_cast<float*>(W + S.off_part);
+  a.part = W + S.off_part;
   a.tile_rows = S.tile_rows;
   const hipError_t e = mla::launch_experts(a, reinterpret_cast<hipStream_t>(stream));
   return e == hipSuccess ? MLA_OK : hip_fail(e, "experts' kernels");

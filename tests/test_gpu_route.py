@@ -1,5 +1,7 @@
 """GPU tests of the router (mla_moe_route) against 64-bit definitions: experts, fanouts and counts equal, weights within
-2^-20 (scores take an exponential of 2 steps, a sum, a quotient and the products, of 2^-24 each)."""
+2^-19, in steps of 2^-24: a score's exponential 2; of a softmax the sum, whose exponentials are off by 1.22 d + 2 at a distance d from the
+largest logit (the difference, its product with log2 e, that constant), weighted by e^-d at most 1.22 * 2.8 + 2, and whose 9 additions
+are rounded; the quotient 1; the sum of the ranks 3 + 1, its quotient 1, the scale 1: below 24."""
 import numpy as np
 import pytest
 
@@ -33,7 +35,7 @@ def check(x, k, bias=None, bf16=False, pad=0, **kw):
     assert np.array_equal(idx, ri)
     bad = np.isnan(rw)
     assert np.array_equal(np.isnan(w), bad)
-    assert (np.abs(w - rw)[~bad] <= 2.0 ** -20 * np.abs(rw)[~bad] + 1e-44).all()
+    assert (np.abs(w - rw)[~bad] <= 2.0 ** -19 * np.abs(rw)[~bad] + 1e-44).all()
     assert np.array_equal(fan, rf)
     taken = np.arange(k)[None, :] < rf[:, None]
     assert np.array_equal(cnt, np.bincount(ri[taken], minlength=x.shape[1]))
