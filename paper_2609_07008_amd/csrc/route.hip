@@ -28,162 +28,130 @@ __device__ __forceinline__ uint64_t order_bits(double v) {
   return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
 }
 
-__device__ __forceinline__ double wave_max(double v) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) v = fmax(v, __shfl_xor(v, d, 64));
-  return v;
+__device__ __forceinline__ double from_order_bits(uint64_t k) {
+  if (k == 0) return __longlong_as_double(0x7ff8000000000000ll);
+  return __longlong_as_double((long long)((k >> 63) ? (k & 0x7FFFFFFFFFFFFFFFull) : ~k));
 }
 
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d, 64);
-  return v;
-}
+// The wave's own LDS accesses, in order
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup"); }
 
-// A row by a whole wave in 64 bits; lane holds experts lane, lane + 64, ...  `group` is LDS of
-// the wave, [E].
-template <int NV>
-__device__ void route_exact(const RouteArgs& a, int64_t r, int lane, double* group) {
+// A row by a whole wave in 64 bits; lane holds experts lane, lane + 64, ...; `score` and `key` are
+// LDS of the wave, [E].  Loops stay rolled: where this runs for one row in hundreds its time is
+// that of fetching its instructions (unrolled by four, some 150 rows of 264,192 cost 30 us).
+__device__ void route_exact(const RouteArgs& a, int64_t r, int lane, double* score, uint64_t* key) {
   const int E = a.n_experts;
-  double s[NV];
-  uint64_t key[NV];   // order of c, or of the logit without a bias
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int e = 64 * i + lane;
-    s[i] = e < E ? (double)logit(a, r, e) : -INFINITY;
-    key[i] = order_bits(s[i]);
+  double m = -INFINITY, sum = 0.0;
+  if (!a.sigmoid) {
+#pragma unroll 1
+    for (int e = lane; e < E; e += 64) m = fmax(m, (double)logit(a, r, e));
+#pragma unroll 1
+    for (int d = 1; d < 64; d *= 2) m = fmax(m, __shfl_xor(m, d, 64));
   }
-  if (a.sigmoid) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) s[i] = 1.0 / (1.0 + exp(-s[i]));
-  } else {
-    double m = -INFINITY, sum = 0.0;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) m = fmax(m, s[i]);
-    m = wave_max(m);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      // a row of -infinity has no weight; lanes past E add none
-      s[i] = 64 * i + lane < E && !(m == -INFINITY && s[i] == m) ? exp(s[i] - m) : 0.0;
-      sum += s[i];
-    }
-    sum = wave_sum(sum);
-    if (sum != 0.0)
-#pragma unroll
-      for (int i = 0; i < NV; ++i) s[i] /= sum;
+#pragma unroll 1
+  for (int e = lane; e < E; e += 64) {
+    const double x = logit(a, r, e), y = exp(a.sigmoid ? -x : x - m);
+    // a row of -infinity alone has no weight
+    const double s = a.sigmoid ? 1.0 / (1.0 + y) : m == -INFINITY && x == m ? 0.0 : y;
+    sum += s;
+    score[e] = s;
+    key[e] = order_bits(x);
   }
+#pragma unroll 1
+  for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d, 64);
   uint32_t open = 0;   // experts of the lane that may be chosen
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int e = 64 * i + lane;
-    if (e >= E) continue;
-    open |= 1u << i;
-    double c = s[i];
-    if (a.bias != nullptr) {
-      c += (double)a.bias[e];
-      key[i] = order_bits(c);
-    }
-    if (a.top_groups < a.n_groups) group[e] = c;
+#pragma unroll 1
+  for (int e = lane; e < E; e += 64) {
+    open |= 1u << (e >> 6);
+    if (!a.sigmoid && sum != 0.0) score[e] /= sum;
+    if (a.bias != nullptr) key[e] = order_bits(score[e] + (double)a.bias[e]);
   }
+  in_order();
   if (a.top_groups < a.n_groups) {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");   // the wave's own LDS accesses, in order
     const int G = a.n_groups, size = E / G;
-    uint64_t score = 0;
+    uint64_t best = 0;
     if (lane < G) {
-      double v0 = -INFINITY, v1 = -INFINITY;
-      uint64_t k0 = 0, k1 = 0;
-      bool any = false;
-      for (int i = 0; i < size; ++i) {
-        const double v = group[lane * size + i];
-        const uint64_t k = order_bits(v);
-        if (!any || k > k0) {
-          v1 = v0;
-          k1 = k0;
-          v0 = v;
-          k0 = k;
-          any = true;
-        } else if (i == 1 || k > k1) {
-          v1 = v;
-          k1 = k;
-        }
+      uint64_t k0 = 0, k1 = 0;   // the two largest, NaN as 0
+#pragma unroll 1
+      for (int e = lane * size; e < (lane + 1) * size; ++e) {
+        const uint64_t k = a.bias != nullptr ? key[e] : order_bits(score[e]);
+        k1 = k > k0 ? k0 : k > k1 ? k : k1;
+        k0 = k > k0 ? k : k0;
       }
-      score = order_bits(a.group_best > 1 && size > 1 ? v0 + v1 : v0);
+      best = a.group_best > 1 && size > 1 ? order_bits(from_order_bits(k0) + from_order_bits(k1)) : k0;
     }
     int before = 0;
+#pragma unroll 1
     for (int g = 0; g < G; ++g) {
-      const uint64_t o = (uint64_t)__shfl((long long)score, g, 64);
-      before += o > score || (o == score && g < lane);
+      const uint64_t o = (uint64_t)__shfl((long long)best, g, 64);
+      before += o > best || (o == best && g < lane);
     }
     const uint64_t kept = __ballot(lane < G && before < a.top_groups);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int e = 64 * i + lane;
-      if (e < E && !((kept >> (e / size)) & 1)) open &= ~(1u << i);
-    }
+#pragma unroll 1
+    for (int e = lane; e < E; e += 64)
+      if (!((kept >> (e / size)) & 1)) open &= ~(1u << (e >> 6));
   }
-  int idx[kMoeMaxTopK];
-  double w[kMoeMaxTopK], total = 0.0;
-#pragma unroll
-  for (int j = 0; j < kMoeMaxTopK; ++j) {
-    idx[j] = 0;
-    w[j] = 0.0;
-    if (j >= a.top_k) continue;
+  int idx = 0;   // lane j: rank j and its score
+  double w = 0.0, total = 0.0;
+#pragma unroll 1
+  for (int j = 0; j < a.top_k; ++j) {
     uint64_t bk = 0;
     int be = INT32_MAX;   // none left
-    double bs = 0.0;
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (((open >> i) & 1) && (be == INT32_MAX || key[i] > bk)) {
-        bk = key[i];
-        be = 64 * i + lane;
-        bs = s[i];
+#pragma unroll 1
+    for (uint32_t rest = open; rest != 0; rest &= rest - 1) {
+      const int e = 64 * __builtin_ctz(rest) + lane;
+      const uint64_t k = key[e];
+      if (be == INT32_MAX || k > bk) {
+        bk = k;
+        be = e;
       }
+    }
     const int mine = be;
-#pragma unroll
+#pragma unroll 1
     for (int d = 1; d < 64; d *= 2) {
       const uint64_t ok = (uint64_t)__shfl_xor((long long)bk, d, 64);
       const int oe = __shfl_xor(be, d, 64);
-      const double os = __shfl_xor(bs, d, 64);
       if (oe != INT32_MAX && (be == INT32_MAX || ok > bk || (ok == bk && oe < be))) {
         bk = ok;
         be = oe;
-        bs = os;
       }
     }
     if (mine == be) open &= ~(1u << (be >> 6));
-    idx[j] = be;
-    w[j] = bs;
-    total += bs;
-  }
-  double upto = 0.0, div = a.renormalize && total != 0.0 ? total : 1.0;
-  int K = a.top_k;
-  bool done = false;
-#pragma unroll
-  for (int j = 0; j < kMoeMaxTopK; ++j) {
-    if (j >= a.top_k) continue;
-    upto += w[j];
-    if (!done && j + 1 >= a.min_k && total > 0.0 && upto >= (double)a.tau * total) {
-      K = j + 1;
-      done = true;
-    }
+    const double s = score[be];
+    total += s;
     if (lane == j) {
-      a.expert_idx[r * a.top_k + j] = idx[j];
-      a.expert_w[r * a.top_k + j] = (float)(w[j] / div * (double)a.scale);
+      idx = be;
+      w = s;
     }
+  }
+  double upto = 0.0;
+  int K = a.top_k;
+#pragma unroll 1
+  for (int j = 0; j + 1 < a.top_k; ++j) {
+    upto += __shfl(w, j, 64);
+    if (j + 1 >= a.min_k && total > 0.0 && upto >= (double)a.tau * total) {
+      K = j + 1;
+      break;
+    }
+  }
+  if (lane < a.top_k) {
+    a.expert_idx[r * a.top_k + lane] = idx;
+    a.expert_w[r * a.top_k + lane] = (float)(w / (a.renormalize && total != 0.0 ? total : 1.0) * (double)a.scale);
   }
   if (lane == 0 && a.fanout != nullptr) a.fanout[r] = K;
+  in_order();
 }
 
-template <int NV>
+// any row, a wave each
+template <int E_MAX>
 __global__ __launch_bounds__(256) void route_wave_kernel(RouteArgs a) {
-  __shared__ double group[4][64 * NV];
+  __shared__ double score[4][E_MAX];
+  __shared__ uint64_t key[4][E_MAX];
   if (a.expert_count != nullptr && blockIdx.x == 0)
     for (int i = threadIdx.x; i < a.n_experts; i += 256) a.expert_count[i] = 0;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int64_t r = (int64_t)blockIdx.x * 4 + wave; r < a.n_rows; r += (int64_t)gridDim.x * 4) {
-    route_exact<NV>(a, r, lane, group[wave]);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
-  }
+  for (int64_t r = (int64_t)blockIdx.x * 4 + wave; r < a.n_rows; r += (int64_t)gridDim.x * 4)
+    route_exact(a, r, lane, score[wave], key[wave]);
 }
 
 // What ranks a row's experts in route_row_kernel
@@ -194,6 +162,13 @@ enum RouteBy {
 };
 
 __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+
+// the conversion itself: in C++ it is undefined past the type's range
+__device__ __forceinline__ uint32_t to_u32(float v) {
+  uint32_t u;
+  asm("v_cvt_u32_f32 %0, %1" : "=v"(u) : "v"(v));
+  return u;
+}
 
 template <int CTRL>
 __device__ __forceinline__ float fmax_dpp(float v) {
@@ -212,12 +187,11 @@ __device__ __forceinline__ float row_sum(float v) {
   return v + __uint_as_float(dpp<0x140>(__float_as_uint(v)));
 }
 
-// lanes of the row whose key is above this lane's
-template <int R>
+// groups of LG lanes, all with the group's key, whose key is above this lane's
+template <int LG, int R = 16 - LG>
 __device__ __forceinline__ uint32_t above(uint32_t key) {
-  const uint32_t n = dpp<0x120 + R>(key) > key ? 1u : 0u;   // row_ror:R
-  if constexpr (R > 1) return n + above<R - 1>(key);
-  return n;
+  if constexpr (R > 0) return (dpp<0x120 + R>(key) > key ? 1u : 0u) + above<LG, R - LG>(key);   // row_ror:R
+  return 0;
 }
 
 // M consecutive logits of row r from expert M sl on, as f32; past E: -infinity
@@ -270,15 +244,17 @@ __device__ __forceinline__ void load_logits(const RouteArgs& a, bool wide, int64
 //
 // Errors of the codes, in steps of 2^-24 of the range 1 + 2 B of c (B the largest finite |bias|):
 // the sigmoid's exponential is off by (1.5 |l| + 2) 2^-24 of itself, of which s (1 - s) <= 1/4 and
-// s (1 - s) |l| < 0.23 reach s; 1 + e, its reciprocal and the bias add 3 s + 1 + B: below 5 (1 + B).
-// With the conversion's two a code is off by at most 7, and the order of two that are 17 apart is
-// certain.  A softmax score takes the sum's error besides (its terms' 1.5 d + 2 weighted by e^-d,
-// and 20 additions): below 50, 113 apart.  A group's score is the sum of two codes: twice that.  In
-// kByLogit codes are the upper 24 bits of the logit's order: exact for bf16, else equal codes are
-// not certain.
+// s (1 - s) |l| < 0.23 reach s; 1 + e and its reciprocal add 3 s: below 4.  The bias in code units
+// is off by 2, the fma by 1/2, the conversion by 1: a code by less than 8, and the order of two
+// that are 17 apart is certain.  A softmax score takes the sum's error besides (its terms' 1.5 d + 2
+// weighted by e^-d, and 20 additions): below 50, 113 apart.  A group's score is the sum of two
+// codes: twice that.  In kByLogit codes are the upper 24 bits of the logit's order: exact for bf16,
+// else equal codes are not certain.  What is no number, or -infinity, has a code at the bottom of
+// its kind, as have the places past E: a row that comes down to it is not certain either.
 template <int M, bool BF16, int BY>
 __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wide, bool count) {
-  __shared__ double group[4][256];
+  __shared__ double score[4][256];
+  __shared__ uint64_t key_of[4][256];
   __shared__ uint32_t hist[256];
   if (count) {   // the only workgroup: it counts as well
     hist[threadIdx.x] = 0;
@@ -292,16 +268,18 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wid
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sl = lane & 15, slot = lane >> 4;
   const int E = a.n_experts, TK = a.top_k, LG = 16 / a.n_groups;
   const bool groups = a.top_groups < a.n_groups;
-  float bias[BY == kByLogit ? 1 : M], low = 0.f, unit = 0.f;
+  float bias[BY == kByLogit ? 1 : M], unit = 0.f;   // c's code is s * unit + bias: 1 .. 2^24 - 15
   if constexpr (BY != kByLogit) {
     float b = 0.f;
 #pragma unroll
     for (int i = 0; i < M; ++i) {
-      bias[i] = a.bias != nullptr && M * sl + i < E ? a.bias[M * sl + i] : 0.f;
+      bias[i] = M * sl + i >= E ? -INFINITY : a.bias != nullptr ? a.bias[M * sl + i] : 0.f;
       if (fabsf(bias[i]) < INFINITY) b = fmaxf(b, fabsf(bias[i]));
     }
-    low = row_max(b);
-    unit = 16777200.f / (1.f + 2.f * low);   // codes 1 .. 2^24 - 1, larger c (an infinite bias) clamped
+    b = row_max(b);
+    unit = 16777200.f / (1.f + 2.f * b);
+#pragma unroll
+    for (int i = 0; i < M; ++i) bias[i] = (bias[i] + b) * unit + 1.f;
   }
   const int64_t stride = (int64_t)gridDim.x * 16, last = a.n_rows - 1;
   int64_t r = ((int64_t)blockIdx.x * 4 + wave) * 4 + slot;
@@ -330,9 +308,8 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wid
       total = row_sum((part[0] + part[1]) + (part[2] + part[3]));
     }
     const float inv = BY == kBySoftmax ? __builtin_amdgcn_rcpf(total) : 0.f;
-    uint32_t m[DEPTH];
-#pragma unroll
-    for (int d = 0; d < DEPTH; ++d) m[d] = 0;
+    typedef uint32_t Keys __attribute__((ext_vector_type(DEPTH)));   // an array's selects become indexed ones
+    Keys m = 0;
 #pragma unroll
     for (int i = 0; i < M; ++i) {
       const int e = M * sl + i;
@@ -341,11 +318,10 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wid
         code = total_order_bits(fmaxf(cur[i], -INFINITY) + 0.0f) >> 8;   // NaN as -infinity, -0 as 0
       } else {
         const float s = BY == kBySigmoid ? __builtin_amdgcn_rcpf(1.f + exp_fast(-cur[i])) : cur[i] * inv;
-        // v_cvt takes NaN and what is below 0 to 0
-        code = (uint32_t)fminf(fmaxf(((s + bias[i]) + low) * unit + 1.f, 1.f), 16777215.f);
+        // v_cvt takes NaN and what is below 0 to 0, +infinity to 2^32 - 1: the largest code
+        code = to_u32(fmaf(s, unit, bias[i]));
       }
-      uint32_t x = (code << 8) | (uint32_t)(255 - e);
-      x = e < E ? x : 0u;
+      const uint32_t x = (code << 8) | (uint32_t)(255 - e);
 #pragma unroll
       for (int d = DEPTH - 1; d > 0; --d) m[d] = med_u32(m[d - 1], m[d], x);
       m[0] = max_u32(m[0], x);
@@ -365,7 +341,8 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wid
       if (LG > 4) join(dpp<0x141>(g0), dpp<0x141>(g1));
       const uint32_t score = BY != kByLogit && a.group_best > 1 ? g0 + g1 : g0;
       const uint32_t key = (score << 4) | (uint32_t)(15 - sl / LG);
-      const bool kept = (int)above<15>(key) < a.top_groups * LG;
+      const int over = (int)(LG == 1 ? above<1>(key) : LG == 2 ? above<2>(key) : LG == 4 ? above<4>(key) : above<8>(key));
+      const bool kept = over < a.top_groups;
       // the least kept score and the largest other
       const uint32_t least = ~row_max_u32(kept ? ~score : 0u), most = row_max_u32(kept ? 0u : score);
       unsure = least < most + 2 * APART || (BY == kByLogit && least <= kNegInfCode);
@@ -399,36 +376,23 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wid
     const float d = a.sigmoid ? -fabsf(x) : x - top;
     float e = expf(d);
     if (!a.sigmoid) e += e * ((x - d) - top);   // what the rounding of the difference took
-    float s = a.sigmoid ? (x < 0.f ? e : 1.f) / (1.f + e) : e / total;
+    float s = a.sigmoid ? (x < 0.f ? e : 1.f) * __builtin_amdgcn_rcpf(1.f + e) : e * __builtin_amdgcn_rcpf(total);
     s = rank ? s : 0.f;
-    const float sum = row_sum(s);
+    float upto = s;   // sums of the ranks up to the lane's
+    upto += __uint_as_float(dpp<0x111>(__float_as_uint(upto)));   // row_shr:1, 2, 4: ranks are below 8
+    upto += __uint_as_float(dpp<0x112>(__float_as_uint(upto)));
+    upto += __uint_as_float(dpp<0x114>(__float_as_uint(upto)));
+    const float sum = row_bcast<7>(upto), want = a.tau * sum;
+    const bool asked = sl + 1 >= a.min_k && sl + 1 < TK;
     // the sum decides little where it is tiny or not a number
-    unsure |= !(sum > 1e-30f);
-    float upto = 0.f;
-    int K = TK;
-    const float want = a.tau * sum, near = 0x1p-18f * sum;
-    auto step = [&](float v, int j) {
-      if (j < TK) {
-        upto += v;
-        if (j + 1 >= a.min_k && j + 1 < TK) {
-          unsure |= fabsf(upto - want) <= near;
-          if (K == TK && upto >= want) K = j + 1;
-        }
-      }
-    };
-    step(row_bcast<0>(s), 0);
-    step(row_bcast<1>(s), 1);
-    step(row_bcast<2>(s), 2);
-    step(row_bcast<3>(s), 3);
-    step(row_bcast<4>(s), 4);
-    step(row_bcast<5>(s), 5);
-    step(row_bcast<6>(s), 6);
-    step(row_bcast<7>(s), 7);
+    unsure |= !(sum > 1e-30f) || (asked && fabsf(upto - want) <= 0x1p-18f * sum);
+    const uint32_t enough = (uint32_t)(__ballot(asked && upto >= want) >> (16 * slot)) & 0xFFFFu;
+    const int K = enough != 0 ? __builtin_ctz(enough) + 1 : TK;
     const uint64_t odd = __ballot(unsure && r <= last);
     if (r <= last && (odd >> (16 * slot) & 0xFFFF) == 0) {
       if (rank) {
         a.expert_idx[r * TK + sl] = my_id;
-        a.expert_w[r * TK + sl] = (a.renormalize ? s / sum : s) * a.scale;
+        a.expert_w[r * TK + sl] = (a.renormalize ? s * __builtin_amdgcn_rcpf(sum) : s) * a.scale;
       }
       if (sl == 0 && a.fanout != nullptr) a.fanout[r] = K;
     }
@@ -440,8 +404,7 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wid
   // rows whose order is not certain, each by the whole wave
   for (; again != 0; again &= again - 1) {
     const int at = __builtin_ctzll(again);
-    route_exact<4>(a, first + (at >> 2) * stride + (at & 3), lane, group[wave]);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+    route_exact(a, first + (at >> 2) * stride + (at & 3), lane, score[wave], key_of[wave]);
   }
   if (count) {
     __syncthreads();   // the rows are written
@@ -505,11 +468,9 @@ hipError_t launch_moe_route(const RouteArgs& a, hipStream_t s) {
     if (count) return e;
   } else {
     const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>((a.n_rows + 3) / 4, 4096))), blk(256);   // no row: the counts are cleared
-    if (E <= 64) route_wave_kernel<1><<<grid, blk, 0, s>>>(a);
-    else if (E <= 128) route_wave_kernel<2><<<grid, blk, 0, s>>>(a);
-    else if (E <= 256) route_wave_kernel<4><<<grid, blk, 0, s>>>(a);
-    else if (E <= 512) route_wave_kernel<8><<<grid, blk, 0, s>>>(a);
-    else route_wave_kernel<16><<<grid, blk, 0, s>>>(a);
+    if (E <= 256) route_wave_kernel<256><<<grid, blk, 0, s>>>(a);
+    else if (E <= 512) route_wave_kernel<512><<<grid, blk, 0, s>>>(a);
+    else route_wave_kernel<1024><<<grid, blk, 0, s>>>(a);
     e = hipGetLastError();
   }
   if (e != hipSuccess || a.expert_count == nullptr || a.n_rows == 0) return e;
