@@ -5,7 +5,6 @@
 // row; the pairs of a token are joined in rank order, in f32.  Within an expert the order of the
 // pairs hangs on LDS atomics, but rows do not meet and the products are exact in i32: the result
 // does not.
-#include <cstdlib>
 #include "i8_rows.h"
 #include "i8_tiles.h"
 
@@ -149,7 +148,7 @@ __device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcp
 // h of 32 MI rows x BN / 2 channels: of a wave's BN / 4 columns the first half are gate
 // channels, the second the same channels of up.
 template <int MI, int BN, int NST>
-__global__ __launch_bounds__(I8_WAVES * 64, 2) void experts_gate_up_kernel(ExpertsArgs a) {
+__global__ __launch_bounds__(I8_WAVES * 64, i8_occupancy(MI, BN, NST)) void experts_gate_up_kernel(ExpertsArgs a) {
   using Tile = I8Tile<MI, BN, NST>;
   constexpr int NI = Tile::NI, BM = Tile::BM, W = BN / 8;   // channels of a wave
   __shared__ __attribute__((aligned(1024))) unsigned char lds[Tile::LDS];
@@ -209,7 +208,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // W_down h of 32 MI rows x BN channels; rows leave through LDS, whole lines of each pair's part
 template <bool F16, int MI, int BN, int NST>
-__global__ __launch_bounds__(I8_WAVES * 64, 2) void experts_down_kernel(ExpertsArgs a) {
+__global__ __launch_bounds__(I8_WAVES * 64, i8_occupancy(MI, BN, NST)) void experts_down_kernel(ExpertsArgs a) {
   using Tile = I8Tile<MI, BN, NST>;
   constexpr int NI = Tile::NI;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[Tile::LDS];
@@ -263,55 +262,65 @@ __global__ __launch_bounds__(I8_WAVES * 64, 2) void experts_down_kernel(ExpertsA
   }
 }
 
-// y of a token: its pairs' parts in rank order, eight channels a thread
+// y of a token: its pairs' parts in rank order, 512 channels a wave.  Lane j reads the token's
+// pair j; what is chosen by it is then uniform.
 template <bool OUT_BF16>
 __global__ __launch_bounds__(256) void experts_join_kernel(ExpertsArgs a) {
-  constexpr int G = 4;   // parts under way at once
-  const int eights = a.d_model / 8;
-  const int64_t units = a.n_rows * eights;
-  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
-    const int64_t n = u / eights;
-    const int c = (int)(u - n * eights) * 8;
+  constexpr int G = 2;   // parts under way at once: more waves hide more (33,792 rows 331 us, with four 363)
+  const int lane = threadIdx.x & 63, d = a.d_model, chunks = (d + 511) / 512;
+  const int units = (int)a.n_rows * chunks;
+  for (int u = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); u < units; u += gridDim.x * 4) {
+    const int n = u / chunks, c = (u - n * chunks) * 512 + lane * 8;
+    int e = -1;
+    float w = 0.f;
+    if (lane < a.top_k) {
+      const int32_t p = n * a.top_k + lane;
+      e = pair_expert(a, p);
+      if (e >= 0) w = OUT_BF16 ? a.ew[p] * (a.hs[p] / kPartUnit) : a.ew[p];
+    }
     float y[8] = {};
-    for (int j0 = 0; j0 < a.top_k; j0 += G) {
-      float v[G][8], s[G][8], w[G];
+    for (uint64_t here = __ballot(e >= 0); here != 0;) {
+      u32x4 v[G][OUT_BF16 ? 1 : 2];
+      f32x4 s[G][2];
+      float wj[G];
+      int got = 0;
 #pragma unroll
-      for (int j = 0; j < G; ++j) {
-        const int32_t p = (int32_t)(n * a.top_k + std::min(j0 + j, a.top_k - 1));
-        const int e = j0 + j < a.top_k ? pair_expert(a, p) : -1;
-        w[j] = 0.f;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[j][k] = s[j][k] = 0.f;
-        if (e < 0) continue;
-        w[j] = a.ew[p];
-        if (OUT_BF16) {
-          w[j] *= a.hs[p] / kPartUnit;
-          const f16x8 x = *(const f16x8*)((const _Float16*)a.part + (int64_t)p * a.d_model + c);
-          const f32x4* ws = (const f32x4*)(a.s_down + (int64_t)e * a.d_model + c);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            v[j][k] = (float)x[k];
-            s[j][k] = ws[k / 4][k % 4];
-          }
-        } else {
-          const f32x4* x = (const f32x4*)((const float*)a.part + (int64_t)p * a.d_model + c);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            v[j][k] = x[k / 4][k % 4];
-            s[j][k] = 1.f;
+      for (int g = 0; g < G; ++g) {
+        if (here == 0) break;
+        const int j = __builtin_ctzll(here);
+        here &= here - 1;
+        got = g + 1;
+        wj[g] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(w), j));
+        const int ej = __builtin_amdgcn_readlane(e, j);
+        if (c < d) {
+          const unsigned char* part = (const unsigned char*)a.part + ((int64_t)n * a.top_k + j) * d * (OUT_BF16 ? 2 : 4);
+          if (OUT_BF16) {
+            v[g][0] = __builtin_nontemporal_load((const u32x4*)(part + c * 2));
+            const f32x4* ws = (const f32x4*)(a.s_down + (int64_t)ej * d + c);
+            s[g][0] = ws[0];
+            s[g][1] = ws[1];
+          } else {
+            v[g][0] = ((const u32x4*)(part + c * 4))[0];
+            v[g][1] = ((const u32x4*)(part + c * 4))[1];
           }
         }
       }
 #pragma unroll
-      for (int j = 0; j < G; ++j)
+      for (int g = 0; g < G; ++g) {
+        if (g >= got) break;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) y[k] += w[j] * (v[j][k] * s[j][k]);
+        for (int k = 0; k < 8; ++k) {
+          const float x = OUT_BF16 ? (float)__builtin_bit_cast(f16x8, v[g][0])[k] * s[g][k / 4][k % 4] : __uint_as_float(v[g][k / 4][k % 4]);
+          y[k] += wj[g] * x;
+        }
+      }
     }
+    if (c >= d) continue;
     if (OUT_BF16) {
-      *(u32x4*)((uint16_t*)a.y + n * a.d_model + c) =
+      *(u32x4*)((uint16_t*)a.y + (int64_t)n * d + c) =
           u32x4{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])};
     } else {
-      f32x4* to = (f32x4*)((float*)a.y + n * a.d_model + c);
+      f32x4* to = (f32x4*)((float*)a.y + (int64_t)n * d + c);
       to[0] = f32x4{y[0], y[1], y[2], y[3]};
       to[1] = f32x4{y[4], y[5], y[6], y[7]};
     }
@@ -349,24 +358,20 @@ hipError_t launch_chunk(const ExpertsArgs& a, hipStream_t s) {
   hipError_t e = launch_start(a, s);
   if (e != hipSuccess) return e;
   switch (a.tile_rows) {
-    case 32: e = launch_gate_up<1, 128, 7>(a, s); break;
-    case 64: e = launch_gate_up<2, 256, 3>(a, s); break;
+    case 64: e = launch_gate_up<2, 128, 3>(a, s); break;
     case 128: e = launch_gate_up<4, 256, 3>(a, s); break;
-    case 192: e = launch_gate_up<6, 256, 2>(a, s); break;
     default: e = launch_gate_up<8, 256, 2>(a, s); break;
   }
   if (e != hipSuccess) return e;
   e = launch_i8_quantize(I8Args{a.h, a.hq, a.hs, a.n_rows * a.top_k, a.d_ffn, a.d_ffn, a.head, a.pairs}, s);
   if (e != hipSuccess) return e;
   switch (a.tile_rows) {
-    case 32: e = launch_down<1, 128, 7>(a, s); break;
-    case 64: e = launch_down<2, 256, 3>(a, s); break;
+    case 64: e = launch_down<2, 128, 3>(a, s); break;
     case 128: e = launch_down<4, 256, 3>(a, s); break;
-    case 192: e = launch_down<6, 256, 2>(a, s); break;
     default: e = launch_down<8, 256, 2>(a, s); break;
   }
   if (e != hipSuccess) return e;
-  const unsigned join = (unsigned)std::min<int64_t>((a.n_rows * (a.d_model / 8) + 255) / 256, 1 << 16);
+  const unsigned join = (unsigned)std::min<int64_t>((a.n_rows * ((a.d_model + 511) / 512) + 3) / 4, 1 << 16);
   if (a.y_bf16) experts_join_kernel<true><<<dim3(join), dim3(256), 0, s>>>(a);
   else experts_join_kernel<false><<<dim3(join), dim3(256), 0, s>>>(a);
   return hipGetLastError();
@@ -374,10 +379,15 @@ hipError_t launch_chunk(const ExpertsArgs& a, hipStream_t s) {
 
 }  // namespace
 
+// The pairs of an expert on average, an upper bound where others hold experts too.  Few: 64 rows x
+// 128 columns, two workgroups a unit, whose time is that of the weights (64 tokens, 6 of 256
+// experts: gate and up 343 us, down 170; 32 x 128 the same, 64 x 256 alone on a unit 350 and 175).
+// Enough to fill them: 128 x 256 (2100 tokens, 6 of 64: 106 and 63 us against 123 and 68 in 64 x 128,
+// 131 and 71 in 256 x 256), then 256 x 256 (33,792 tokens, 6 of 256: 2606 and 1450 against 2897 and
+// 1597 in 128 x 256).
 int32_t experts_tile_rows(int64_t n_pairs, int32_t n_experts) {
   const int64_t avg = n_pairs / n_experts;
-  if (getenv("TILE_ROWS")) return atoi(getenv("TILE_ROWS"));
-  return n_pairs <= 16 ? 32 : avg <= 48 ? 64 : avg <= 256 ? 128 : 256;
+  return avg <= 128 ? 64 : avg <= 384 ? 128 : 256;
 }
 
 hipError_t launch_experts(const ExpertsArgs& all, hipStream_t s) {

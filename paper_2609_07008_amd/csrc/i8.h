@@ -80,7 +80,7 @@ struct ExpertsArgs {
   int32_t tile_rows;
 };
 
-// rows of a tile (32 .. 256), by the pairs that an expert has on average
+// rows of a tile (64, 128 or 256), by the pairs that an expert has on average
 int32_t experts_tile_rows(int64_t n_pairs, int32_t n_experts);
 inline int64_t experts_max_tiles(int64_t n_pairs, int32_t n_experts, int32_t tile_rows) {
   return n_pairs / tile_rows + (n_experts < n_pairs ? n_experts : n_pairs);

@@ -36,13 +36,13 @@ __global__ __launch_bounds__(256) void i8_dequantize_kernel(I8Args a, int segs) 
 }
 
 constexpr int kWbGroup = 8;                              // row panels per column panel in the tile walk
-constexpr int64_t kI8FewRows = 32, kI8FewBlocks = 512;   // largest requests of the few-row kernel
+constexpr int64_t kI8FewRows = 32, kI8FewBlocks = 256;   // largest requests of the few-row kernel
 
 // y = W_b z in tiles (i8_tiles.h).  Workgroups go to the 8 XCDs round-robin, so XCD x takes a
 // contiguous range of tiles, and inside it tiles walk 8 row panels per column panel.  The output
 // leaves through LDS as whole 128-byte lines.
 template <bool OUT_BF16, int MI, int BN, int NST>
-__global__ __launch_bounds__(I8_WAVES * 64, 2) void wb_i8_tile_kernel(WbI8Args a, int m_tiles, int n_tiles, bool stream_out) {
+__global__ __launch_bounds__(I8_WAVES * 64, i8_occupancy(MI, BN, NST)) void wb_i8_tile_kernel(WbI8Args a, int m_tiles, int n_tiles, bool stream_out) {
   using Tile = I8Tile<MI, BN, NST>;
   constexpr int NI = Tile::NI, BM = Tile::BM;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[Tile::LDS];
@@ -100,8 +100,9 @@ __global__ __launch_bounds__(I8_WAVES * 64, 2) void wb_i8_tile_kernel(WbI8Args a
         *(f32x4 MLA_LDS*)(sb + lc * ROW + (((j * 4 + lg) ^ (lc & SW)) * 16)) = v;
     }
 #pragma unroll
-    for (int p = 0; p < 16 / RPI; ++p) {
+    for (int p = 0; p < (16 + RPI - 1) / RPI; ++p) {
       const int r = p * RPI + rl;
+      if (RPI > 16 && r >= 16) continue;   // half of the lanes hold all rows
       const u32x4 v = *(const u32x4 MLA_LDS*)(sb + r * ROW + ((cl ^ (r & SW)) * 16));
       const int64_t m = m0 + Tile::row_of(wm, i) + r;
       if (m >= a.n_rows) continue;
@@ -215,25 +216,34 @@ hipError_t launch_tiles(const WbI8Args& a, hipStream_t s) {
 
 template <bool OUT_BF16>
 hipError_t launch_out(const WbI8Args& a, hipStream_t s) {
+  // Up to 32 rows and a workgroup of 16 channels a compute unit, the few-row kernel: 4096 -> 4096
+  // at 16 rows 8.2 us, in tiles of 32 x 64 9.4.
   const int64_t few_blocks = ((int64_t)a.d_out + 15) / 16;
   if (a.n_rows <= kI8FewRows && few_blocks <= kI8FewBlocks) {
     if (a.n_rows <= 16) wb_i8_rows_kernel<OUT_BF16, 1, 4><<<dim3((unsigned)few_blocks), dim3(I8_WAVES * 64), 0, s>>>(a);
     else wb_i8_rows_kernel<OUT_BF16, 2, 3><<<dim3((unsigned)few_blocks), dim3(I8_WAVES * 64), 0, s>>>(a);
     return hipGetLastError();
   }
-  // the tile whose rounds over the 256 compute units cost least
+  // The tile whose rounds over the 256 compute units cost least: a round of 32 mi rows x 256
+  // channels taken as 6 (mi + 3), x 128 as 2 (mi + 7), x 64 as 9 and 10 (mi = 1, 2; two fit a unit,
+  // and a second round comes in under the first).  At 4096 channels, weights from memory: 64 rows
+  // 9.9 us at 32 x 64 against 14.8 at 32 x 128, 300 rows 16.6 at 64 x 128 against 21 at 32 x 64, 1000 rows 23.8 at 128 x 128 against 26.4 at 64 x 256, 2100 rows 41.6 at 160 x 256
+  // against 46.7 at 256 x 256, 4096 rows 58 at 256 x 256 against 71 at 128 x 256; 33 rows of 7168 ->
+  // 16384 23.7 at 64 x 64 against 27.5 at 32 x 128.
   int best = 8;
   int64_t cost = INT64_MAX;
-  auto tile = [&](int id, int mi, int bn, int w) {
+  auto tile = [&](int id, int mi, int bn, int w, int first) {
     const int64_t tiles = (a.n_rows + 32 * mi - 1) / (32 * mi) * ((a.d_out + bn - 1) / bn);
-    const int64_t c = (tiles + 255) / 256 * w;
+    const int64_t c = (tiles + 255) / 256 * w + first;
     if (c < cost) {
       cost = c;
       best = id;
     }
   };
-  for (int mi = 8; mi >= 2; --mi) tile(mi, mi, 256, 3 * (mi + 3));
-  for (int mi = 4; mi >= 1; --mi) tile(10 + mi, mi, 128, mi + 7);
+  for (int mi = 8; mi >= 2; --mi) tile(mi, mi, 256, 6 * (mi + 3), 0);
+  for (int mi = 4; mi >= 1; --mi) tile(10 + mi, mi, 128, 2 * (mi + 7), 0);
+  tile(22, 2, 64, 10, 1);
+  tile(21, 1, 64, 9, 1);
   switch (best) {
     case 2: return launch_tiles<OUT_BF16, 2, 256, 3>(a, s);
     case 3: return launch_tiles<OUT_BF16, 3, 256, 3>(a, s);
@@ -245,6 +255,8 @@ hipError_t launch_out(const WbI8Args& a, hipStream_t s) {
     case 12: return launch_tiles<OUT_BF16, 2, 128, 6>(a, s);
     case 13: return launch_tiles<OUT_BF16, 3, 128, 5>(a, s);
     case 14: return launch_tiles<OUT_BF16, 4, 128, 4>(a, s);
+    case 21: return launch_tiles<OUT_BF16, 1, 64, 6>(a, s);
+    case 22: return launch_tiles<OUT_BF16, 2, 64, 5>(a, s);
     default: return launch_tiles<OUT_BF16, 8, 256, 2>(a, s);
   }
 }

@@ -19,6 +19,9 @@ constexpr int I8_ROWB = 128;   // bytes of a row of a slice
 
 __device__ __forceinline__ int i8_swz(int r) { return (r >> 1) & 7; }
 
+// waves a SIMD: two workgroups a unit where both fit its LDS
+constexpr int i8_occupancy(int mi, int bn, int nst) { return (32 * mi + bn) * I8_ROWB * nst <= 80 * 1024 ? 4 : 2; }
+
 template <int MI, int BN, int NST>
 struct I8Tile {
   static constexpr int NI = BN / 64, BM = 32 * MI;

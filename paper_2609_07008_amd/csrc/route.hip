@@ -397,8 +397,9 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wid
       if (sl == 0 && a.fanout != nullptr) a.fanout[r] = K;
     }
     // a bit a row and turn
-    again |= (uint64_t)((odd & 0xFFFF) != 0 | ((odd >> 16 & 0xFFFF) != 0) << 1 | ((odd >> 32 & 0xFFFF) != 0) << 2 | ((odd >> 48) != 0) << 3)
-             << (4 * turn);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if ((odd >> (16 * k) & 0xFFFF) != 0) again |= 1ull << (4 * turn + k);
     ++turn;
   }
   // rows whose order is not certain, each by the whole wave
