@@ -520,6 +520,19 @@ def cache_attend(geom, q, pos, pages, seq_pages, cache, page_rows: int, out_o, o
 SCORINGS = {"softmax": 0, "sigmoid": 1}   # MLA_SOFTMAX, MLA_SIGMOID
 
 
+def _route_cfg(top_k, scoring="softmax", n_groups=1, top_groups=1, group_best=1, renormalize=True, scale=1.0, min_k=1, tau=2.0):
+    if scoring not in SCORINGS:
+        _refuse(f"scoring {scoring!r}, expected one of {sorted(SCORINGS)}")
+    return RouteCfg(SCORINGS[scoring], n_groups, top_groups, group_best, top_k, min_k, bool(renormalize), scale, tau)
+
+
+def check_route(n_experts: int, top_k: int, **cfg):
+    """Host-only: refuses what mla_moe_route would refuse for these experts and this choice
+    (keyword arguments of moe_route)."""
+    _check(LIB.mla_moe_route(0, int(n_experts), None, MLA_F32, int(n_experts), None, ctypes.byref(_route_cfg(int(top_k), **cfg)), None, None, None,
+                             None, None))
+
+
 def moe_route(logits, expert_idx, expert_w, fanout=None, expert_count=None, bias=None, scoring: str = "softmax", n_groups: int = 1,
               top_groups: int = 1, group_best: int = 1, renormalize: bool = True, scale: float = 1.0, min_k: int = 1,
               tau: float = 2.0, stream=None):
@@ -541,9 +554,7 @@ def moe_route(logits, expert_idx, expert_w, fanout=None, expert_count=None, bias
         _tensor("expert_count", expert_count, dev, torch.int32, (e,))
     if bias is not None:
         _tensor("bias", bias, dev, torch.float32, (e,))
-    if scoring not in SCORINGS:
-        _refuse(f"scoring {scoring!r}, expected one of {sorted(SCORINGS)}")
-    cfg = RouteCfg(SCORINGS[scoring], n_groups, top_groups, group_best, k, min_k, bool(renormalize), scale, tau)
+    cfg = _route_cfg(k, scoring, n_groups, top_groups, group_best, renormalize, scale, min_k, tau)
     _check(LIB.mla_moe_route(n, e, _addr(logits), MLA_BF16 if bf16 else MLA_F32, logits.stride(0) if n > 1 else e, _addr(bias),
                              ctypes.byref(cfg), _addr(expert_idx), _addr(expert_w), _addr(fanout), _addr(expert_count),
                              _queue(stream, dev)))

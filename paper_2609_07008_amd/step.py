@@ -188,3 +188,55 @@ class DecodeStep:
         self.oproj(w_o, stream)
         self.project(wb_codes, wb_scales, stream)
         return self.y
+
+
+class MoeStep:
+    """A mixture-of-experts layer for a fixed batch of n_rows tokens:
+      mla_shared_wb      logits = W_r x, the router's own weight in bf16,
+      mla_moe_route      each row's experts, weights and (tau <= 1) fanout,
+      mla_moe_experts_i8 y = the weighted experts in 8 bits,
+    for the experts [first_expert, first_expert + n_local) of n_experts; with a share of them
+    run() returns this device's part of y.  Every call only enqueues kernels: run() may be
+    captured and replayed.  Buffers and argument marshalling only."""
+
+    def __init__(self, n_rows: int, d_model: int, d_ffn: int, n_experts: int, top_k: int, device="cuda", n_local=None,
+                 first_expert: int = 0, min_k=None, tau: float = 2.0, y_dtype=torch.bfloat16, with_count: bool = False, **route):
+        """route: scoring, n_groups, top_groups, group_best, renormalize, scale of mla.moe_route."""
+        self.n_local = int(n_experts if n_local is None else n_local)
+        self.first_expert, self.n_experts, self.d_model = int(first_expert), int(n_experts), int(d_model)
+        if self.n_local < 1 or self.first_expert < 0 or self.first_expert + self.n_local > self.n_experts:
+            raise mla.MlaError(2, f"experts [{first_expert}, {first_expert} + {self.n_local}) of {n_experts}")
+        if d_model % 64 or d_model > mla.WB_MAX_D_IN:
+            raise mla.MlaError(2 if d_model % 64 else 3, f"d_model {d_model}; the router's product takes multiples of 64 up to {mla.WB_MAX_D_IN}")
+        self.route_args = dict(route, min_k=int(top_k if min_k is None else min_k), tau=float(tau))
+        mla.check_route(n_experts, top_k, **self.route_args)
+        dev = torch.device(device)
+        ws = mla.moe_experts_i8_query(n_rows, d_model, d_ffn, self.n_local, top_k, y_dtype)
+        self.ws = torch.empty((ws,), dtype=torch.uint8, device=dev)
+        self.logits = torch.empty((n_rows, n_experts), dtype=torch.float32, device=dev)
+        self.expert_idx = torch.empty((n_rows, top_k), dtype=torch.int32, device=dev)
+        self.expert_w = torch.empty((n_rows, top_k), dtype=torch.float32, device=dev)
+        self.fanout = torch.empty((n_rows,), dtype=torch.int32, device=dev)
+        self.count = torch.empty((n_experts,), dtype=torch.int32, device=dev) if with_count else None
+        self.y = torch.empty((n_rows, d_model), dtype=y_dtype, device=dev)
+
+    def route(self, x, w_r, bias=None, stream=None):
+        mla.check_tensor("x", x, torch.bfloat16)
+        mla.check_tensor("w_r", w_r, torch.bfloat16)
+        if x.shape != (self.logits.shape[0], self.d_model) or w_r.shape != (self.n_experts, self.d_model):
+            raise mla.MlaError(2, f"x is {tuple(x.shape)}, w_r {tuple(w_r.shape)}; made for {self.logits.shape[0]} rows, [{self.n_experts}, {self.d_model}]")
+        mla.shared_wb(x, w_r, self.logits, stream)
+        mla.moe_route(self.logits, self.expert_idx, self.expert_w, self.fanout, self.count, bias=bias, stream=stream, **self.route_args)
+
+    def experts(self, x, w_gate_up, s_gate_up, w_down, s_down, stream=None):
+        mla.moe_experts_i8(x, self.expert_idx, self.expert_w, w_gate_up, s_gate_up, w_down, s_down, self.y, self.ws, fanout=self.fanout,
+                           first_expert=self.first_expert, stream=stream)
+
+    def run(self, x, w_r, w_gate_up, s_gate_up, w_down, s_down, bias=None, stream=None):
+        """x [n_rows, d_model] bfloat16, w_r [n_experts, d_model] bfloat16, bias [n_experts]
+        float32 or None, the weights as mla.moe_experts_i8 takes them.  Returns y [n_rows,
+        d_model].  Every call checks its own arguments: where one refuses, those before it have
+        run, and run() may be called again."""
+        self.route(x, w_r, bias, stream)
+        self.experts(x, w_gate_up, s_gate_up, w_down, s_down, stream)
+        return self.y

@@ -170,3 +170,23 @@ def test_thousands_of_pairs():
     some = torch.randperm(n, generator=torch.Generator().manual_seed(1))[:60].cuda()
     want, off, _ = layer.want(x[some], idx[some], w[some], fanout[some])
     assert (np.abs(y[some].cpu().numpy() - want) <= off).all()
+
+
+def test_rows_past_a_chunk():
+    """More rows than are taken at a time: each chunk's rows as by themselves."""
+    import torch
+    n = 65536 + 700
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randn((n, 64), generator=gen, device="cuda").to(torch.bfloat16)
+    idx = torch.randint(0, 5, (n, 2), generator=gen, device="cuda", dtype=torch.int32)
+    w, fanout = torch.rand((n, 2), generator=gen, device="cuda"), torch.randint(0, 3, (n,), generator=gen, device="cuda", dtype=torch.int32)
+    layer = Layer(64, 64, 4, 10, first=1)
+    for out in ("f32", "bf16"):
+        y = layer.run(x, idx, w, fanout, out)
+        for lo in (0, 65400, 65536, n - 100):
+            part = slice(lo, lo + 100)
+            rows = layer.run(x[part].contiguous(), idx[part].contiguous(), w[part].contiguous(), fanout[part].contiguous(), out)
+            assert torch.equal(rows, y[part])
+    some = torch.tensor([0, 65535, 65536, n - 1], device="cuda")
+    want, off, _ = layer.want(x[some], idx[some], w[some], fanout[some])
+    assert (np.abs(layer.run(x, idx, w, fanout)[some].cpu().numpy() - want) <= off).all()

@@ -113,3 +113,15 @@ def test_binding_refuses_host_and_wrong_tensors(mla):
                  lambda: mla.moe_experts_i8(x, i, w, wgu, torch.zeros((1, 128)), wd, torch.zeros((1, 64)), x, ws)):
         with pytest.raises(mla.MlaError):
             call()
+
+
+def test_moe_step_refusals(mla):
+    """What a step could not run is refused where it is made."""
+    from paper_2609_07008_amd.step import MoeStep
+    ok = dict(n_rows=2, d_model=128, d_ffn=64, n_experts=16, top_k=4, device="cpu")
+    MoeStep(**ok)
+    for bad in (dict(n_rows=-1), dict(d_model=96), dict(d_model=16448), dict(d_ffn=32), dict(n_experts=3), dict(top_k=9), dict(n_local=17), dict(n_local=0),
+                dict(first_expert=1), dict(first_expert=-1, n_local=3), dict(min_k=5), dict(min_k=0), dict(tau=NAN), dict(scoring="tanh"),
+                dict(n_groups=5, top_groups=5), dict(n_groups=4, top_groups=5), dict(n_groups=8, top_groups=1), dict(scale=INF)):
+        with pytest.raises(mla.MlaError):
+            MoeStep(**{**ok, **bad})
