@@ -148,13 +148,10 @@ __device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcp
 // h of 32 MI rows x BN / 2 channels: of a wave's BN / 4 columns the first half are gate
 // channels, the second the same channels of up.
 template <int MI, int BN, int NST>
-__global__ __launch_bounds__(I8_WAVES * 64, i8_occupancy(MI, BN, NST)) void experts_gate_up_kernel(ExpertsArgs a) {
+__device__ __forceinline__ void gate_up_tile(const ExpertsArgs& a, const Place& at, unsigned char* lds) {
   using Tile = I8Tile<MI, BN, NST>;
-  constexpr int NI = Tile::NI, BM = Tile::BM, W = BN / 8;   // channels of a wave
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[Tile::LDS];
+  constexpr int NI = Tile::NI, W = BN / 8;   // channels of a wave
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Place at = my_tile(a, (a.d_ffn + BN / 2 - 1) / (BN / 2));
-  if (!at.any) return;
   const int f0 = at.col * (BN / 2), d = a.d_model, f = a.d_ffn;
   const int8_t* w = a.w_gu + (int64_t)at.expert * 2 * f * d;
   Tile tile;
@@ -208,13 +205,10 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // W_down h of 32 MI rows x BN channels; rows leave through LDS, whole lines of each pair's part
 template <bool F16, int MI, int BN, int NST>
-__global__ __launch_bounds__(I8_WAVES * 64, i8_occupancy(MI, BN, NST)) void experts_down_kernel(ExpertsArgs a) {
+__device__ __forceinline__ void down_tile(const ExpertsArgs& a, const Place& at, unsigned char* lds) {
   using Tile = I8Tile<MI, BN, NST>;
   constexpr int NI = Tile::NI;
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[Tile::LDS];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Place at = my_tile(a, (a.d_model + BN - 1) / BN);
-  if (!at.any) return;
   const int n0 = at.col * BN, d = a.d_model, f = a.d_ffn;
   Tile tile;
   tile.aim(wave, lane, [&](bool is_a, int r0, int r, const unsigned char*& src, uint32_t& off) {
@@ -327,19 +321,51 @@ __global__ __launch_bounds__(256) void experts_join_kernel(ExpertsArgs a) {
   }
 }
 
-template <int MI, int BN, int NST>
+// LDS of a kernel of tiles of 32 MI rows x BN, three or (MI = 8) two slices, and of the lower ones in it
+constexpr int experts_lds(int mi, int bn) {
+  const int own = (32 * mi + bn) * I8_ROWB * (mi == 8 ? 2 : 3), low = mi > 2 ? (16 * mi + bn) * I8_ROWB * 3 : 0;
+  return own > low ? own : low;
+}
+
+// A tile with half of its rows, or a quarter, goes as a lower one: with the sums of the others
+// left out, what is left of a step is its loads' way, which more slices in LDS cover.
+template <int MI, int BN>
+__global__ __launch_bounds__(I8_WAVES * 64, experts_lds(MI, BN) <= 80 * 1024 ? 4 : 2) void experts_gate_up_kernel(ExpertsArgs a) {
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[experts_lds(MI, BN)];
+  const Place at = my_tile(a, (a.d_ffn + BN / 2 - 1) / (BN / 2));
+  if (!at.any) return;
+  if (MI == 2 || at.rows > 16 * MI) return gate_up_tile<MI, BN, MI == 8 ? 2 : 3>(a, at, lds);
+  if constexpr (MI == 8) {
+    if (at.rows > 64) return gate_up_tile<4, BN, 3>(a, at, lds);
+  }
+  if constexpr (MI > 2) gate_up_tile<2, BN, 3>(a, at, lds);
+}
+
+template <bool F16, int MI, int BN>
+__global__ __launch_bounds__(I8_WAVES * 64, experts_lds(MI, BN) <= 80 * 1024 ? 4 : 2) void experts_down_kernel(ExpertsArgs a) {
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[experts_lds(MI, BN)];
+  const Place at = my_tile(a, (a.d_model + BN - 1) / BN);
+  if (!at.any) return;
+  if (MI == 2 || at.rows > 16 * MI) return down_tile<F16, MI, BN, MI == 8 ? 2 : 3>(a, at, lds);
+  if constexpr (MI == 8) {
+    if (at.rows > 64) return down_tile<F16, 4, BN, 3>(a, at, lds);
+  }
+  if constexpr (MI > 2) down_tile<F16, 2, BN, 3>(a, at, lds);
+}
+
+template <int MI, int BN>
 hipError_t launch_gate_up(const ExpertsArgs& a, hipStream_t s) {
   const int64_t total = experts_max_tiles(a.n_rows * a.top_k, a.n_experts, 32 * MI) * ((a.d_ffn + BN / 2 - 1) / (BN / 2));
-  experts_gate_up_kernel<MI, BN, NST><<<dim3((unsigned)(8 * ((total + 7) / 8))), dim3(I8_WAVES * 64), 0, s>>>(a);
+  experts_gate_up_kernel<MI, BN><<<dim3((unsigned)(8 * ((total + 7) / 8))), dim3(I8_WAVES * 64), 0, s>>>(a);
   return hipGetLastError();
 }
 
-template <int MI, int BN, int NST>
+template <int MI, int BN>
 hipError_t launch_down(const ExpertsArgs& a, hipStream_t s) {
   const int64_t total = experts_max_tiles(a.n_rows * a.top_k, a.n_experts, 32 * MI) * ((a.d_model + BN - 1) / BN);
   const dim3 grid((unsigned)(8 * ((total + 7) / 8))), blk(I8_WAVES * 64);
-  if (a.y_bf16) experts_down_kernel<true, MI, BN, NST><<<grid, blk, 0, s>>>(a);
-  else experts_down_kernel<false, MI, BN, NST><<<grid, blk, 0, s>>>(a);
+  if (a.y_bf16) experts_down_kernel<true, MI, BN><<<grid, blk, 0, s>>>(a);
+  else experts_down_kernel<false, MI, BN><<<grid, blk, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -358,17 +384,17 @@ hipError_t launch_chunk(const ExpertsArgs& a, hipStream_t s) {
   hipError_t e = launch_start(a, s);
   if (e != hipSuccess) return e;
   switch (a.tile_rows) {
-    case 64: e = launch_gate_up<2, 128, 3>(a, s); break;
-    case 128: e = launch_gate_up<4, 256, 3>(a, s); break;
-    default: e = launch_gate_up<8, 256, 2>(a, s); break;
+    case 64: e = launch_gate_up<2, 128>(a, s); break;
+    case 128: e = launch_gate_up<4, 256>(a, s); break;
+    default: e = launch_gate_up<8, 256>(a, s); break;
   }
   if (e != hipSuccess) return e;
   e = launch_i8_quantize(I8Args{a.h, a.hq, a.hs, a.n_rows * a.top_k, a.d_ffn, a.d_ffn, a.head, a.pairs}, s);
   if (e != hipSuccess) return e;
   switch (a.tile_rows) {
-    case 64: e = launch_down<2, 128, 3>(a, s); break;
-    case 128: e = launch_down<4, 256, 3>(a, s); break;
-    default: e = launch_down<8, 256, 2>(a, s); break;
+    case 64: e = launch_down<2, 128>(a, s); break;
+    case 128: e = launch_down<4, 256>(a, s); break;
+    default: e = launch_down<8, 256>(a, s); break;
   }
   if (e != hipSuccess) return e;
   const unsigned join = (unsigned)std::min<int64_t>((a.n_rows * ((a.d_model + 511) / 512) + 3) / 4, 1 << 16);
