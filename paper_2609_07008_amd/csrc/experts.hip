@@ -57,7 +57,33 @@ __device__ void scan_counts(const ExpertsArgs& a, int c, int* place, int* wave_s
   }
 }
 
-constexpr int kOneBlockPairs = 8192;   // pairs that one workgroup counts and places
+constexpr int kBlockPairs = 4;                       // pairs of a thread while they are counted and placed
+constexpr int kOneBlockPairs = 2048 * kBlockPairs;   // pairs that one workgroup counts and places
+
+// experts of up to N pairs of each thread from lo on, all loads under way at once
+template <int N>
+struct Pairs {
+  int e[N];
+  __device__ __forceinline__ Pairs(const ExpertsArgs& a, int64_t lo, int64_t hi) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int64_t p = lo + i * 1024 + threadIdx.x;
+      e[i] = p < hi ? pair_expert(a, (int32_t)p) : -1;
+    }
+  }
+  __device__ __forceinline__ void count(int* hist) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (e[i] >= 0) atomicAdd(&hist[e[i]], 1);
+  }
+  __device__ __forceinline__ void place(const ExpertsArgs& a, int64_t lo, int* at) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int p = (int)lo + i * 1024 + threadIdx.x;
+      if (e[i] >= 0) a.pairs[atomicAdd(&at[e[i]], 1)] = int2{p / a.top_k, p};
+    }
+  }
+};
 
 // Workgroups [0, blocks): the pairs of each expert, counted a share each; a single one places
 // them as well.  The others quantize rows of x.
@@ -69,31 +95,32 @@ __global__ __launch_bounds__(1024) void experts_start_kernel(ExpertsArgs a, int 
                            ((int64_t)blockIdx.x - blocks) * 4 + threadIdx.x / 256, ((int64_t)gridDim.x - blocks) * 4, hist);
     return;
   }
-  for (int i = threadIdx.x; i < a.n_experts; i += 1024) hist[i] = 0;
-  __syncthreads();
-  const int64_t n_pairs = a.n_rows * a.top_k, per = (n_pairs + blocks - 1) / blocks;
-  const int64_t lo = blockIdx.x * per, hi = std::min(lo + per, n_pairs);
-  for (int64_t p = lo + threadIdx.x; p < hi; p += 1024) {
-    const int e = pair_expert(a, (int32_t)p);
-    if (e >= 0) atomicAdd(&hist[e], 1);
-  }
-  __syncthreads();
-  if (blocks > 1) {
-    for (int i = threadIdx.x; i < a.n_experts; i += 1024) a.hist[blockIdx.x * a.n_experts + i] = hist[i];
+  const int64_t n_pairs = a.n_rows * a.top_k;
+  if (blocks == 1) {
+    const Pairs<2 * kBlockPairs> mine(a, 0, n_pairs);
+    for (int i = threadIdx.x; i < a.n_experts; i += 1024) hist[i] = 0;
+    __syncthreads();
+    mine.count(hist);
+    __syncthreads();
+    scan_counts(a, (int)threadIdx.x < a.n_experts ? hist[threadIdx.x] : 0, hist, sums, true);
+    __syncthreads();
+    mine.place(a, 0, hist);
     return;
   }
-  const int c = (int)threadIdx.x < a.n_experts ? hist[threadIdx.x] : 0;
-  scan_counts(a, c, hist, sums, true);
+  for (int i = threadIdx.x; i < a.n_experts; i += 1024) hist[i] = 0;
   __syncthreads();
-  for (int64_t p = lo + threadIdx.x; p < hi; p += 1024) {
-    const int e = pair_expert(a, (int32_t)p);
-    if (e >= 0) a.pairs[atomicAdd(&hist[e], 1)] = int2{(int)p / a.top_k, (int)p};
-  }
+  const int64_t per = (n_pairs + blocks - 1) / blocks, lo = blockIdx.x * per, hi = std::min(lo + per, n_pairs);
+  for (int64_t p = lo; p < hi; p += 1024 * kBlockPairs) Pairs<kBlockPairs>(a, p, hi).count(hist);
+  __syncthreads();
+  for (int i = threadIdx.x; i < a.n_experts; i += 1024) a.hist[blockIdx.x * a.n_experts + i] = hist[i];
 }
 
 // every workgroup adds up the counts of all, and so knows where its own pairs go
 __global__ __launch_bounds__(1024) void experts_place_kernel(ExpertsArgs a) {
   __shared__ int place[kExpertsMax], sums[32];
+  const int64_t n_pairs = a.n_rows * a.top_k, per = (n_pairs + gridDim.x - 1) / gridDim.x;
+  const int64_t lo = blockIdx.x * per, hi = std::min(lo + per, n_pairs);
+  Pairs<kBlockPairs> mine(a, lo, hi);
   int total = 0, before = 0;
   if ((int)threadIdx.x < a.n_experts) {
     const int* h = a.hist + threadIdx.x;
@@ -107,12 +134,8 @@ __global__ __launch_bounds__(1024) void experts_place_kernel(ExpertsArgs a) {
   scan_counts(a, total, place, sums, blockIdx.x == 0);
   if ((int)threadIdx.x < a.n_experts) place[threadIdx.x] += before;
   __syncthreads();
-  const int64_t n_pairs = a.n_rows * a.top_k, per = (n_pairs + gridDim.x - 1) / gridDim.x;
-  const int64_t lo = blockIdx.x * per, hi = std::min(lo + per, n_pairs);
-  for (int64_t p = lo + threadIdx.x; p < hi; p += 1024) {
-    const int e = pair_expert(a, (int32_t)p);
-    if (e >= 0) a.pairs[atomicAdd(&place[e], 1)] = int2{(int)p / a.top_k, (int)p};
-  }
+  mine.place(a, lo, place);
+  for (int64_t p = lo + 1024 * kBlockPairs; p < hi; p += 1024 * kBlockPairs) Pairs<kBlockPairs>(a, p, hi).place(a, p, place);
 }
 
 constexpr int kExpertsGroup = 8;   // row tiles per column tile in the walk of an expert

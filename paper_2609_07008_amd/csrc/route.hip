@@ -37,9 +37,10 @@ __device__ __forceinline__ double from_order_bits(uint64_t k) {
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup"); }
 
 // A row by a whole wave in 64 bits; lane holds experts lane, lane + 64, ...; `score` and `key` are
-// LDS of the wave, [E].  Loops stay rolled: where this runs for one row in hundreds its time is
+// LDS of the wave, [E].  Lane j returns
+// the expert of rank j if the row executes it, else -1.  Loops stay rolled: where this runs for one row in hundreds its time is
 // that of fetching its instructions (unrolled by four, some 150 rows of 264,192 cost 30 us).
-__device__ void route_exact(const RouteArgs& a, int64_t r, int lane, double* score, uint64_t* key) {
+__device__ int route_exact(const RouteArgs& a, int64_t r, int lane, double* score, uint64_t* key) {
   const int E = a.n_experts;
   double m = -INFINITY, sum = 0.0;
   if (!a.sigmoid) {
@@ -140,6 +141,7 @@ __device__ void route_exact(const RouteArgs& a, int64_t r, int lane, double* sco
   }
   if (lane == 0 && a.fanout != nullptr) a.fanout[r] = K;
   in_order();
+  return lane < (a.fanout != nullptr ? K : a.top_k) ? idx : -1;
 }
 
 // any row, a wave each
@@ -287,7 +289,7 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wid
   // write nothing), so the DPP exchanges see whole rows
   const int64_t first = r - slot;
   uint64_t again = 0;
-  int turn = 0;
+  int turn = 0, taken = -1;   // taken: the expert that a lane's rank of the last turn executes
   float cur[M];
   if (r - slot <= last) load_logits<M, BF16>(a, wide, r < last ? r : last, sl, cur);
   for (; r - slot <= last; r += stride) {
@@ -390,6 +392,7 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wid
     const int K = enough != 0 ? __builtin_ctz(enough) + 1 : TK;
     const uint64_t odd = __ballot(unsure && r <= last);
     if (r <= last && (odd >> (16 * slot) & 0xFFFF) == 0) {
+      taken = sl < (a.fanout != nullptr ? K : TK) ? my_id : -1;
       if (rank) {
         a.expert_idx[r * TK + sl] = my_id;
         a.expert_w[r * TK + sl] = (a.renormalize ? s * __builtin_amdgcn_rcpf(sum) : s) * a.scale;
@@ -405,15 +408,11 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wid
   // rows whose order is not certain, each by the whole wave
   for (; again != 0; again &= again - 1) {
     const int at = __builtin_ctzll(again);
-    route_exact(a, first + (at >> 2) * stride + (at & 3), lane, score[wave], key_of[wave]);
+    const int expert = route_exact(a, first + (at >> 2) * stride + (at & 3), lane, score[wave], key_of[wave]);
+    if (count && expert >= 0) atomicAdd(&hist[expert], 1u);
   }
-  if (count) {
-    __syncthreads();   // the rows are written
-    const int n = (int)a.n_rows * TK;
-    if ((int)threadIdx.x < n) {
-      const int row = threadIdx.x / TK;
-      if ((int)threadIdx.x - row * TK < (a.fanout != nullptr ? a.fanout[row] : TK)) atomicAdd(&hist[a.expert_idx[threadIdx.x]], 1u);
-    }
+  if (count) {   // one turn
+    if (taken >= 0) atomicAdd(&hist[taken], 1u);
     __syncthreads();
     if ((int)threadIdx.x < E) a.expert_count[threadIdx.x] = (int32_t)hist[threadIdx.x];
   }
