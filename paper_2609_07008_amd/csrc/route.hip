@@ -3,11 +3,12 @@
 // them the top_k experts, equal ones to the lower index.  Weights are the chosen s.
 //
 // Which expert comes first hangs on values next to one another, so choices and fanouts are those
-// of 64-bit scores.  route_exact computes them so, a row a wave.  Up to 256 experts a row is
-// first tried in 32 bits by 16 lanes (route_row_kernel, four rows a wave): c becomes a 24-bit
-// fixed-point code over its whole range, above the inverted index in a 32-bit key, and whatever
-// hangs on two codes that the errors could have swapped sends its row to route_exact: one in some
-// hundreds of rows of random logits.
+// of 64-bit scores.  route_exact computes them so, a row a wave.  A row is first tried in 32 bits
+// (route_row_kernel, by 16 lanes up to 256 experts, else by a wave): c becomes a fixed-point code of
+// 24 or 22 bits over its whole range, above the inverted index in a 32-bit key, and whatever hangs
+// on two codes that the errors could have swapped sends its row to route_exact: one in some
+// hundreds of rows of random logits.  Where groups do not fall on whole lanes every row takes
+// the 64-bit path.
 #include "rank.h"
 #include "route.h"
 
@@ -172,27 +173,42 @@ __device__ __forceinline__ uint32_t to_u32(float v) {
   return u;
 }
 
-template <int CTRL>
-__device__ __forceinline__ float fmax_dpp(float v) {
-  return fmaxf(v, __uint_as_float(dpp<CTRL>(__float_as_uint(v))));
+// Over the L lanes (16 or 64) of a row, in each of them
+template <int L, class F>
+__device__ __forceinline__ uint32_t over_row(uint32_t v, F&& f) {
+  v = f(v, dpp<0xB1>(v));
+  v = f(v, dpp<0x4E>(v));
+  v = f(v, dpp<0x141>(v));
+  v = f(v, dpp<0x140>(v));
+  if constexpr (L == 64) {
+    const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = f(p[0], p[1]);
+    const auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = f(q[0], q[1]);
+  }
+  return v;
 }
+template <int L>
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+  return over_row<L>(v, [](uint32_t x, uint32_t y) { return max_u32(x, y); });
+}
+template <int L>
 __device__ __forceinline__ float row_max(float v) {
-  v = fmax_dpp<0xB1>(v);
-  v = fmax_dpp<0x4E>(v);
-  v = fmax_dpp<0x141>(v);
-  return fmax_dpp<0x140>(v);
+  return __uint_as_float(over_row<L>(__float_as_uint(v), [](uint32_t x, uint32_t y) {
+    return __float_as_uint(fmaxf(__uint_as_float(x), __uint_as_float(y)));
+  }));
 }
+template <int L>
 __device__ __forceinline__ float row_sum(float v) {
-  v += __uint_as_float(dpp<0xB1>(__float_as_uint(v)));
-  v += __uint_as_float(dpp<0x4E>(__float_as_uint(v)));
-  v += __uint_as_float(dpp<0x141>(__float_as_uint(v)));
-  return v + __uint_as_float(dpp<0x140>(__float_as_uint(v)));
+  return __uint_as_float(over_row<L>(__float_as_uint(v), [](uint32_t x, uint32_t y) {
+    return __float_as_uint(__uint_as_float(x) + __uint_as_float(y));
+  }));
 }
 
-// groups of LG lanes, all with the group's key, whose key is above this lane's
+// groups of LG lanes of 16, all with the group's key, whose key is above this lane's
 template <int LG, int R = 16 - LG>
-__device__ __forceinline__ uint32_t above(uint32_t key) {
-  if constexpr (R > 0) return (dpp<0x120 + R>(key) > key ? 1u : 0u) + above<LG, R - LG>(key);   // row_ror:R
+__device__ __forceinline__ int above(uint32_t key) {
+  if constexpr (R > 0) return (dpp<0x120 + R>(key) > key ? 1 : 0) + above<LG, R - LG>(key);   // row_ror:R
   return 0;
 }
 
@@ -239,38 +255,43 @@ __device__ __forceinline__ void load_logits(const RouteArgs& a, bool wide, int64
   }
 }
 
-// 16 lanes a row, four rows a wave; lane sl holds experts M sl .. M sl + M - 1, so that with groups
-// (E = 16 M, n_groups divides 16) a group is 16 / n_groups whole lanes.  Each lane keeps its DEPTH
-// largest keys sorted (a max and medians per key); a round takes the row's maximum of the lanes'
-// largest in four DPP steps and the owner drops it.
+// L lanes a row: 16, four rows a wave, up to 256 experts, or the whole wave; lane sl holds experts
+// M sl .. M sl + M - 1, and with groups a group is 1, 2, 4, ... whole lanes (of `lg`).  Each lane
+// keeps its DEPTH largest keys sorted (a max and medians per key); a round takes the row's maximum
+// of the lanes' largest and the owner drops it.
 //
 // Errors of the codes, in steps of 2^-24 of the range 1 + 2 B of c (B the largest finite |bias|):
 // the sigmoid's exponential is off by (1.5 |l| + 2) 2^-24 of itself, of which s (1 - s) <= 1/4 and
 // s (1 - s) |l| < 0.23 reach s; 1 + e and its reciprocal add 3 s: below 4.  The bias in code units
 // is off by 2, the fma by 1/2, the conversion by 1: a code by less than 8, and the order of two
 // that are 17 apart is certain.  A softmax score takes the sum's error besides (its terms' 1.5 d + 2
-// weighted by e^-d, and 20 additions): below 50, 113 apart.  A group's score is the sum of two
-// codes: twice that.  In kByLogit codes are the upper 24 bits of the logit's order: exact for bf16,
-// else equal codes are not certain.  What is no number, or -infinity, has a code at the bottom of
-// its kind, as have the places past E: a row that comes down to it is not certain either.
-template <int M, bool BF16, int BY>
-__global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wide, bool count) {
-  __shared__ double score[4][256];
-  __shared__ uint64_t key_of[4][256];
-  __shared__ uint32_t hist[256];
+// weighted by e^-d, and 20 additions): below 50, 113 apart.  Codes of 22 bits, under indexes of 10,
+// are off by a quarter of that and by the last two: less than 4 and 16.  A group's score is the
+// sum of two codes: twice that.  In kByLogit codes are the upper bits of the logit's order: exact
+// for bf16, else equal codes are not certain.  What is no number, or -infinity, has a code at the
+// bottom of its kind, as have the places past E: a row that comes down to it is not certain either.
+template <int L, int M, bool BF16, int BY>
+__global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, int lg, bool wide, bool count) {
+  constexpr int ROWS = 64 / L, E_MAX = L * M, IB = L == 16 ? 8 : 10;   // rows a wave, bits of an index
+  constexpr int DEPTH = L == 64 ? (M < 5 ? M : 5) : (M < 6 ? M : 6);
+  constexpr uint32_t APART = BY == kBySigmoid ? (L == 16 ? 17 : 7) : BY == kBySoftmax ? (L == 16 ? 113 : 31) : BF16 ? 0 : 1;
+  constexpr uint32_t kNegInfCode = 0x007FFFFFu >> IB;   // of total_order_bits(-infinity)
+  constexpr uint32_t kIndex = (1u << IB) - 1;
+  // a buffer of the 64-bit path for each wave, or (whole waves a row) one for each in turn
+  constexpr int BUFS = L == 16 ? 4 : 1;
+  __shared__ double score[BUFS][E_MAX];
+  __shared__ uint64_t key_of[BUFS][E_MAX];
+  __shared__ uint32_t hist[E_MAX];
+  const int E = a.n_experts, TK = a.top_k;
   if (count) {   // the only workgroup: it counts as well
-    hist[threadIdx.x] = 0;
+    for (int i = threadIdx.x; i < E_MAX; i += 256) hist[i] = 0;
     __syncthreads();
   } else if (a.expert_count != nullptr && blockIdx.x == 0) {
-    if ((int)threadIdx.x < a.n_experts) a.expert_count[threadIdx.x] = 0;
+    for (int i = threadIdx.x; i < E; i += 256) a.expert_count[i] = 0;
   }
-  constexpr int DEPTH = M < 6 ? M : 6;
-  constexpr uint32_t APART = BY == kBySigmoid ? 17 : BY == kBySoftmax ? 113 : BF16 ? 0 : 1;
-  constexpr uint32_t kNegInfCode = 0x007FFFFFu >> 8;   // of total_order_bits(-infinity)
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sl = lane & 15, slot = lane >> 4;
-  const int E = a.n_experts, TK = a.top_k, LG = 16 / a.n_groups;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sl = lane % L, slot = lane / L;
   const bool groups = a.top_groups < a.n_groups;
-  float bias[BY == kByLogit ? 1 : M], unit = 0.f;   // c's code is s * unit + bias: 1 .. 2^24 - 15
+  float bias[BY == kByLogit ? 1 : M], unit = 0.f;   // c's code is s * unit + bias: from 1 to 15 below the largest
   if constexpr (BY != kByLogit) {
     float b = 0.f;
 #pragma unroll
@@ -278,16 +299,16 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wid
       bias[i] = M * sl + i >= E ? -INFINITY : a.bias != nullptr ? a.bias[M * sl + i] : 0.f;
       if (fabsf(bias[i]) < INFINITY) b = fmaxf(b, fabsf(bias[i]));
     }
-    b = row_max(b);
-    unit = 16777200.f / (1.f + 2.f * b);
+    b = row_max<L>(b);
+    unit = (float)((1 << (32 - IB)) - 16) / (1.f + 2.f * b);
 #pragma unroll
     for (int i = 0; i < M; ++i) bias[i] = (bias[i] + b) * unit + 1.f;
   }
-  const int64_t stride = (int64_t)gridDim.x * 16, last = a.n_rows - 1;
-  int64_t r = ((int64_t)blockIdx.x * 4 + wave) * 4 + slot;
+  const int64_t stride = (int64_t)gridDim.x * (4 * ROWS), last = a.n_rows - 1;
+  const int64_t first = ((int64_t)blockIdx.x * 4 + wave) * ROWS;
+  int64_t r = first + slot;
   // every lane runs the same number of turns (rows past the end work on a copy of the last and
-  // write nothing), so the DPP exchanges see whole rows
-  const int64_t first = r - slot;
+  // write nothing), so the exchanges see whole rows
   uint64_t again = 0;
   int turn = 0, taken = -1;   // taken: the expert that a lane's rank of the last turn executes
   float cur[M];
@@ -299,7 +320,7 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wid
       top = cur[0];
 #pragma unroll
       for (int i = 1; i < M; ++i) top = fmaxf(top, cur[i]);
-      top = row_max(top);
+      top = row_max<L>(top);
       float part[4] = {};
 #pragma unroll
       for (int i = 0; i < M; ++i) {
@@ -307,7 +328,7 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wid
         part[i & 3] += e;
         if constexpr (BY == kBySoftmax) cur[i] = e;
       }
-      total = row_sum((part[0] + part[1]) + (part[2] + part[3]));
+      total = row_sum<L>((part[0] + part[1]) + (part[2] + part[3]));
     }
     const float inv = BY == kBySoftmax ? __builtin_amdgcn_rcpf(total) : 0.f;
     typedef uint32_t Keys __attribute__((ext_vector_type(DEPTH)));   // an array's selects become indexed ones
@@ -317,13 +338,13 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wid
       const int e = M * sl + i;
       uint32_t code;
       if constexpr (BY == kByLogit) {
-        code = total_order_bits(fmaxf(cur[i], -INFINITY) + 0.0f) >> 8;   // NaN as -infinity, -0 as 0
+        code = total_order_bits(fmaxf(cur[i], -INFINITY) + 0.0f) >> IB;   // NaN as -infinity, -0 as 0
       } else {
         const float s = BY == kBySigmoid ? __builtin_amdgcn_rcpf(1.f + exp_fast(-cur[i])) : cur[i] * inv;
         // v_cvt takes NaN and what is below 0 to 0, +infinity to 2^32 - 1: the largest code
         code = to_u32(fmaf(s, unit, bias[i]));
       }
-      const uint32_t x = (code << 8) | (uint32_t)(255 - e);
+      const uint32_t x = (code << IB) | (kIndex - (uint32_t)e);
 #pragma unroll
       for (int d = DEPTH - 1; d > 0; --d) m[d] = med_u32(m[d - 1], m[d], x);
       m[0] = max_u32(m[0], x);
@@ -332,21 +353,31 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wid
     if (r - slot + stride <= last) load_logits<M, BF16>(a, wide, r + stride < last ? r + stride : last, sl, cur);
     bool unsure = false;
     if (groups) {
-      uint32_t g0 = m[0] >> 8, g1 = m[1] >> 8;
+      uint32_t g0 = m[0] >> IB, g1 = m[1] >> IB;
       auto join = [&](uint32_t o0, uint32_t o1) {
         const uint32_t lo = g0 < o0 ? g0 : o0;
         g0 = max_u32(g0, o0);
         g1 = max_u32(lo, max_u32(g1, o1));
       };
-      if (LG > 1) join(dpp<0xB1>(g0), dpp<0xB1>(g1));
-      if (LG > 2) join(dpp<0x4E>(g0), dpp<0x4E>(g1));
-      if (LG > 4) join(dpp<0x141>(g0), dpp<0x141>(g1));
+      if (lg > 1) join(dpp<0xB1>(g0), dpp<0xB1>(g1));
+      if (lg > 2) join(dpp<0x4E>(g0), dpp<0x4E>(g1));
+      if (lg > 4) join(dpp<0x141>(g0), dpp<0x141>(g1));
+      if (L == 64) {
+        if (lg > 8) join(dpp<0x140>(g0), dpp<0x140>(g1));
+        if (lg > 16) join((uint32_t)__shfl_xor((int)g0, 16, 64), (uint32_t)__shfl_xor((int)g1, 16, 64));
+      }
       const uint32_t score = BY != kByLogit && a.group_best > 1 ? g0 + g1 : g0;
-      const uint32_t key = (score << 4) | (uint32_t)(15 - sl / LG);
-      const int over = (int)(LG == 1 ? above<1>(key) : LG == 2 ? above<2>(key) : LG == 4 ? above<4>(key) : above<8>(key));
+      // places past the last group come behind every group
+      const uint32_t key = L == 16 ? (score << 4) | (uint32_t)(15 - sl / lg) : (score << 6) | (uint32_t)(63 - sl / lg);
+      int over = 0;
+      if constexpr (L == 16) {
+        over = lg == 1 ? above<1>(key) : lg == 2 ? above<2>(key) : lg == 4 ? above<4>(key) : above<8>(key);
+      } else {
+        for (int g = 0; g < a.n_groups; ++g) over += (uint32_t)__builtin_amdgcn_readlane((int)key, g * lg) > key ? 1 : 0;
+      }
       const bool kept = over < a.top_groups;
       // the least kept score and the largest other
-      const uint32_t least = ~row_max_u32(kept ? ~score : 0u), most = row_max_u32(kept ? 0u : score);
+      const uint32_t least = ~row_max<L>(kept ? ~score : 0u), most = row_max<L>(kept ? 0u : score);
       unsure = least < most + 2 * APART || (BY == kByLogit && least <= kNegInfCode);
 #pragma unroll
       for (int d = 0; d < DEPTH; ++d) m[d] = kept ? m[d] : 0u;
@@ -358,10 +389,10 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wid
 #pragma unroll
     for (int j = 0; j < kMoeMaxTopK; ++j) {
       if (j < TK) {
-        const uint32_t top_key = row_max_u32(m[0]);
-        if (sl == j) my_id = 255 - (int32_t)(top_key & 0xFFu);
-        unsure |= before - (top_key >> 8) < APART;
-        before = top_key >> 8;
+        const uint32_t top_key = row_max<L>(m[0]);
+        if (sl == j) my_id = (int32_t)(kIndex - (top_key & kIndex));
+        unsure |= before - (top_key >> IB) < APART;
+        before = top_key >> IB;
         const bool own = m[0] == top_key;
         drops += own;
 #pragma unroll
@@ -369,12 +400,12 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wid
         m[DEPTH - 1] = own ? 0u : m[DEPTH - 1];
       }
     }
-    unsure |= before - (row_max_u32(m[0]) >> 8) < APART;   // the runner-up; nothing left: code 0
+    unsure |= before - (row_max<L>(m[0]) >> IB) < APART;   // the runner-up; nothing left: code 0
     unsure |= full && drops >= DEPTH;                      // the lane's next key is not known
     unsure |= BY == kByLogit ? before <= kNegInfCode : before <= APART + 1;
     // the ranks' scores: lane j of the row holds rank j
     const bool rank = sl < TK;
-    const float x = rank ? logit(a, rc, my_id) : 0.f;
+    const float x = rank ? logit(a, rc, my_id < E ? my_id : 0) : 0.f;   // a place past E: not certain, see above
     const float d = a.sigmoid ? -fabsf(x) : x - top;
     float e = expf(d);
     if (!a.sigmoid) e += e * ((x - d) - top);   // what the rounding of the difference took
@@ -384,14 +415,14 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wid
     upto += __uint_as_float(dpp<0x111>(__float_as_uint(upto)));   // row_shr:1, 2, 4: ranks are below 8
     upto += __uint_as_float(dpp<0x112>(__float_as_uint(upto)));
     upto += __uint_as_float(dpp<0x114>(__float_as_uint(upto)));
-    const float sum = row_bcast<7>(upto), want = a.tau * sum;
+    const float sum = row_bcast<7>(upto), want = a.tau * sum;   // of whole waves in the first 16 lanes
     const bool asked = sl + 1 >= a.min_k && sl + 1 < TK;
     // the sum decides little where it is tiny or not a number
-    unsure |= !(sum > 1e-30f) || (asked && fabsf(upto - want) <= 0x1p-18f * sum);
-    const uint32_t enough = (uint32_t)(__ballot(asked && upto >= want) >> (16 * slot)) & 0xFFFFu;
+    unsure |= (sl < 16 && !(sum > 1e-30f)) || (asked && fabsf(upto - want) <= 0x1p-18f * sum);
+    const uint32_t enough = (uint32_t)(__ballot(asked && upto >= want) >> (16 * (L == 16 ? slot : 0))) & 0xFFFFu;
     const int K = enough != 0 ? __builtin_ctz(enough) + 1 : TK;
-    const uint64_t odd = __ballot(unsure && r <= last);
-    if (r <= last && (odd >> (16 * slot) & 0xFFFF) == 0) {
+    const uint64_t odd = __ballot(unsure && r <= last), mine = L == 16 ? 0xFFFFull << (16 * slot) : ~0ull;
+    if (r <= last && (odd & mine) == 0) {
       taken = sl < (a.fanout != nullptr ? K : TK) ? my_id : -1;
       if (rank) {
         a.expert_idx[r * TK + sl] = my_id;
@@ -401,70 +432,91 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, bool wid
     }
     // a bit a row and turn
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if ((odd >> (16 * k) & 0xFFFF) != 0) again |= 1ull << (4 * turn + k);
+    for (int k = 0; k < ROWS; ++k)
+      if ((L == 16 ? odd >> (16 * k) & 0xFFFF : odd) != 0) again |= 1ull << (ROWS * turn + k);
     ++turn;
   }
   // rows whose order is not certain, each by the whole wave
-  for (; again != 0; again &= again - 1) {
-    const int at = __builtin_ctzll(again);
-    const int expert = route_exact(a, first + (at >> 2) * stride + (at & 3), lane, score[wave], key_of[wave]);
-    if (count && expert >= 0) atomicAdd(&hist[expert], 1u);
+  for (int w = 0; w < (BUFS == 1 ? 4 : 1); ++w) {
+    if (BUFS == 4 || wave == w)
+      for (; again != 0; again &= again - 1) {
+        const int at = __builtin_ctzll(again);
+        const int expert = route_exact(a, first + (at / ROWS) * stride + (at % ROWS), lane, score[wave % BUFS], key_of[wave % BUFS]);
+        if (count && expert >= 0) atomicAdd(&hist[expert], 1u);
+      }
+    if (BUFS == 1) __syncthreads();
   }
   if (count) {   // one turn
     if (taken >= 0) atomicAdd(&hist[taken], 1u);
     __syncthreads();
-    if ((int)threadIdx.x < E) a.expert_count[threadIdx.x] = (int32_t)hist[threadIdx.x];
+    for (int i = threadIdx.x; i < E; i += 256) a.expert_count[i] = (int32_t)hist[i];
   }
 }
 
-constexpr int64_t kRouteOneBlock = 16;   // rows of a call that one workgroup routes and counts
-constexpr int kRouteTurns = 16;          // of a wave, four rows each: a bit of a word a row
+// How a row lies on the lanes of route_row_kernel: L of them, M experts each, lg a group; L = 0
+// where it does not fit
+struct RowShape {
+  int L, M, lg;
+};
 
-template <int M, bool BF16>
-hipError_t launch_rows(const RouteArgs& a, bool wide, bool count, hipStream_t s) {
-  const int64_t blocks = (a.n_rows + 15) / 16;
-  const dim3 grid((unsigned)std::max(std::min<int64_t>(blocks, 2048), (blocks + kRouteTurns - 1) / kRouteTurns)), blk(256);
+RowShape row_shape(const RouteArgs& a) {
+  const int E = a.n_experts, G = a.top_groups < a.n_groups ? a.n_groups : 1, size = E / G;
+  for (const int L : {16, 64})
+    for (const int M : {2, 4, 8, 10, 12, 16}) {
+      if (L == 64 && (M < 8 || M == 10)) continue;   // not built
+      if (G == 1) {
+        if (M > 2 && E <= L * M) return {L, M, L};
+        continue;
+      }
+      const int lg = size / M;
+      if (size % M == 0 && (lg & (lg - 1)) == 0 && lg > 0 && G * lg <= L) return {L, M, lg};
+    }
+  return {0, 0, 0};
+}
+
+template <int L, int M, bool BF16>
+hipError_t launch_rows(const RouteArgs& a, int lg, bool count, hipStream_t s) {
+  constexpr int ROWS = 4 * (64 / L);   // of a workgroup; a wave takes 64 rows at most, a bit of a word each
+  const int64_t blocks = (a.n_rows + ROWS - 1) / ROWS;
+  const dim3 grid((unsigned)std::max(std::min<int64_t>(blocks, 2048), (blocks + L - 1) / L)), blk(256);
+  // vectors of 4 (2 where a lane's share is not whole fours) logits
+  const int64_t bytes = (M % 4 == 0 ? 4 : 2) * (BF16 ? 2 : 4);
+  const bool wide = reinterpret_cast<uintptr_t>(a.logits) % bytes == 0 && a.stride * (BF16 ? 2 : 4) % bytes == 0;
   if (a.bias == nullptr && (a.top_groups == a.n_groups || a.group_best == 1))
-    route_row_kernel<M, BF16, kByLogit><<<grid, blk, 0, s>>>(a, wide, count);
-  else if (a.sigmoid) route_row_kernel<M, BF16, kBySigmoid><<<grid, blk, 0, s>>>(a, wide, count);
-  else route_row_kernel<M, BF16, kBySoftmax><<<grid, blk, 0, s>>>(a, wide, count);
+    route_row_kernel<L, M, BF16, kByLogit><<<grid, blk, 0, s>>>(a, lg, wide, count);
+  else if (a.sigmoid) route_row_kernel<L, M, BF16, kBySigmoid><<<grid, blk, 0, s>>>(a, lg, wide, count);
+  else route_row_kernel<L, M, BF16, kBySoftmax><<<grid, blk, 0, s>>>(a, lg, wide, count);
   return hipGetLastError();
 }
 
 template <bool BF16>
-hipError_t launch_by_width(const RouteArgs& a, int m, bool count, hipStream_t s) {
-  // vectors of 4 (2 where a lane's share is not whole fours) logits
-  const int64_t bytes = (m % 4 == 0 ? 4 : 2) * (BF16 ? 2 : 4);
-  const bool wide = reinterpret_cast<uintptr_t>(a.logits) % bytes == 0 && a.stride * (BF16 ? 2 : 4) % bytes == 0;
-  switch (m) {
-    case 4: return launch_rows<4, BF16>(a, wide, count, s);
-    case 8: return launch_rows<8, BF16>(a, wide, count, s);
-    case 10: return launch_rows<10, BF16>(a, wide, count, s);
-    case 12: return launch_rows<12, BF16>(a, wide, count, s);
-    default: return launch_rows<16, BF16>(a, wide, count, s);
+hipError_t launch_shape(const RouteArgs& a, const RowShape& S, bool count, hipStream_t s) {
+  if (S.L == 64) {
+    if (S.M == 8) return launch_rows<64, 8, BF16>(a, S.lg, count, s);
+    if (S.M == 12) return launch_rows<64, 12, BF16>(a, S.lg, count, s);
+    return launch_rows<64, 16, BF16>(a, S.lg, count, s);
   }
-}
-
-// experts a lane of route_row_kernel, or 0 where the row does not fit it
-int row_share(const RouteArgs& a) {
-  for (int m : {4, 8, 10, 12, 16}) {
-    if (a.n_experts > 16 * m) continue;
-    if (a.top_groups == a.n_groups || (a.n_experts == 16 * m && 16 % a.n_groups == 0)) return m;
-    return 0;
+  switch (S.M) {
+    case 2: return launch_rows<16, 2, BF16>(a, S.lg, count, s);
+    case 4: return launch_rows<16, 4, BF16>(a, S.lg, count, s);
+    case 8: return launch_rows<16, 8, BF16>(a, S.lg, count, s);
+    case 10: return launch_rows<16, 10, BF16>(a, S.lg, count, s);
+    case 12: return launch_rows<16, 12, BF16>(a, S.lg, count, s);
+    default: return launch_rows<16, 16, BF16>(a, S.lg, count, s);
   }
-  return 0;
 }
 
 }  // namespace
 
 hipError_t launch_moe_route(const RouteArgs& a, hipStream_t s) {
   if (a.n_rows == 0 && a.expert_count == nullptr) return hipSuccess;
-  const int E = a.n_experts, share = a.n_rows > 0 ? row_share(a) : 0;
+  const int E = a.n_experts;
+  const RowShape S = a.n_rows > 0 ? row_shape(a) : RowShape{0, 0, 0};
   hipError_t e;
-  if (share != 0) {
-    const bool count = a.expert_count != nullptr && a.n_rows <= kRouteOneBlock;
-    e = a.logits_bf16 ? launch_by_width<true>(a, share, count, s) : launch_by_width<false>(a, share, count, s);
+  if (S.L != 0) {
+    // as many rows as one workgroup takes at once: it counts them too
+    const bool count = a.expert_count != nullptr && a.n_rows <= 4 * (64 / S.L);
+    e = a.logits_bf16 ? launch_shape<true>(a, S, count, s) : launch_shape<false>(a, S, count, s);
     if (count) return e;
   } else {
     const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>((a.n_rows + 3) / 4, 4096))), blk(256);   // no row: the counts are cleared
