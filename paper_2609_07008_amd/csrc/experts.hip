@@ -279,6 +279,182 @@ __device__ __forceinline__ void down_tile(const ExpertsArgs& a, const Place& at,
   }
 }
 
+// Few pairs (a new token, or some): what counts is the weights' way and the number of launches, so
+// gate and up find their tiles themselves and quantize the rows that they take, and so does down.
+// A workgroup takes up to P rows of one expert and 128 rows of its weight; the rows' codes lie in
+// LDS over all of K (64 KB; P falls as K grows), and each of 8 waves streams 16 rows of the weight
+// through its own stages: it waits for its own loads alone, no barrier in the loop.
+// One token through 8 of 256 experts 4096 x 2048: 55 -> 48 us for the whole call.
+constexpr int kFewPanel = 65536, kFewStages = 5;
+
+// The t-th block of up to `most` pairs of one expert, by all lanes of a wave: lane l holds pair l.
+// The pairs of the block in row_pair, and how many (0: no such block); `expert` is its expert.
+__device__ __forceinline__ int few_block(const ExpertsArgs& a, int n_pairs, int t, int most, int lane, int& expert, int* row_pair) {
+  const int e = lane < n_pairs ? pair_expert(a, lane) : -1;
+  int nth = 0;   // pairs of the same expert before the lane's
+  for (int m = 0; m < n_pairs; ++m) nth += __builtin_amdgcn_readlane(e, m) == e && m < lane;
+  const bool first = e >= 0 && nth % most == 0;
+  const uint64_t firsts = __ballot(first);
+  const uint64_t at = __ballot(first && __popcll(firsts & ((1ull << lane) - 1)) == t);
+  if (at == 0) return 0;
+  const int l = __builtin_ctzll(at), from = __builtin_amdgcn_readlane(nth, l);
+  expert = __builtin_amdgcn_readlane(e, l);
+  const bool mine = e == expert && nth >= from && nth < from + most;
+  if (mine) row_pair[nth - from] = lane;
+  return __popcll(__ballot(mine));
+}
+
+// One of the two products: 16 rows of a weight a wave (w_row(q): row of q = 0 .. 15), rows of bf16
+// (x_row(r)) quantized.  Codes of k of row r: slice k / 128 of the panel, chunk k / 16 % 8 at slot
+// chunk ^ i8_swz(r); NV: vectors of 8 of a lane in a row.
+template <int NV, class WRow, class XRow>
+__device__ __forceinline__ i32x4 few_product(unsigned char* lds, float* scale, int rows, int k_len, int wave, int lane, WRow&& w_row, XRow&& x_row) {
+  constexpr int P = 128 / NV;   // NV = 8, 16, 32: up to 4096, 8192, 16384 of K
+  const int nk = (k_len + I8_ROWB - 1) / I8_ROWB, cut = k_len % I8_ROWB ? nk - 1 : nk;
+  unsigned char* stage = lds + kFewPanel + wave * (kFewStages * 2048);
+  const unsigned char* src[2];
+  uint32_t voff[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    src[j] = (const unsigned char*)w_row(8 * j);
+    voff[j] = (uint32_t)((const unsigned char*)w_row(8 * j + (lane >> 3)) - src[j]) + (((lane & 7) ^ i8_swz(8 * j + (lane >> 3))) * 16);
+  }
+  auto load = [&](int kt, int st) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      uint32_t v = voff[j];
+      if (kt == cut) v -= (((lane >> 2) ^ j) & 1) * 64;   // of a last half slice the lower chunks again
+      dma16(src[j] + (int64_t)kt * I8_ROWB, v, (const unsigned char MLA_LDS*)(stage + st * 2048 + j * 1024));
+    }
+  };
+  u32x4 x[NV];
+  auto read = [&](int r) {
+    const uint16_t* p = x_row(r);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * 64 + lane) * 8;
+      x[i] = c < k_len ? *(const u32x4*)(p + c) : u32x4{0, 0, 0, 0};
+    }
+  };
+  auto code = [&](int r) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) m = umax(m, umax(x[i][k] & 0x7fffu, (x[i][k] >> 16) & 0x7fffu));
+    m = wave_max(m);
+    const bool finite = m < 0x7f80u;
+    const I8Coder coder(finite ? m : 0);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (i * 64 + lane) * 8;
+      if (c < k_len)
+        *(u32x2 MLA_LDS*)((unsigned char MLA_LDS*)lds + c / 128 * (P * 128) + r * 128 + ((c / 16 % 8) ^ i8_swz(r)) * 16 + c % 16) =
+            finite ? codes8(coder, x[i]) : u32x2{0, 0};
+    }
+    if (lane == 0) scale[r] = finite ? __uint_as_float(m << 16) / 127.0f : __uint_as_float(0x7fc00000u);
+  };
+  if (wave < rows) read(wave);
+#pragma unroll
+  for (int s = 0; s < kFewStages; ++s)
+    if (s < nk) load(s, s);
+  if (wave < rows) code(wave);
+  if (wave + 8 < rows) {
+    read(wave + 8);
+    code(wave + 8);
+  }
+  __syncthreads();
+  const int lg = lane >> 4, lc = lane & 15;
+  const unsigned char MLA_LDS* A = (const unsigned char MLA_LDS*)lds + (lc % P) * 128;
+  const unsigned char MLA_LDS* B = (const unsigned char MLA_LDS*)stage + lc * 128;
+  const int ca = (lg ^ i8_swz(lc % P)) * 16, cb = (lg ^ i8_swz(lc)) * 16;
+  i32x4 acc = {0, 0, 0, 0};
+  int st = 0;
+  for (int kt = 0; kt < nk; ++kt) {
+    // this wave's slice kt has landed; near the end fewer are under way
+    if (kt + kFewStages <= nk) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * (kFewStages - 1)) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const i32x4 b0 = *(const i32x4 MLA_LDS*)(B + st * 2048 + cb), b1 = *(const i32x4 MLA_LDS*)(B + st * 2048 + (cb ^ 64));
+    const i32x4 a0 = *(const i32x4 MLA_LDS*)(A + kt * (P * 128) + ca), a1 = *(const i32x4 MLA_LDS*)(A + kt * (P * 128) + (ca ^ 64));
+    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(b0, a0, acc, 0, 0, 0);
+    if (kt != cut) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(b1, a1, acc, 0, 0, 0);
+    if (kt + kFewStages < nk) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the stage is read
+      load(kt + kFewStages, st);
+    }
+    st = st == kFewStages - 1 ? 0 : st + 1;
+  }
+  return acc;
+}
+
+constexpr int kFewLds = kFewPanel + I8_WAVES * kFewStages * 2048;
+
+// h of up to P rows x 64 channels: of a wave's 16 weight rows 8 are gate's, 8 up's
+template <int NV>
+__global__ __launch_bounds__(I8_WAVES * 64, 2) void experts_few_gate_up_kernel(ExpertsArgs a, int n_pairs, int cols) {
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[kFewLds];
+  __shared__ int row_pair[16];
+  __shared__ float scale[16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t = blockIdx.x / cols, f = a.d_ffn, d = a.d_model;
+  int expert = 0;
+  // every wave finds the block, and all write the same rows
+  const int rows = few_block(a, n_pairs, t, 128 / NV, lane, expert, row_pair);
+  if (rows == 0) return;
+  __syncthreads();
+  const int f0 = (int)(blockIdx.x % cols) * 64 + 8 * wave;
+  const int8_t* w = a.w_gu + (int64_t)expert * 2 * f * d;
+  const i32x4 acc = few_product<NV>(
+      lds, scale, rows, d, wave, lane, [&](int q) { return w + (int64_t)((q >> 3) * f + f0 + (q & 7)) * d; },
+      [&](int r) { return a.x + (int64_t)(__builtin_amdgcn_readfirstlane(row_pair[r]) / a.top_k) * a.x_stride; });
+  const int lg = lane >> 4, lc = lane & 15, c = f0 + (lg & 1) * 4;   // lg 0, 1: gate; 2, 3: up
+  const f32x4 s = *(const f32x4*)(a.s_gu + (int64_t)expert * 2 * f + (lg >> 1) * f + c);
+  const float xs = scale[lc < rows ? lc : 0];
+  float v[4], h[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    v[e] = (float)acc[e] * s[e] * xs;
+    const float up = __shfl_xor(v[e], 32, 64);
+    h[e] = silu(v[e]) * up;
+  }
+  if (lg < 2 && lc < rows) *(u32x2*)(a.h + (int64_t)row_pair[lc] * f + c) = u32x2{pack_bf16x2(h[0], h[1]), pack_bf16x2(h[2], h[3])};
+}
+
+template <bool F16, int NV>
+__global__ __launch_bounds__(I8_WAVES * 64, 2) void experts_few_down_kernel(ExpertsArgs a, int n_pairs, int cols) {
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[kFewLds];
+  __shared__ int row_pair[16];
+  __shared__ float scale[16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t = blockIdx.x / cols, col = (int)(blockIdx.x % cols), f = a.d_ffn, d = a.d_model;
+  int expert = 0;
+  const int rows = few_block(a, n_pairs, t, 128 / NV, lane, expert, row_pair);
+  if (rows == 0) return;
+  __syncthreads();
+  const int n0 = col * 128 + 16 * wave;
+  const int8_t* w = a.w_down + (int64_t)expert * d * f;
+  // channels past the end are clamped to the last one (their results are not stored)
+  const i32x4 acc = few_product<NV>(
+      lds, scale, rows, f, wave, lane, [&](int q) { return w + (int64_t)std::min(n0 + q, d - 1) * f; },
+      [&](int r) { return a.h + (int64_t)__builtin_amdgcn_readfirstlane(row_pair[r]) * f; });
+  const int lg = lane >> 4, lc = lane & 15, c = n0 + lg * 4;
+  if (col == 0 && (int)threadIdx.x < rows) a.hs[row_pair[threadIdx.x]] = scale[threadIdx.x];
+  if (lc >= rows || c >= d) return;
+  const int64_t at = (int64_t)row_pair[lc] * d + c;
+  if (F16) {
+    f16x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (_Float16)((float)acc[e] * kPartUnit);
+    *(f16x4*)((_Float16*)a.part + at) = v;
+  } else {
+    const f32x4 s = *(const f32x4*)(a.s_down + (int64_t)expert * d + c);
+    f32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (float)acc[e] * s[e] * scale[lc];
+    *(f32x4*)((float*)a.part + at) = v;
+  }
+}
+
 // y of a token: its pairs' parts in rank order, 512 channels a wave.  Lane j reads the token's
 // pair j; what is chosen by it is then uniform.
 template <bool OUT_BF16>
@@ -403,7 +579,32 @@ hipError_t launch_start(const ExpertsArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_chunk(const ExpertsArgs& a, hipStream_t s) {
+template <int NV>
+void launch_few_gate_up(const ExpertsArgs& a, int n_pairs, hipStream_t s) {
+  const int cols = a.d_ffn / 64;
+  experts_few_gate_up_kernel<NV><<<dim3((unsigned)(n_pairs * cols)), dim3(I8_WAVES * 64), 0, s>>>(a, n_pairs, cols);
+}
+
+template <int NV>
+void launch_few_down(const ExpertsArgs& a, int n_pairs, hipStream_t s) {
+  const int cols = (a.d_model + 127) / 128;
+  const dim3 grid((unsigned)(n_pairs * cols)), blk(I8_WAVES * 64);
+  if (a.y_bf16) experts_few_down_kernel<true, NV><<<grid, blk, 0, s>>>(a, n_pairs, cols);
+  else experts_few_down_kernel<false, NV><<<grid, blk, 0, s>>>(a, n_pairs, cols);
+}
+
+hipError_t launch_few(const ExpertsArgs& a, hipStream_t s) {
+  const int n_pairs = (int)a.n_rows * a.top_k;
+  if (a.d_model <= 4096) launch_few_gate_up<8>(a, n_pairs, s);
+  else if (a.d_model <= 8192) launch_few_gate_up<16>(a, n_pairs, s);
+  else launch_few_gate_up<32>(a, n_pairs, s);
+  if (a.d_ffn <= 4096) launch_few_down<8>(a, n_pairs, s);
+  else if (a.d_ffn <= 8192) launch_few_down<16>(a, n_pairs, s);
+  else launch_few_down<32>(a, n_pairs, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_many(const ExpertsArgs& a, hipStream_t s) {
   hipError_t e = launch_start(a, s);
   if (e != hipSuccess) return e;
   switch (a.tile_rows) {
@@ -419,6 +620,11 @@ hipError_t launch_chunk(const ExpertsArgs& a, hipStream_t s) {
     case 128: e = launch_down<4, 256>(a, s); break;
     default: e = launch_down<8, 256>(a, s); break;
   }
+  return e;
+}
+
+hipError_t launch_chunk(const ExpertsArgs& a, hipStream_t s) {
+  const hipError_t e = a.few ? launch_few(a, s) : launch_many(a, s);
   if (e != hipSuccess) return e;
   const unsigned join = (unsigned)std::min<int64_t>((a.n_rows * ((a.d_model + 511) / 512) + 3) / 4, 1 << 16);
   if (a.y_bf16) experts_join_kernel<true><<<dim3(join), dim3(256), 0, s>>>(a);

@@ -41,6 +41,7 @@ struct WbI8Args {
 hipError_t launch_wb_i8(const WbI8Args& a, hipStream_t s);
 
 constexpr int kExpertsChunk = 65536;    // rows taken at a time: what the workspace holds
+constexpr int kExpertsFewPairs = 16;     // pairs of a call whose products find their rows themselves
 constexpr int kDispatchBlocks = 128;    // workgroups that count and place pairs, at most
 
 // One block of rows of an expert.  Its pairs lie at places [row0, row0 + count) of the expert
@@ -78,6 +79,7 @@ struct ExpertsArgs {
   float* hs;                 // [rows top_k] by pair
   void* part;                // [rows top_k, d_model] by pair: W_down h in f32, or (y in bf16) its sums in f16
   int32_t tile_rows;
+  int32_t few;               // the whole call has at most kExpertsFewPairs pairs: h and part lie apart
 };
 
 // rows of a tile (64, 128 or 256), by the pairs that an expert has on average

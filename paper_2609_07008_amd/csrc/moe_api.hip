@@ -32,6 +32,7 @@ mla_status check_i8(int64_t n_rows, int32_t n_cols, const void* x, int64_t x_str
 // Where the tables and intermediates of mla_moe_experts_i8 lie in its workspace
 struct ExpertsSplit {
   int32_t tile_rows;
+  bool few;
   int64_t off_hist, off_head, off_tiles, off_pairs, off_xq, off_xs, off_h, off_hq, off_hs, off_part;
   size_t total;
 };
@@ -68,8 +69,14 @@ mla_status experts_split(const mla_moe_layer* L, int64_t n_rows, int32_t out_dty
   S->off_xs = take(rows * 4);
   S->off_hq = take(pairs * f);
   S->off_hs = take(pairs * 4);
-  // h is read for the last time before the first of the parts is written
-  S->off_h = S->off_part = take(std::max(pairs * f * 2, pairs * d * (out_dtype == MLA_BF16 ? 2 : 4)));
+  const int64_t h = pairs * f * 2, part = pairs * d * (out_dtype == MLA_BF16 ? 2 : 4);
+  S->few = n_rows * L->top_k <= mla::kExpertsFewPairs;
+  if (S->few) {
+    S->off_h = take(h);
+    S->off_part = take(part);
+  } else {   // h is read for the last time before the first of the parts is written
+    S->off_h = S->off_part = take(std::max(h, part));
+  }
   S->total = (size_t)std::max<int64_t>(at, 256);
   return MLA_OK;
 }
@@ -237,6 +244,7 @@ mla_status mla_moe_experts_i8(const mla_moe_layer* layer, int64_t n_rows, const 
   a.hs = reinterpret_cast<float*>(W + S.off_hs);
   a.part = W + S.off_part;
   a.tile_rows = S.tile_rows;
+  a.few = S.few;
   const hipError_t e = mla::launch_experts(a, reinterpret_cast<hipStream_t>(stream));
   return e == hipSuccess ? MLA_OK : hip_fail(e, "experts' kernels");
 }

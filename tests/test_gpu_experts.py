@@ -70,6 +70,33 @@ def test_widest():
     Layer(64, 16384, 2, 2).check(x, idx, w)
 
 
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("n,d,f,k", [(1, 64, 64, 16), (2, 4160, 128, 8), (4, 192, 4160, 4), (1, 8256, 64, 3), (16, 64, 8256, 1), (3, 16384, 64, 5), (5, 128, 1088, 3),
+                                     (1, 4096, 64, 1), (8, 8192, 64, 2)])
+def test_few_pairs(n, d, f, k, out):
+    """Up to 16 pairs, where the products find and quantize their rows themselves: all widths of their panels, all pairs at one
+    expert (more than a block of rows), at different ones, some elsewhere; the bits of a call with one row more that is padding."""
+    import torch
+    x, idx, w, fanout = _tokens(n, d, 16, k, d + f)
+    layer = Layer(d, f, 3, n + k, first=2)
+    idx = idx % 6
+    for i, fan in ((idx, None), (torch.full_like(idx, 3), None), (idx, fanout)):
+        layer.check(x, i, w, fan, out)
+        pad = 20 // k
+        more = lambda t, v: None if t is None else torch.cat((t, torch.full((pad, *t.shape[1:]), v, dtype=t.dtype, device="cuda")))
+        assert torch.equal(layer.run(more(x, 1), more(i, -1), more(w, 0), more(fan, 1), out)[:n], layer.run(x, i, w, fan, out))
+
+
+def test_few_pairs_odd_rows():
+    import torch
+    x, idx, w, _ = _tokens(4, 256, 6, 3, 30)
+    x[0, 9], x[1] = float("nan"), 0.0
+    layer = Layer(256, 128, 6, 31)
+    y = layer.run(x, idx, w)
+    assert bool(y[0].isnan().all()) and bool((y[1] == 0).all()) and bool(y[2:].isfinite().all())
+    assert bool((layer.run(x, torch.full_like(idx, -1), w) == 0).all())
+
+
 def test_share_and_padding():
     """Experts [5, 8) of 16; indexes outside the layer; every value of fanout."""
     import torch
