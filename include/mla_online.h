@@ -664,7 +664,7 @@ mla_status mla_cache_attend(const mla_geom* geom, int32_t n_seqs, int32_t n_q, c
  * scores (its order stays that of the logits), a row of -infinity alone has scores 0.
  * An expert with bias -infinity is chosen only where nothing else is left.
  *
- *   n_rows, n_experts   N token rows, E experts (top_k <= E <= 1024)
+ *   n_rows, n_experts   N token rows (below 2^31), E experts (top_k <= E <= 1024)
  *   logits        device [N, E] f32 or bf16 (logits_dtype), rows logits_stride elements
  *                 apart (at least E), aligned to their type
  *   bias          device f32 [E] or NULL
@@ -720,8 +720,8 @@ mla_status mla_i8_dequantize(int64_t n_rows, int32_t n_cols, const void* codes, 
 
 /* y = W_b z as mla_shared_wb, both sides in 8 bits: a row of z has a scale, and so has an
  * output channel.  The sum of a product of codes is exact in i32 (d_in at most 16384);
- * y = (sum * w_scale) * z_scale in f32, rounded once more to a bf16 y.  Any number of rows;
- * a row of z gives the same bits in any call.
+ * y = (sum * w_scale) * z_scale in f32, rounded once more to a bf16 y.  Up to 2^27 rows; a
+ * row of z gives the same bits in any call.
  *   n_rows, d_in, d_out  as for mla_shared_wb (d_out up to MLA_WB_I8_MAX_D_OUT)
  *   z_codes, z_scales    device int8 [N, d_in] (16-byte aligned), f32 [N]
  *   w_codes, w_scales    device int8 [d_out, d_in] (16-byte aligned), f32 [d_out]

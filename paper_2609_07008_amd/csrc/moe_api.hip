@@ -107,6 +107,7 @@ mla_status mla_moe_route(int64_t n_rows, int32_t n_experts, const void* logits, 
   if (cfg->group_best != 1 && cfg->group_best != 2) return fail(MLA_ERR_SHAPE, "group_best = %d, expected 1 or 2", cfg->group_best);
   if (!std::isfinite(cfg->scale)) return fail(MLA_ERR_SHAPE, "scale is not finite");
   if (std::isnan(cfg->tau)) return fail(MLA_ERR_SHAPE, "tau is NaN");
+  if (n_rows > INT32_MAX) return fail(MLA_ERR_UNSUPPORTED, "n_rows = %lld; built: up to 2^31-1", (long long)n_rows);
   if (logits_stride < n_experts) return fail(MLA_ERR_SHAPE, "logits_stride = %lld < n_experts = %d", (long long)logits_stride, n_experts);
   if (n_rows > INT64_MAX / 8 / logits_stride) return fail(MLA_ERR_SHAPE, "n_rows * logits_stride overflows");
   if (n_rows > 0 && (logits == nullptr || expert_idx == nullptr || expert_w == nullptr))
@@ -168,7 +169,7 @@ mla_status mla_shared_wb_i8(int64_t n_rows, int32_t d_in, int32_t d_out, const v
   if (d_out < 1) return fail(MLA_ERR_SHAPE, "d_out = %d", d_out);
   if (d_out > MLA_WB_I8_MAX_D_OUT) return fail(MLA_ERR_UNSUPPORTED, "d_out = %d; built: up to %d", d_out, MLA_WB_I8_MAX_D_OUT);
   if (out_dtype != MLA_BF16 && out_dtype != MLA_F32) return fail(MLA_ERR_SHAPE, "out_dtype %d", out_dtype);
-  if (n_rows / 256 + 1 > (int64_t)(1 << 22) / (d_out / 256 + 1))
+  if (n_rows > (1 << 27) || n_rows / 256 + 1 > (int64_t)(1 << 22) / (d_out / 256 + 1))
     return fail(MLA_ERR_UNSUPPORTED, "n_rows = %lld, d_out = %d: too many tiles", (long long)n_rows, d_out);
   if (n_rows == 0) return MLA_OK;
   if (z_codes == nullptr || z_scales == nullptr || w_codes == nullptr || w_scales == nullptr || y == nullptr)

@@ -203,7 +203,7 @@ class MoeStep:
                  first_expert: int = 0, min_k=None, tau: float = 2.0, y_dtype=torch.bfloat16, with_count: bool = False, **route):
         """route: scoring, n_groups, top_groups, group_best, renormalize, scale of mla.moe_route."""
         self.n_local = int(n_experts if n_local is None else n_local)
-        self.first_expert, self.n_experts, self.d_model = int(first_expert), int(n_experts), int(d_model)
+        self.first_expert, self.n_experts, self.d_model, self.d_ffn = int(first_expert), int(n_experts), int(d_model), int(d_ffn)
         if self.n_local < 1 or self.first_expert < 0 or self.first_expert + self.n_local > self.n_experts:
             raise mla.MlaError(2, f"experts [{first_expert}, {first_expert} + {self.n_local}) of {n_experts}")
         if d_model % 64 or d_model > mla.WB_MAX_D_IN:
@@ -229,6 +229,9 @@ class MoeStep:
         mla.moe_route(self.logits, self.expert_idx, self.expert_w, self.fanout, self.count, bias=bias, stream=stream, **self.route_args)
 
     def experts(self, x, w_gate_up, s_gate_up, w_down, s_down, stream=None):
+        mla.check_tensor("w_down", w_down, torch.int8)
+        if w_down.shape != (self.n_local, self.d_model, self.d_ffn):
+            raise mla.MlaError(2, f"w_down is {tuple(w_down.shape)}; made for [{self.n_local}, {self.d_model}, {self.d_ffn}]")
         mla.moe_experts_i8(x, self.expert_idx, self.expert_w, w_gate_up, s_gate_up, w_down, s_down, self.y, self.ws, fanout=self.fanout,
                            first_expert=self.first_expert, stream=stream)
 

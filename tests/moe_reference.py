@@ -79,7 +79,8 @@ def experts(x, idx, w, fanout, w_gu, s_gu, w_down, s_down, first=0):
 
     A product's sum is exact and then takes three roundings (to f32, two scales): relative 3 * 2^-24.  Of h = silu(g) u: g's
     error counts (1 + |g|) times in silu, the exponential's is at most (1.5 |g| + 2) steps of 2^-24, and the other operations
-    (the second factor's 3 roundings, 1 + e, the quotient, the product) 6 more: (5 |g| + 12) * 2^-24 in all.  Where a bf16 border
+    (the second factor's 3 roundings, 1 + e, the reciprocal's 2, two products) 8 more: (4.5 |g| + 13) * 2^-24 in all, taken as
+    (5 |g| + 13).  Where a bf16 border
     is nearer than that, h may be the neighbour, a step of at most 2^-7 of it, and its code another one; where that is the row's
     largest value every code may be another one, and the scale is 2^-7 off.  The sum over the pairs takes a product and an addition
     each, and parts three roundings."""
@@ -97,7 +98,7 @@ def experts(x, idx, w, fanout, w_gu, s_gu, w_down, s_down, first=0):
             with np.errstate(over="ignore"):
                 v = g / (1.0 + np.exp(-g)) * u
             h = bf16(v)
-            err = np.abs(v) * (5 * np.abs(g) + 12) * 2.0 ** -24
+            err = np.abs(v) * (5 * np.abs(g) + 13) * 2.0 ** -24
             odd = (bf16(v - err) != h) | (bf16(v + err) != h)
             hq, hs = quantize(h[None])
             dh = np.where(odd, np.abs(h) * 2.0 ** -7 + hs, 0.0)

@@ -217,3 +217,24 @@ def test_rows_past_a_chunk():
     some = torch.tensor([0, 65535, 65536, n - 1], device="cuda")
     want, off, _ = layer.want(x[some], idx[some], w[some], fanout[some])
     assert (np.abs(layer.run(x, idx, w, fanout)[some].cpu().numpy() - want) <= off).all()
+
+
+def test_tiles_of_every_filling():
+    """Experts whose pairs fill a tile by one row, by a part of it, whole, and by a row more, in each tile height (64, 128, 256 rows
+    by the pairs of an expert on average): rows as by themselves, and some against the definition."""
+    import torch
+    gen = torch.Generator().manual_seed(6)
+    for sizes in ((1, 31, 32, 33, 63, 64, 65, 0, 130), (1, 64, 65, 127, 128, 129, 200, 0, 300, 600), (1, 33, 64, 65, 128, 129, 224, 255, 256, 257, 0, 511, 900, 1900)):
+        n, e = sum(sizes), len(sizes)
+        layer = Layer(320, 192, e, n)
+        x = torch.randn((n, 320), generator=gen).to(torch.bfloat16).cuda()
+        idx = torch.repeat_interleave(torch.arange(e), torch.tensor(sizes))[torch.randperm(n, generator=gen)].to(torch.int32).reshape(n, 1).cuda()
+        w = torch.rand((n, 1), generator=gen).cuda()
+        for out in ("f32", "bf16"):
+            y = layer.run(x, idx, w, out=out)
+            for lo in range(0, n, 150):   # other rows beside them, other tiles
+                part = slice(lo, lo + 150)
+                assert torch.equal(layer.run(x[part].contiguous(), idx[part].contiguous(), w[part].contiguous(), out=out), y[part])
+        some = torch.randperm(n, generator=gen)[:40].cuda()
+        want, off, _ = layer.want(x[some], idx[some], w[some])
+        assert (np.abs(layer.run(x, idx, w)[some].cpu().numpy() - want) <= off).all()

@@ -28,7 +28,7 @@ ROUTE = dict(n=2, e=256, logits=A, dtype=1, stride=256, bias=A, scoring=1, group
     (dict(scoring=2), SHAPE), (dict(scoring=-1), SHAPE), (dict(groups=0), SHAPE), (dict(groups=7), SHAPE), (dict(groups=-8), SHAPE),
     (dict(groups=128), UNSUPPORTED), (dict(kept=0), SHAPE), (dict(kept=9), SHAPE), (dict(groups=64, kept=1), SHAPE), (dict(best=0), SHAPE), (dict(best=3), SHAPE),
     (dict(k=0), UNSUPPORTED), (dict(k=9), UNSUPPORTED), (dict(min_k=0), SHAPE), (dict(min_k=9), SHAPE), (dict(scale=NAN), SHAPE), (dict(scale=INF), SHAPE),
-    (dict(tau=NAN), SHAPE), (dict(stride=255), SHAPE), (dict(n=2 ** 60), SHAPE), (dict(logits=None), NULL), (dict(idx=None), NULL), (dict(w=None), NULL),
+    (dict(tau=NAN), SHAPE), (dict(stride=255), SHAPE), (dict(n=2 ** 31), UNSUPPORTED), (dict(n=2 ** 60), UNSUPPORTED), (dict(stride=2 ** 62), SHAPE), (dict(logits=None), NULL), (dict(idx=None), NULL), (dict(w=None), NULL),
     (dict(logits=A + 2), SHAPE), (dict(dtype=0, logits=A + 1), SHAPE), (dict(bias=A + 2), SHAPE), (dict(idx=A + 2), SHAPE), (dict(w=A + 1), SHAPE),
     (dict(fan=A + 2), SHAPE), (dict(count=A + 2), SHAPE), (dict(cfg=None), NULL),
     (dict(n=0, logits=None, bias=None, idx=None, w=None, fan=None, count=None), OK)])
@@ -59,7 +59,7 @@ WB = dict(n=2, d_in=128, d_out=8, z=A, zs=A, w=A, ws=A, out=1, y=A)
 
 @pytest.mark.parametrize("over,status", [
     (dict(n=-1), SHAPE), (dict(d_in=0), SHAPE), (dict(d_in=96), SHAPE), (dict(d_in=16448), UNSUPPORTED), (dict(d_out=0), SHAPE),
-    (dict(d_out=2 ** 24 + 1), UNSUPPORTED), (dict(n=2 ** 40), UNSUPPORTED), (dict(n=2 ** 20, d_out=2 ** 20), UNSUPPORTED), (dict(out=2), SHAPE),
+    (dict(d_out=2 ** 24 + 1), UNSUPPORTED), (dict(n=2 ** 40), UNSUPPORTED), (dict(n=2 ** 27 + 1), UNSUPPORTED), (dict(n=2 ** 20, d_out=2 ** 20), UNSUPPORTED), (dict(out=2), SHAPE),
     (dict(z=None), NULL), (dict(zs=None), NULL), (dict(w=None), NULL), (dict(ws=None), NULL), (dict(y=None), NULL), (dict(z=A + 8), SHAPE),
     (dict(w=A + 4), SHAPE), (dict(y=A + 8), SHAPE), (dict(zs=A + 2), SHAPE), (dict(ws=A + 1), SHAPE),
     (dict(n=0, z=None, zs=None, w=None, ws=None, y=None), OK)])
