@@ -379,6 +379,13 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, int lg, 
       // the least kept score and the largest other
       const uint32_t least = ~row_max<L>(kept ? ~score : 0u), most = row_max<L>(kept ? 0u : score);
       unsure = least < most + 2 * APART || (BY == kByLogit && least <= kNegInfCode);
+      if constexpr (BY == kByLogit) {
+        // Groups go by scores, and those of different logits may be equal in 64 bits: a sigmoid next to
+        // 1 or to 1/2, an exponential of next to `top` or out of range.  Codes apart are logits 2^-16
+        // of themselves apart, which elsewhere is far above a step of the score.
+        const float x = from_total_order_bits(least << IB);
+        unsure |= !(fabsf(x) >= 0x1p-20f * fmaxf(1.f, fabsf(top)) && top - x < 600.f && !(a.sigmoid && x > 24.f));
+      }
 #pragma unroll
       for (int d = 0; d < DEPTH; ++d) m[d] = kept ? m[d] : 0u;
     }

@@ -148,3 +148,17 @@ def test_many_rows():
     x, rng = _logits(30011, 256, 77)
     check(np.float32(x), 6, 0.1 * rng.standard_normal(256), scoring="sigmoid", n_groups=8, top_groups=4, group_best=2, min_k=3, tau=0.9)
     check(np.float32(x), 8, None, bf16=True, scoring="softmax", min_k=3, tau=0.9)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("e,g,kept", [(64, 8, 2), (256, 8, 3), (256, 32, 6), (1024, 16, 3)])
+def test_groups_of_scores_that_meet(e, g, kept, bf16):
+    """Groups whose best logits differ and whose scores are equal in 64 bits: sigmoids of 40 and more (1), logits next to 0, a
+    softmax's exponentials below its range: the lower group.  Multiples of 8 and 50 keep the others' scores well apart."""
+    rng = np.random.default_rng(e + g)
+    far = rng.integers(-20, 21, (90, e)) * 8.0
+    near = rng.integers(-9, 10, (90, e)) * 2.0 ** -70
+    low = rng.integers(-60, 1, (90, e)) * 50.0
+    low[:, 3] = 100.0
+    for scoring, x in (("sigmoid", far), ("sigmoid", near), ("softmax", near), ("softmax", low), ("softmax", np.where(rng.random((90, e)) < 0.5, near, low))):
+        check(x, 6, None, bf16=bf16, scoring=scoring, n_groups=g, top_groups=kept, min_k=2, tau=0.7)
