@@ -473,7 +473,7 @@ __global__ __launch_bounds__(256) void experts_join_kernel(ExpertsArgs a) {
     if (lane < a.top_k) {
       const int32_t p = n * a.top_k + lane;
       e = pair_expert(a, p);
-      if (e >= 0) w = OUT_BF16 ? a.ew[p] * (a.hs[p] / kPartUnit) : a.ew[p];
+      if (e >= 0) w = OUT_BF16 ? a.ew[p] * a.hs[p] : a.ew[p];
     }
     float y[8] = {};
     for (uint64_t here = __ballot(e >= 0); here != 0;) {
@@ -514,6 +514,8 @@ __global__ __launch_bounds__(256) void experts_join_kernel(ExpertsArgs a) {
     }
     if (c >= d) continue;
     if (OUT_BF16) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] /= kPartUnit;   // here: a scale of h that large would overflow
       *(u32x4*)((uint16_t*)a.y + (int64_t)n * d + c) =
           u32x4{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])};
     } else {

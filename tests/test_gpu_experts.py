@@ -177,6 +177,22 @@ def test_weights_and_unused_parts():
     assert torch.equal(layer.run(x, idx, w, fanout, ws=ws), y) and bool(y.isfinite().all())
 
 
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [3, 40])
+def test_activations_of_any_size(n, out):
+    """h of up to 1e38, whose scale is above what a factor of 4096 leaves room for, and small ones: y in the range of ordinary numbers."""
+    x, idx, w, _ = _tokens(n, 128, 4, 2, 40)
+    x = x * 1024
+    for up, down in ((2.0 ** 126, 2.0 ** -113), (2.0 ** -60, 2.0 ** 60)):
+        layer = Layer(128, 64, 4, 41)
+        layer.s_gu /= 1024
+        layer.s_gu[:, 64:] *= up
+        layer.s_down *= down
+        y = layer.run(x, idx, w, None, out)
+        assert bool(y.isfinite().all())
+        layer.check(x, idx, w, None, out)
+
+
 def test_no_rows():
     import torch
     x, idx, w, _ = _tokens(2, 64, 2, 1, 13)
