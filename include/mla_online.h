@@ -649,8 +649,8 @@ mla_status mla_cache_attend(const mla_geom* geom, int32_t n_seqs, int32_t n_q, c
  * logit; c = s + bias chooses (a bias for balance changes who is chosen, not the
  * weights):
  *   1. the experts lie in n_groups groups of consecutive ones; a group scores the sum
- *      of its group_best largest c; the top_groups best groups stay (equal scores: the
- *      lower group);
+ *      of its group_best largest c; the top_groups best groups stay (equal scores, also of
+ *      different logits that have one score in 64 bits: the lower group);
  *   2. of their experts the top_k with the largest c, in that order (equal c: the lower
  *      index).  Without a bias the order is that of the logits;
  *   3. weights w_j = s of rank j, divided by their sum if `renormalize` (where the sum is
@@ -739,8 +739,9 @@ mla_status mla_shared_wb_i8(int64_t n_rows, int32_t d_in, int32_t d_out, const v
  *   h_nj = silu(W_gate[e] x_n) * (W_up[e] x_n),   silu(g) = g / (1 + exp(-g))
  * x is quantized a row as mla_i8_quantize does, h is rounded to bf16 and then quantized a
  * row; sums of products are exact in i32 and scaled as in mla_shared_wb_i8; the pairs of
- * a token are summed in f32 in rank order.  A row's result does not depend on the other
- * rows, and a call gives the same bits again.
+ * a token are summed in f32 in rank order.  For a bf16 y the sum of a pair's products is
+ * held in f16 until then, within 2^-11 of its value.  A row's result does not depend on
+ * the other rows, and a call gives the same bits again.
  *
  * A device may hold a share of the experts, [first_expert, first_expert + n_experts):
  * pairs of others add nothing (y of the devices is then summed by the caller; MLA_F32
