@@ -662,7 +662,8 @@ mla_status mla_cache_attend(const mla_geom* geom, int32_t n_seqs, int32_t n_q, c
  * rounding apart come out in their order; weights are within 2^-19 of their value.
  * A NaN never ranks before a number; a row with a NaN or a +infinity has NaN softmax
  * scores (its order stays that of the logits), a row of -infinity alone has scores 0.
- * An expert with bias -infinity is chosen only where nothing else is left.
+ * An expert with bias -infinity is chosen only where nothing else is left; a group whose
+ * group_best largest c have one among them scores -infinity.
  *
  *   n_rows, n_experts   N token rows (below 2^31), E experts (top_k <= E <= 1024)
  *   logits        device [N, E] f32 or bf16 (logits_dtype), rows logits_stride elements

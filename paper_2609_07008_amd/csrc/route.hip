@@ -366,7 +366,8 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, int lg, 
         if (lg > 8) join(dpp<0x140>(g0), dpp<0x140>(g1));
         if (lg > 16) join((uint32_t)__shfl_xor((int)g0, 16, 64), (uint32_t)__shfl_xor((int)g1, 16, 64));
       }
-      const uint32_t score = BY != kByLogit && a.group_best > 1 ? g0 + g1 : g0;
+      // the second best at the bottom (-infinity or NaN): the sum is as well
+      const uint32_t score = BY != kByLogit && a.group_best > 1 && a.n_groups < E ? (g1 == 0 ? 0 : g0 + g1) : g0;
       // places past the last group come behind every group
       const uint32_t key = L == 16 ? (score << 4) | (uint32_t)(15 - sl / lg) : (score << 6) | (uint32_t)(63 - sl / lg);
       int over = 0;

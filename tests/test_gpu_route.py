@@ -162,3 +162,19 @@ def test_groups_of_scores_that_meet(e, g, kept, bf16):
     low[:, 3] = 100.0
     for scoring, x in (("sigmoid", far), ("sigmoid", near), ("softmax", near), ("softmax", low), ("softmax", np.where(rng.random((90, e)) < 0.5, near, low))):
         check(x, 6, None, bf16=bf16, scoring=scoring, n_groups=g, top_groups=kept, min_k=2, tau=0.7)
+
+
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("e,g,kept", [(64, 8, 4), (256, 8, 4), (256, 32, 9), (512, 16, 5)])
+def test_groups_with_one_expert_left(e, g, kept, scoring):
+    """Biases of -infinity and NaN that leave a group one expert, the best of all, or none: the sum of its two best is -infinity or
+    no number, and the group comes behind the others."""
+    x, rng = _logits(200, e, e + kept)
+    size = e // g
+    for off in (-np.inf, np.nan):
+        for left in ((1,), (1, 0), (0, 1, 1)):
+            bias = 0.01 * rng.standard_normal(e)
+            for i, n in enumerate(left):
+                bias[i * size + n:(i + 1) * size] = off
+                x[:, i * size] = 6.0
+            check(x, 6, bias, scoring=scoring, n_groups=g, top_groups=kept, group_best=2, min_k=2, tau=0.7)
