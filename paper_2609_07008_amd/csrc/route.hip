@@ -7,8 +7,8 @@
 // (route_row_kernel, by 16 lanes up to 256 experts, else by a wave): c becomes a fixed-point code of
 // 24 or 22 bits over its whole range, above the inverted index in a 32-bit key, and whatever hangs
 // on two codes that the errors could have swapped sends its row to route_exact: one in some
-// hundreds of rows of random logits.  Where groups do not fall on whole lanes every row takes
-// the 64-bit path.
+// hundreds of rows of random logits.  Where groups do not fit the lanes every row takes the
+// 64-bit path.
 #include "rank.h"
 #include "route.h"
 
@@ -160,6 +160,7 @@ __global__ __launch_bounds__(256) void route_wave_kernel(RouteArgs a) {
 // What ranks a row's experts in route_row_kernel
 enum RouteBy {
   kByLogit,     // no bias: the order of the logits themselves
+  kByPair,      // the same, groups by the scores of their two best
   kBySigmoid,   // c = sigmoid + bias
   kBySoftmax,   // c = softmax + bias
 };
@@ -212,15 +213,17 @@ __device__ __forceinline__ int above(uint32_t key) {
   return 0;
 }
 
-// M consecutive logits of row r from expert M sl on, as f32; past E: -infinity
+// Vectors of logits are loaded in a lane's places below its end, or in all, or in none
+enum { kNarrow, kWide, kWhole };
+
+// M consecutive logits of row r from expert e0 on, as f32; from `end` on: -infinity
 template <int M, bool BF16>
-__device__ __forceinline__ void load_logits(const RouteArgs& a, bool wide, int64_t r, int sl, float (&v)[M]) {
-  const int e0 = M * sl, E = a.n_experts;
+__device__ __forceinline__ void load_logits(const RouteArgs& a, int wide, int64_t r, int e0, int end, float (&v)[M]) {
   constexpr int V = M % 4 == 0 ? 4 : 2;
 #pragma unroll
   for (int i = 0; i < M; i += V) {
     const int e = e0 + i;
-    if (wide && e + V <= E) {
+    if (wide == kWhole || (wide == kWide && e + V <= end)) {
       if constexpr (BF16) {
         const uint32_t* p = (const uint32_t*)((const uint16_t*)a.logits + r * a.stride + e);
         uint32_t u[V / 2];
@@ -250,14 +253,14 @@ __device__ __forceinline__ void load_logits(const RouteArgs& a, bool wide, int64
       }
     } else {
 #pragma unroll
-      for (int k = 0; k < V; ++k) v[i + k] = e + k < E ? logit(a, r, e + k) : -INFINITY;
+      for (int k = 0; k < V; ++k) v[i + k] = e + k < end ? logit(a, r, e + k) : -INFINITY;
     }
   }
 }
 
-// L lanes a row: 16, four rows a wave, up to 256 experts, or the whole wave; lane sl holds experts
-// M sl .. M sl + M - 1, and with groups a group is 1, 2, 4, ... whole lanes (of `lg`).  Each lane
-// keeps its DEPTH largest keys sorted (a max and medians per key); a round takes the row's maximum
+// L lanes a row: 16, four rows a wave, up to 256 experts, or the whole wave; a lane holds M
+// consecutive experts, and with groups a group has 1, 2, 4, ... lanes (`lg`), the last of which may
+// have places past its end.  Each lane keeps its DEPTH largest keys sorted (a max and medians per key); a round takes the row's maximum
 // of the lanes' largest and the owner drops it.
 //
 // Errors of the codes, in steps of 2^-24 of the range 1 + 2 B of c (B the largest finite |bias|):
@@ -267,16 +270,20 @@ __device__ __forceinline__ void load_logits(const RouteArgs& a, bool wide, int64
 // that are 17 apart is certain.  A softmax score takes the sum's error besides (its terms' 1.5 d + 2
 // weighted by e^-d, and 20 additions): below 50, 113 apart.  Codes of 22 bits, under indexes of 10,
 // are off by a quarter of that and by the last two: less than 4 and 16.  A group's score is the
-// sum of two codes: twice that.  In kByLogit codes are the upper bits of the logit's order: exact
+// sum of two codes: twice that.  Without a bias codes are the upper bits of the logit's order: exact
 // for bf16, else equal codes are not certain.  What is no number, or -infinity, has a code at the
-// bottom of its kind, as have the places past E: a row that comes down to it is not certain either.
+// bottom of its kind, as have the places past the end: a row that comes down to it is not certain
+// either.  Ranks nearer than that are certain all the same if logits and biases are equal (bf16
+// logits often are): then so are c, and the lower index has the larger key.
 template <int L, int M, bool BF16, int BY>
-__global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, int lg, bool wide, bool count) {
+__global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, int lg, int wide, bool count) {
   constexpr int ROWS = 64 / L, E_MAX = L * M, IB = L == 16 ? 8 : 10;   // rows a wave, bits of an index
   constexpr int DEPTH = L == 64 ? (M < 5 ? M : 5) : (M < 6 ? M : 6);
+  constexpr bool LOGIT = BY == kByLogit || BY == kByPair;
   constexpr uint32_t APART = BY == kBySigmoid ? (L == 16 ? 17 : 7) : BY == kBySoftmax ? (L == 16 ? 113 : 31) : BF16 ? 0 : 1;
   constexpr uint32_t kNegInfCode = 0x007FFFFFu >> IB;   // of total_order_bits(-infinity)
   constexpr uint32_t kIndex = (1u << IB) - 1;
+  constexpr uint32_t kTwo = 2 * 0x3f800000u;   // bits of 1 twice: kTwo - bits of l carries on from 1 the order of 2 - l
   // a buffer of the 64-bit path for each wave, or (whole waves a row) one for each in turn
   constexpr int BUFS = L == 16 ? 4 : 1;
   __shared__ double score[BUFS][E_MAX];
@@ -291,12 +298,18 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, int lg, 
   }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sl = lane % L, slot = lane / L;
   const bool groups = a.top_groups < a.n_groups;
-  float bias[BY == kByLogit ? 1 : M], unit = 0.f;   // c's code is s * unit + bias: from 1 to 15 below the largest
-  if constexpr (BY != kByLogit) {
+  int e0 = M * sl, end = E;   // the lane's experts
+  if (groups) {
+    const int size = E / a.n_groups, g = sl / lg;
+    e0 = g < a.n_groups ? g * size + M * (sl % lg) : 0;
+    end = g < a.n_groups ? (g + 1) * size : 0;
+  }
+  float bias[LOGIT ? 1 : M], unit = 0.f;   // c's code is s * unit + bias: from 1 to 15 below the largest
+  if constexpr (!LOGIT) {
     float b = 0.f;
 #pragma unroll
     for (int i = 0; i < M; ++i) {
-      bias[i] = M * sl + i >= E ? -INFINITY : a.bias != nullptr ? a.bias[M * sl + i] : 0.f;
+      bias[i] = e0 + i < end ? a.bias[e0 + i] : -INFINITY;
       if (fabsf(bias[i]) < INFINITY) b = fmaxf(b, fabsf(bias[i]));
     }
     b = row_max<L>(b);
@@ -312,7 +325,7 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, int lg, 
   uint64_t again = 0;
   int turn = 0, taken = -1;   // taken: the expert that a lane's rank of the last turn executes
   float cur[M];
-  if (r - slot <= last) load_logits<M, BF16>(a, wide, r < last ? r : last, sl, cur);
+  if (r - slot <= last) load_logits<M, BF16>(a, wide, r < last ? r : last, e0, end, cur);
   for (; r - slot <= last; r += stride) {
     const int64_t rc = r < last ? r : last;
     float top = 0.f, total = 0.f;   // softmax: largest logit, sum of exponentials
@@ -324,7 +337,7 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, int lg, 
       float part[4] = {};
 #pragma unroll
       for (int i = 0; i < M; ++i) {
-        const float e = exp_fast(cur[i] - top);   // past E: 0
+        const float e = exp_fast(cur[i] - top);   // past the end: 0
         part[i & 3] += e;
         if constexpr (BY == kBySoftmax) cur[i] = e;
       }
@@ -333,11 +346,13 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, int lg, 
     const float inv = BY == kBySoftmax ? __builtin_amdgcn_rcpf(total) : 0.f;
     typedef uint32_t Keys __attribute__((ext_vector_type(DEPTH)));   // an array's selects become indexed ones
     Keys m = 0;
+    bool unsure = false;
 #pragma unroll
     for (int i = 0; i < M; ++i) {
-      const int e = M * sl + i;
+      const int e = e0 + i;
       uint32_t code;
-      if constexpr (BY == kByLogit) {
+      if constexpr (BY == kByPair) unsure |= cur[i] != cur[i];   // a group's sum with it is no number
+      if constexpr (LOGIT) {
         code = total_order_bits(fmaxf(cur[i], -INFINITY) + 0.0f) >> IB;   // NaN as -infinity, -0 as 0
       } else {
         const float s = BY == kBySigmoid ? __builtin_amdgcn_rcpf(1.f + exp_fast(-cur[i])) : cur[i] * inv;
@@ -350,8 +365,7 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, int lg, 
       m[0] = max_u32(m[0], x);
     }
     // the next row, over the registers just consumed
-    if (r - slot + stride <= last) load_logits<M, BF16>(a, wide, r + stride < last ? r + stride : last, sl, cur);
-    bool unsure = false;
+    if (r - slot + stride <= last) load_logits<M, BF16>(a, wide, r + stride < last ? r + stride : last, e0, end, cur);
     if (groups) {
       uint32_t g0 = m[0] >> IB, g1 = m[1] >> IB;
       auto join = [&](uint32_t o0, uint32_t o1) {
@@ -366,8 +380,38 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, int lg, 
         if (lg > 8) join(dpp<0x140>(g0), dpp<0x140>(g1));
         if (lg > 16) join((uint32_t)__shfl_xor((int)g0, 16, 64), (uint32_t)__shfl_xor((int)g1, 16, 64));
       }
-      // the second best at the bottom (-infinity or NaN): the sum is as well
-      const uint32_t score = BY != kByLogit && a.group_best > 1 && a.n_groups < E ? (g1 == 0 ? 0 : g0 + g1) : g0;
+      uint32_t score;
+      uint32_t lo = 0, hi = 0;   // kByPair: the order of a sum less and plus its error
+      if constexpr (BY == kByPair) {
+        // The scores (a softmax's without its sum) of the middles of the two codes: the logit is off by
+        // |x| 2^(IB - 24), the exponential by (1.5 * 70 + 2) 2^-24 of itself and what follows by 6.  Taken
+        // twice and more, in relative terms.  Sigmoids that add up to more than 1 are ordered by what
+        // lacks to 2, sigmoid(-x) each, which has its bits where they have none.
+        float sum = 0.f, err = 0.f, lack = 0.f, lack_err = 0.f;
+        auto add = [&](uint32_t code) {
+          const float x = code <= kNegInfCode ? -1e30f : fminf(from_total_order_bits((code << IB) | (1u << (IB - 1))), 1e30f);
+          const float off = fabsf(x) * (1.f / (1 << (22 - IB))) + 0x1p-15f;
+          const float s = a.sigmoid ? __builtin_amdgcn_rcpf(1.f + exp_fast(-x)) : exp_fast(x - top);
+          sum += s;
+          err += s * off;
+          if (a.sigmoid) {
+            const float l = __builtin_amdgcn_rcpf(1.f + exp_fast(x));
+            lack += l;
+            lack_err += l * off;
+          }
+        };
+        add(g0);
+        add(g1);
+        const bool by_lack = a.sigmoid && sum > 1.f;
+        auto order = [&](float v, float l) { return by_lack ? kTwo - __float_as_uint(fmaxf(l, 0.f)) : __float_as_uint(fmaxf(v, 0.f)); };
+        const bool group = sl / lg < a.n_groups;
+        score = group ? order(sum, lack) >> (L == 16 ? 3 : 5) : 0u;
+        lo = order(sum - err, lack + lack_err);
+        hi = group ? order(sum + err, lack - lack_err) : 0u;
+      } else {
+        // the second best at the bottom (-infinity or NaN): the sum is as well
+        score = !LOGIT && a.group_best > 1 && a.n_groups < E ? (g1 == 0 ? 0 : g0 + g1) : g0;
+      }
       // places past the last group come behind every group
       const uint32_t key = L == 16 ? (score << 4) | (uint32_t)(15 - sl / lg) : (score << 6) | (uint32_t)(63 - sl / lg);
       int over = 0;
@@ -377,43 +421,76 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, int lg, 
         for (int g = 0; g < a.n_groups; ++g) over += (uint32_t)__builtin_amdgcn_readlane((int)key, g * lg) > key ? 1 : 0;
       }
       const bool kept = over < a.top_groups;
-      // the least kept score and the largest other
-      const uint32_t least = ~row_max<L>(kept ? ~score : 0u), most = row_max<L>(kept ? 0u : score);
-      unsure = least < most + 2 * APART || (BY == kByLogit && least <= kNegInfCode);
-      if constexpr (BY == kByLogit) {
-        // Groups go by scores, and those of different logits may be equal in 64 bits: a sigmoid next to
-        // 1 or to 1/2, an exponential of next to `top` or out of range.  Codes apart are logits 2^-16
-        // of themselves apart, which elsewhere is far above a step of the score.
-        const float x = from_total_order_bits(least << IB);
-        unsure |= !(fabsf(x) >= 0x1p-20f * fmaxf(1.f, fabsf(top)) && top - x < 600.f && !(a.sigmoid && x > 24.f));
+      if constexpr (BY == kByPair) {
+        // a sum of next to nothing, or 2^-33 from 2, may have 64-bit equals
+        const uint32_t least = ~row_max<L>(kept ? ~lo : 0u), most = row_max<L>(kept ? 0u : hi);
+        unsure |= !(least > most && least > __builtin_bit_cast(uint32_t, 1e-30f)) || (a.sigmoid && most > kTwo - __builtin_bit_cast(uint32_t, 0x1p-33f));
+      } else {
+        // the least kept score and the largest other
+        const uint32_t least = ~row_max<L>(kept ? ~score : 0u), most = row_max<L>(kept ? 0u : score);
+        unsure = least < most + 2 * APART;
+        if constexpr (LOGIT) {
+          // Groups go by scores, and those of different logits may be equal in 64 bits: a sigmoid next to
+          // 1 or to 1/2, an exponential of next to `top` or out of range.  Codes apart are logits 2^-16
+          // of themselves apart, which elsewhere is far above a step of the score.
+          const float x = from_total_order_bits(least << IB);
+          unsure |= least <= kNegInfCode || !(fabsf(x) >= 0x1p-20f * fmaxf(1.f, fabsf(top)) && top - x < 600.f && !(a.sigmoid && x > 24.f));
+        }
       }
 #pragma unroll
       for (int d = 0; d < DEPTH; ++d) m[d] = kept ? m[d] : 0u;
     }
     const bool full = M > DEPTH && m[DEPTH - 1] != 0;
-    int32_t my_id = 0;
-    uint32_t before = 0xFFFFFFFFu;   // code of the rank before
+    uint32_t my_key = 0, before = 0;   // key of the lane's rank, and of the last one
     int drops = 0;
+    auto drop = [&](uint32_t top_key, bool there) {
+      const bool own = there && m[0] == top_key;
+      drops += own;
+#pragma unroll
+      for (int d = 0; d + 1 < DEPTH; ++d) m[d] = own ? m[d + 1] : m[d];
+      m[DEPTH - 1] = own ? 0u : m[DEPTH - 1];
+    };
 #pragma unroll
     for (int j = 0; j < kMoeMaxTopK; ++j) {
       if (j < TK) {
-        const uint32_t top_key = row_max<L>(m[0]);
-        if (sl == j) my_id = (int32_t)(kIndex - (top_key & kIndex));
-        unsure |= before - (top_key >> IB) < APART;
-        before = top_key >> IB;
-        const bool own = m[0] == top_key;
-        drops += own;
-#pragma unroll
-        for (int d = 0; d + 1 < DEPTH; ++d) m[d] = own ? m[d + 1] : m[d];
-        m[DEPTH - 1] = own ? 0u : m[DEPTH - 1];
+        before = row_max<L>(m[0]);
+        if (sl == j) my_key = before;
+        drop(before, true);
       }
     }
-    unsure |= before - (row_max<L>(m[0]) >> IB) < APART;   // the runner-up; nothing left: code 0
-    unsure |= full && drops >= DEPTH;                      // the lane's next key is not known
-    unsure |= BY == kByLogit ? before <= kNegInfCode : before <= APART + 1;
+    unsure |= LOGIT ? before >> IB <= kNegInfCode : before >> IB <= APART + 1;
+    // logit and bias of a key's expert; a place past E is not certain, see above
+    auto expert = [&](uint32_t key) { return (int32_t)(kIndex - (key & kIndex)); };
+    auto values = [&](uint32_t key, float& x, float& b) {
+      const int32_t e = expert(key) < E ? expert(key) : 0;
+      x = logit(a, rc, e);
+      b = LOGIT ? 0.f : a.bias[e];
+    };
     // the ranks' scores: lane j of the row holds rank j
     const bool rank = sl < TK;
-    const float x = rank ? logit(a, rc, my_id < E ? my_id : 0) : 0.f;   // a place past E: not certain, see above
+    const int32_t my_id = expert(my_key);
+    float x = 0.f, b = 0.f;
+    if (rank) values(my_key, x, b);
+    uint32_t next = row_max<L>(m[0]);   // the runner-up; nothing left: code 0
+    if constexpr (APART > 0) {
+      const uint32_t prev = dpp<0x111>(my_key);   // row_shr:1
+      const bool same = x == __uint_as_float(dpp<0x111>(__float_as_uint(x))) && b == __uint_as_float(dpp<0x111>(__float_as_uint(b)));
+      unsure |= rank && sl > 0 && (prev >> IB) - (my_key >> IB) < APART && !same;
+      // runners-up equal to the last rank come behind it: the first that is not decides
+      bool near = (before >> IB) - (next >> IB) < APART;
+      for (int more = 0; more < DEPTH && __ballot(near) != 0; ++more) {
+        float xn, bn;
+        values(next, xn, bn);
+        const int from = lane - sl + TK - 1;
+        const bool equal = near && xn == __shfl(x, from, 64) && bn == __shfl(b, from, 64);
+        unsure |= near && !equal;
+        drop(next, equal);
+        next = row_max<L>(m[0]);
+        near = equal && (before >> IB) - (next >> IB) < APART;
+      }
+      unsure |= near;
+    }
+    unsure |= full && drops >= DEPTH;   // the lane's next key is not known
     const float d = a.sigmoid ? -fabsf(x) : x - top;
     float e = expf(d);
     if (!a.sigmoid) e += e * ((x - d) - top);   // what the rounding of the difference took
@@ -476,8 +553,9 @@ RowShape row_shape(const RouteArgs& a) {
         if (M > 2 && E <= L * M) return {L, M, L};
         continue;
       }
-      const int lg = size / M;
-      if (size % M == 0 && (lg & (lg - 1)) == 0 && lg > 0 && G * lg <= L) return {L, M, lg};
+      int lg = 1;
+      while (lg * M < size) lg *= 2;
+      if (G * lg <= L) return {L, M, lg};
     }
   return {0, 0, 0};
 }
@@ -488,10 +566,13 @@ hipError_t launch_rows(const RouteArgs& a, int lg, bool count, hipStream_t s) {
   const int64_t blocks = (a.n_rows + ROWS - 1) / ROWS;
   const dim3 grid((unsigned)std::max(std::min<int64_t>(blocks, 2048), (blocks + L - 1) / L)), blk(256);
   // vectors of 4 (2 where a lane's share is not whole fours) logits
-  const int64_t bytes = (M % 4 == 0 ? 4 : 2) * (BF16 ? 2 : 4);
-  const bool wide = reinterpret_cast<uintptr_t>(a.logits) % bytes == 0 && a.stride * (BF16 ? 2 : 4) % bytes == 0;
-  if (a.bias == nullptr && (a.top_groups == a.n_groups || a.group_best == 1))
-    route_row_kernel<L, M, BF16, kByLogit><<<grid, blk, 0, s>>>(a, lg, wide, count);
+  const int64_t vec = M % 4 == 0 ? 4 : 2, bytes = vec * (BF16 ? 2 : 4);
+  const bool groups = a.top_groups < a.n_groups;
+  const bool fit = reinterpret_cast<uintptr_t>(a.logits) % bytes == 0 && a.stride * (BF16 ? 2 : 4) % bytes == 0 &&
+                   (!groups || a.n_experts / a.n_groups % vec == 0);
+  const int wide = !fit ? kNarrow : a.n_experts == L * M ? kWhole : kWide;   // E places: no lane has one past its end
+  if (a.bias == nullptr && groups && a.group_best > 1) route_row_kernel<L, M, BF16, kByPair><<<grid, blk, 0, s>>>(a, lg, wide, count);
+  else if (a.bias == nullptr) route_row_kernel<L, M, BF16, kByLogit><<<grid, blk, 0, s>>>(a, lg, wide, count);
   else if (a.sigmoid) route_row_kernel<L, M, BF16, kBySigmoid><<<grid, blk, 0, s>>>(a, lg, wide, count);
   else route_row_kernel<L, M, BF16, kBySoftmax><<<grid, blk, 0, s>>>(a, lg, wide, count);
   return hipGetLastError();

@@ -178,3 +178,32 @@ def test_groups_with_one_expert_left(e, g, kept, scoring):
                 bias[i * size + n:(i + 1) * size] = off
                 x[:, i * size] = 6.0
             check(x, 6, bias, scoring=scoring, n_groups=g, top_groups=kept, group_best=2, min_k=2, tau=0.7)
+
+
+@pytest.mark.parametrize("e,g,kept,k", [(200, 8, 3, 8), (200, 5, 2, 6), (200, 4, 1, 8), (200, 2, 1, 5), (60, 4, 2, 6), (60, 2, 1, 8), (96, 16, 4, 8), (35, 5, 2, 4), (14, 7, 3, 4),
+                                        (6, 6, 4, 3), (254, 2, 1, 8), (252, 4, 3, 8), (255, 15, 5, 7), (500, 4, 2, 8), (999, 3, 2, 8), (1022, 2, 1, 8), (945, 63, 9, 8), (130, 13, 4, 6),
+                                        (31, 31, 8, 8), (124, 62, 7, 8)])
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+def test_groups_of_any_size(scoring, e, g, kept, k):
+    """Groups that do not fill their lanes, in every order of the logits."""
+    x, rng = _logits(237, e, e + g)
+    for bias in (rng.standard_normal(e) * (0.2 if scoring == "sigmoid" else 0.3 / e), None):
+        for best in (1, 2):
+            for bf16 in (False, True):
+                check(x, k, bias, bf16=bf16, pad=best, scoring=scoring, n_groups=g, top_groups=kept, group_best=best, min_k=1, tau=0.8)
+
+
+@pytest.mark.parametrize("e,groups", [(256, dict()), (256, dict(n_groups=8, top_groups=4, group_best=2)), (512, dict()), (1024, dict(n_groups=16, top_groups=5, group_best=2)),
+                                      (40, dict())])
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+def test_equal_ranks(scoring, e, groups):
+    """Logits in steps and biases of few values: chosen experts, and the last one and those behind it, are often equal; a few of
+    them differ by less than the codes do."""
+    x, rng = _logits(700, e, e)
+    x = np.rint(x * 8) / 8
+    for bias in (None, np.zeros(e), rng.integers(-2, 3, e) * 0.001):
+        check(x, 5, bias, scoring=scoring, min_k=2, tau=0.8, **groups)
+        near = x + np.where(rng.random(x.shape) < 0.02, 2.0 ** -20, 0.0)
+        check(near, 8, bias, scoring=scoring, min_k=8, **groups)
+    x = np.repeat(np.rint(rng.standard_normal((300, 1)) * 4), e, 1)   # all equal
+    check(x, 6, np.zeros(e), scoring=scoring, min_k=3, tau=0.7, **groups)
