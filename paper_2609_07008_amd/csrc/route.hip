@@ -493,7 +493,10 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, int lg, 
     unsure |= full && drops >= DEPTH;   // the lane's next key is not known
     const float d = a.sigmoid ? -fabsf(x) : x - top;
     float e = expf(d);
-    if (!a.sigmoid) e += e * ((x - d) - top);   // what the rounding of the difference took
+    if (!a.sigmoid) {   // what the rounding of the difference took, whichever of the two is larger
+      const float x1 = d + top, top1 = x1 - d;
+      e += e * ((x - x1) - (top - top1));
+    }
     float s = a.sigmoid ? (x < 0.f ? e : 1.f) * __builtin_amdgcn_rcpf(1.f + e) : e * __builtin_amdgcn_rcpf(total);
     s = rank ? s : 0.f;
     float upto = s;   // sums of the ranks up to the lane's

@@ -207,3 +207,14 @@ def test_equal_ranks(scoring, e, groups):
         check(near, 8, bias, scoring=scoring, min_k=8, **groups)
     x = np.repeat(np.rint(rng.standard_normal((300, 1)) * 4), e, 1)   # all equal
     check(x, 6, np.zeros(e), scoring=scoring, min_k=3, tau=0.7, **groups)
+
+
+@pytest.mark.parametrize("e", [64, 256, 1000])
+def test_weights_far_from_the_largest(e):
+    """Largest logits of up to 120 of either sign and others that lie up to 60 below: the difference's rounding does not reach the weight."""
+    rng = np.random.default_rng(e)
+    top = rng.uniform(-120, 120, (4000, 1))
+    x = np.repeat(top - 90.0, e, 1)
+    x[:, :8] = top - np.sort(rng.uniform(0, 60, (4000, 8)), axis=1) * (np.arange(8) > 0)
+    for renorm in (False, True):
+        check(x, 8, None, scoring="softmax", min_k=8, renormalize=renorm)
