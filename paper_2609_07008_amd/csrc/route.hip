@@ -268,8 +268,9 @@ __device__ __forceinline__ void load_logits(const RouteArgs& a, int wide, int64_
 // s (1 - s) |l| < 0.23 reach s; 1 + e and its reciprocal add 3 s: below 4.  The bias in code units
 // is off by 2, the fma by 1/2, the conversion by 1: a code by less than 8, and the order of two
 // that are 17 apart is certain.  A softmax score takes the sum's error besides (its terms' 1.5 d + 2
-// weighted by e^-d, and 20 additions): below 50, 113 apart.  Codes of 22 bits, under indexes of 10,
-// are off by a quarter of that and by the last two: less than 4 and 16.  A group's score is the
+// weighted by e^-d, and 20 additions), relative, below 50, and its factor's 2: with the bias's 2 and
+// the last two below 56 of its range, the row's largest score + 2 B: 113 apart.  Codes of 22 bits,
+// under indexes of 10, are off by a quarter of that and by the last two: less than 4 and 16.  A group's score is the
 // sum of two codes: twice that.  Without a bias codes are the upper bits of the logit's order: exact
 // for bf16, else equal codes are not certain.  What is no number, or -infinity, has a code at the
 // bottom of its kind, as have the places past the end: a row that comes down to it is not certain
@@ -304,7 +305,7 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, int lg, 
     e0 = g < a.n_groups ? g * size + M * (sl % lg) : 0;
     end = g < a.n_groups ? (g + 1) * size : 0;
   }
-  float bias[LOGIT ? 1 : M], unit = 0.f;   // c's code is s * unit + bias: from 1 to 15 below the largest
+  float bias[LOGIT ? 1 : M], unit = 0.f, two_b = 0.f;   // c's code is (s + b + B) unit + 1: from 1 to 15 below the largest
   if constexpr (!LOGIT) {
     float b = 0.f;
 #pragma unroll
@@ -313,9 +314,10 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, int lg, 
       if (fabsf(bias[i]) < INFINITY) b = fmaxf(b, fabsf(bias[i]));
     }
     b = row_max<L>(b);
-    unit = (float)((1 << (32 - IB)) - 16) / (1.f + 2.f * b);
+    two_b = 2.f * b;
+    unit = (float)((1 << (32 - IB)) - 16) / (1.f + two_b);   // of a softmax for each row
 #pragma unroll
-    for (int i = 0; i < M; ++i) bias[i] = (bias[i] + b) * unit + 1.f;
+    for (int i = 0; i < M; ++i) bias[i] = BY == kBySoftmax ? bias[i] + b : (bias[i] + b) * unit + 1.f;
   }
   const int64_t stride = (int64_t)gridDim.x * (4 * ROWS), last = a.n_rows - 1;
   const int64_t first = ((int64_t)blockIdx.x * 4 + wave) * ROWS;
@@ -343,7 +345,12 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, int lg, 
       }
       total = row_sum<L>((part[0] + part[1]) + (part[2] + part[3]));
     }
-    const float inv = BY == kBySoftmax ? __builtin_amdgcn_rcpf(total) : 0.f;
+    float inv = 0.f;
+    if constexpr (BY == kBySoftmax) {   // the row's largest score: its codes span that and 2 B
+      inv = __builtin_amdgcn_rcpf(total);
+      unit = (float)((1 << (32 - IB)) - 16) * __builtin_amdgcn_rcpf(inv + two_b);
+      inv *= unit;
+    }
     typedef uint32_t Keys __attribute__((ext_vector_type(DEPTH)));   // an array's selects become indexed ones
     Keys m = 0;
     bool unsure = false;
@@ -355,9 +362,9 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, int lg, 
       if constexpr (LOGIT) {
         code = total_order_bits(fmaxf(cur[i], -INFINITY) + 0.0f) >> IB;   // NaN as -infinity, -0 as 0
       } else {
-        const float s = BY == kBySigmoid ? __builtin_amdgcn_rcpf(1.f + exp_fast(-cur[i])) : cur[i] * inv;
         // v_cvt takes NaN and what is below 0 to 0, +infinity to 2^32 - 1: the largest code
-        code = to_u32(fmaf(s, unit, bias[i]));
+        if constexpr (BY == kBySigmoid) code = to_u32(fmaf(__builtin_amdgcn_rcpf(1.f + exp_fast(-cur[i])), unit, bias[i]));
+        else code = to_u32(fmaf(cur[i], inv, fmaf(bias[i], unit, 1.f)));
       }
       const uint32_t x = (code << IB) | (kIndex - (uint32_t)e);
 #pragma unroll
