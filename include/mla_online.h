@@ -740,9 +740,8 @@ mla_status mla_shared_wb_i8(int64_t n_rows, int32_t d_in, int32_t d_out, const v
  *   h_nj = silu(W_gate[e] x_n) * (W_up[e] x_n),   silu(g) = g / (1 + exp(-g))
  * x is quantized a row as mla_i8_quantize does, h is rounded to bf16 and then quantized a
  * row; sums of products are exact in i32 and scaled as in mla_shared_wb_i8; the pairs of
- * a token are summed in f32 in rank order.  For a bf16 y the sum of a pair's products is
- * held in f16 until then, within 2^-11 of its value.  A row's result does not depend on
- * the other rows, and a call gives the same bits again.
+ * a token are summed in f32 in rank order, and a bf16 y is that sum rounded once.  A row's
+ * result does not depend on the other rows, and a call gives the same bits again.
  *
  * A device may hold a share of the experts, [first_expert, first_expert + n_experts):
  * pairs of others add nothing (y of the devices is then summed by the caller; MLA_F32

@@ -6,8 +6,8 @@
 // pairs hangs on LDS atomics, but rows do not meet and the products are exact in i32: the result
 // does not.
 // With few rows an expert the time is that of its weights: 64 tokens over 256 experts 4096 x 2048, of
-// which 129 are met, 505 us, 6.3 TB/s.  With many it is the products': 33,792 tokens 4.7 ms, of which
-// gate and up 2.58 (2.0 POP/s), down 1.45, the join 0.34, quantizing x and h 0.08 and 0.15.
+// which 129 are met, 505 us, 6.3 TB/s.  With many it is the products': 33,792 tokens 5.2 ms, of which
+// gate and up 2.57 (2.0 POP/s), down 1.74, the join 0.53, quantizing x and h 0.08 and 0.15.
 #include "i8_rows.h"
 #include "i8_tiles.h"
 
@@ -220,17 +220,11 @@ __device__ __forceinline__ void gate_up_tile(const ExpertsArgs& a, const Place& 
   }
 }
 
-// A sum of W_down's products on its way to the join of a bf16 y: f16 of sum * 2^-12.  Sums are
-// below 128 * 127 * 16384 and whole, so that none overflows, none but 0 is subnormal, and each
-// is rounded by half a step 2^-11 of it: an eighth of what the rounding of y to bf16 is.  Scales
-// come on in f32 at the join.  f32 parts would be 2.5 GB out and 2.5 GB in for 33,792 rows x 4096.
-constexpr float kPartUnit = 0x1p-12f;
-
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-
-// W_down h of 32 MI rows x BN channels; rows leave through LDS, whole lines of each pair's part
-template <bool F16, int MI, int BN, int NST>
+// W_down h of 32 MI rows x BN channels, in f32 and without the scale of h: that is one number a pair,
+// which the join has at hand (here it is a load that waits for a load; down and join of 33,792 rows
+// 2.44 ms with it, 2.27 without).  Rows leave through LDS, whole lines of each pair's part: 2.5 GB out,
+// and in again at the join.
+template <int MI, int BN, int NST>
 __device__ __forceinline__ void down_tile(const ExpertsArgs& a, const Place& at, unsigned char* lds) {
   using Tile = I8Tile<MI, BN, NST>;
   constexpr int NI = Tile::NI;
@@ -244,40 +238,30 @@ __device__ __forceinline__ void down_tile(const ExpertsArgs& a, const Place& at,
   });
   tile.product(lds, wave, lane, f, (at.rows + 31) / 32);
   const int wm = wave >> 2, wn = wave & 3, lg = lane >> 4, lc = lane & 15;
-  constexpr int ES = F16 ? 2 : 4, ROW = BN / 4 * ES, CH = ROW / 16, RPI = 64 / CH, SW = CH < 8 ? CH - 1 : 7;
+  constexpr int ROW = BN, CH = ROW / 16, RPI = 64 / CH, SW = CH < 8 ? CH - 1 : 7;   // bytes of a wave's BN / 4 sums
   unsigned char MLA_LDS* sw = (unsigned char MLA_LDS*)lds + wave * (2 * 16 * ROW);
   f32x4 ws[NI];
-  if (!F16) {
 #pragma unroll
-    for (int j = 0; j < NI; ++j)
-      ws[j] = *(const f32x4*)(a.s_down + (int64_t)at.expert * d + std::min(n0 + wn * (BN / 4) + j * 16 + lg * 4, d - 4));
-  }
-  const int rl = lane / CH, cl = lane % CH, n = n0 + wn * (BN / 4) + cl * (16 / ES);
+  for (int j = 0; j < NI; ++j)
+    ws[j] = *(const f32x4*)(a.s_down + (int64_t)at.expert * d + std::min(n0 + wn * (BN / 4) + j * 16 + lg * 4, d - 4));
+  const int rl = lane / CH, cl = lane % CH, n = n0 + wn * (BN / 4) + cl * 4;
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
     const int r0 = Tile::row_of(wm, i);
     if (r0 >= at.rows) break;
     unsigned char MLA_LDS* sb = sw + (i & 1) * (16 * ROW);
-    const float hs = F16 ? 0.f : a.hs[a.pairs[at.row + std::min(r0 + lc, at.rows - 1)].y];
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
-      if (F16) {
-        f16x4 v;
+      f32x4 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (_Float16)((float)tile.acc[i][j][e] * kPartUnit);
-        *(f16x4 MLA_LDS*)(sb + lc * ROW + (((j * 2 + (lg >> 1)) ^ (lc & SW)) * 16) + (lg & 1) * 8) = v;
-      } else {
-        f32x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (float)tile.acc[i][j][e] * ws[j][e] * hs;
-        *(f32x4 MLA_LDS*)(sb + lc * ROW + (((j * 4 + lg) ^ (lc & SW)) * 16)) = v;
-      }
+      for (int e = 0; e < 4; ++e) v[e] = (float)tile.acc[i][j][e] * ws[j][e];
+      *(f32x4 MLA_LDS*)(sb + lc * ROW + (((j * 4 + lg) ^ (lc & SW)) * 16)) = v;
     }
 #pragma unroll
     for (int p = 0; p < 16 / RPI; ++p) {
       const int r = p * RPI + rl, m = r0 + r;
-      const u32x4 v = *(const u32x4 MLA_LDS*)(sb + r * ROW + ((cl ^ (r & SW)) * 16));
-      if (m < at.rows && n < d) *(u32x4*)((unsigned char*)a.part + ((int64_t)a.pairs[at.row + m].y * d + n) * ES) = v;
+      const f32x4 v = *(const f32x4 MLA_LDS*)(sb + r * ROW + ((cl ^ (r & SW)) * 16));
+      if (m < at.rows && n < d) *(f32x4*)(a.part + (int64_t)a.pairs[at.row + m].y * d + n) = v;
     }
   }
 }
@@ -424,7 +408,7 @@ __global__ __launch_bounds__(I8_WAVES * 64, 2) void experts_few_gate_up_kernel(E
   if (lg < 2 && lc < rows) *(u32x2*)(a.h + (int64_t)row_pair[lc] * f + c) = u32x2{pack_bf16x2(h[0], h[1]), pack_bf16x2(h[2], h[3])};
 }
 
-template <bool F16, int NV>
+template <int NV>
 __global__ __launch_bounds__(I8_WAVES * 64, 2) void experts_few_down_kernel(ExpertsArgs a, int n_pairs, int cols) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[kFewLds];
   __shared__ int row_pair[16];
@@ -444,42 +428,37 @@ __global__ __launch_bounds__(I8_WAVES * 64, 2) void experts_few_down_kernel(Expe
   const int lg = lane >> 4, lc = lane & 15, c = n0 + lg * 4;
   if (col == 0 && (int)threadIdx.x < rows) a.hs[row_pair[threadIdx.x]] = scale[threadIdx.x];
   if (lc >= rows || c >= d) return;
-  const int64_t at = (int64_t)row_pair[lc] * d + c;
-  if (F16) {
-    f16x4 v;
+  const f32x4 s = *(const f32x4*)(a.s_down + (int64_t)expert * d + c);
+  f32x4 v;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (_Float16)((float)acc[e] * kPartUnit);
-    *(f16x4*)((_Float16*)a.part + at) = v;
-  } else {
-    const f32x4 s = *(const f32x4*)(a.s_down + (int64_t)expert * d + c);
-    f32x4 v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (float)acc[e] * s[e] * scale[lc];
-    *(f32x4*)((float*)a.part + at) = v;
-  }
+  for (int e = 0; e < 4; ++e) v[e] = (float)acc[e] * s[e];
+  *(f32x4*)(a.part + (int64_t)row_pair[lc] * d + c) = v;
 }
 
 // y of a token: its pairs' parts in rank order, 512 channels a wave.  Lane j reads the token's
 // pair j; what is chosen by it is then uniform.
 template <bool OUT_BF16>
 __global__ __launch_bounds__(256) void experts_join_kernel(ExpertsArgs a) {
-  constexpr int G = 2;   // parts under way at once: more waves hide more (33,792 rows 331 us, with four 363)
+  constexpr int G = 2;   // parts under way at once (33,792 rows 530 us, with four the same)
   const int lane = threadIdx.x & 63, d = a.d_model, chunks = (d + 511) / 512;
   const int units = (int)a.n_rows * chunks;
   for (int u = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); u < units; u += gridDim.x * 4) {
     const int n = u / chunks, c = (u - n * chunks) * 512 + lane * 8;
-    int e = -1;
-    float w = 0.f;
+    bool mine = false;
+    float w = 0.f, hs = 0.f;
     if (lane < a.top_k) {
       const int32_t p = n * a.top_k + lane;
-      e = pair_expert(a, p);
-      if (e >= 0) w = OUT_BF16 ? a.ew[p] * a.hs[p] : a.ew[p];
+      mine = pair_expert(a, p) >= 0;
+      if (mine) {
+        w = a.ew[p];
+        hs = a.hs[p];
+      }
     }
+    auto of = [](float v, int j) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), j)); };
     float y[8] = {};
-    for (uint64_t here = __ballot(e >= 0); here != 0;) {
-      u32x4 v[G][OUT_BF16 ? 1 : 2];
-      f32x4 s[G][2];
-      float wj[G];
+    for (uint64_t here = __ballot(mine); here != 0;) {
+      f32x4 v[G][2];
+      float wj[G], hj[G];
       int got = 0;
 #pragma unroll
       for (int g = 0; g < G; ++g) {
@@ -487,35 +466,23 @@ __global__ __launch_bounds__(256) void experts_join_kernel(ExpertsArgs a) {
         const int j = __builtin_ctzll(here);
         here &= here - 1;
         got = g + 1;
-        wj[g] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(w), j));
-        const int ej = __builtin_amdgcn_readlane(e, j);
+        wj[g] = of(w, j);
+        hj[g] = of(hs, j);
         if (c < d) {
-          const unsigned char* part = (const unsigned char*)a.part + ((int64_t)n * a.top_k + j) * d * (OUT_BF16 ? 2 : 4);
-          if (OUT_BF16) {
-            v[g][0] = __builtin_nontemporal_load((const u32x4*)(part + c * 2));
-            const f32x4* ws = (const f32x4*)(a.s_down + (int64_t)ej * d + c);
-            s[g][0] = ws[0];
-            s[g][1] = ws[1];
-          } else {
-            v[g][0] = ((const u32x4*)(part + c * 4))[0];
-            v[g][1] = ((const u32x4*)(part + c * 4))[1];
-          }
+          const f32x4* part = (const f32x4*)(a.part + ((int64_t)n * a.top_k + j) * d + c);
+          v[g][0] = __builtin_nontemporal_load(part);
+          v[g][1] = __builtin_nontemporal_load(part + 1);
         }
       }
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         if (g >= got) break;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float x = OUT_BF16 ? (float)__builtin_bit_cast(f16x8, v[g][0])[k] * s[g][k / 4][k % 4] : __uint_as_float(v[g][k / 4][k % 4]);
-          y[k] += wj[g] * x;
-        }
+        for (int k = 0; k < 8; ++k) y[k] += wj[g] * (v[g][k / 4][k % 4] * hj[g]);
       }
     }
     if (c >= d) continue;
     if (OUT_BF16) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] /= kPartUnit;   // here: a scale of h that large would overflow
       *(u32x4*)((uint16_t*)a.y + (int64_t)n * d + c) =
           u32x4{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])};
     } else {
@@ -546,16 +513,16 @@ __global__ __launch_bounds__(I8_WAVES * 64, experts_lds(MI, BN) <= 80 * 1024 ? 4
   if constexpr (MI > 2) gate_up_tile<2, BN, 3>(a, at, lds);
 }
 
-template <bool F16, int MI, int BN>
+template <int MI, int BN>
 __global__ __launch_bounds__(I8_WAVES * 64, experts_lds(MI, BN) <= 80 * 1024 ? 4 : 2) void experts_down_kernel(ExpertsArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[experts_lds(MI, BN)];
   const Place at = my_tile(a, (a.d_model + BN - 1) / BN);
   if (!at.any) return;
-  if (MI == 2 || at.rows > 16 * MI) return down_tile<F16, MI, BN, MI == 8 ? 2 : 3>(a, at, lds);
+  if (MI == 2 || at.rows > 16 * MI) return down_tile<MI, BN, MI == 8 ? 2 : 3>(a, at, lds);
   if constexpr (MI == 8) {
-    if (at.rows > 64) return down_tile<F16, 4, BN, 3>(a, at, lds);
+    if (at.rows > 64) return down_tile<4, BN, 3>(a, at, lds);
   }
-  if constexpr (MI > 2) down_tile<F16, 2, BN, 3>(a, at, lds);
+  if constexpr (MI > 2) down_tile<2, BN, 3>(a, at, lds);
 }
 
 template <int MI, int BN>
@@ -568,9 +535,7 @@ hipError_t launch_gate_up(const ExpertsArgs& a, hipStream_t s) {
 template <int MI, int BN>
 hipError_t launch_down(const ExpertsArgs& a, hipStream_t s) {
   const int64_t total = experts_max_tiles(a.n_rows * a.top_k, a.n_experts, 32 * MI) * ((a.d_model + BN - 1) / BN);
-  const dim3 grid((unsigned)(8 * ((total + 7) / 8))), blk(I8_WAVES * 64);
-  if (a.y_bf16) experts_down_kernel<true, MI, BN><<<grid, blk, 0, s>>>(a);
-  else experts_down_kernel<false, MI, BN><<<grid, blk, 0, s>>>(a);
+  experts_down_kernel<MI, BN><<<dim3((unsigned)(8 * ((total + 7) / 8))), dim3(I8_WAVES * 64), 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -594,9 +559,7 @@ void launch_few_gate_up(const ExpertsArgs& a, int n_pairs, hipStream_t s) {
 template <int NV>
 void launch_few_down(const ExpertsArgs& a, int n_pairs, hipStream_t s) {
   const int cols = (a.d_model + 127) / 128;
-  const dim3 grid((unsigned)(n_pairs * cols)), blk(I8_WAVES * 64);
-  if (a.y_bf16) experts_few_down_kernel<true, NV><<<grid, blk, 0, s>>>(a, n_pairs, cols);
-  else experts_few_down_kernel<false, NV><<<grid, blk, 0, s>>>(a, n_pairs, cols);
+  experts_few_down_kernel<NV><<<dim3((unsigned)(n_pairs * cols)), dim3(I8_WAVES * 64), 0, s>>>(a, n_pairs, cols);
 }
 
 hipError_t launch_few(const ExpertsArgs& a, hipStream_t s) {

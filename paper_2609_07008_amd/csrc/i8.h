@@ -77,7 +77,7 @@ struct ExpertsArgs {
   uint16_t* h;               // [rows top_k, d_ffn] bf16
   int8_t* hq;                // [rows top_k, d_ffn]
   float* hs;                 // [rows top_k] by pair
-  void* part;                // [rows top_k, d_model] by pair: W_down h in f32, or (y in bf16) its sums in f16
+  float* part;               // [rows top_k, d_model] by pair: W_down h without the scale of h
   int32_t tile_rows;
   int32_t few;               // the whole call has at most kExpertsFewPairs pairs: h and part lie apart
 };

@@ -69,7 +69,7 @@ mla_status experts_split(const mla_moe_layer* L, int64_t n_rows, int32_t out_dty
   S->off_xs = take(rows * 4);
   S->off_hq = take(pairs * f);
   S->off_hs = take(pairs * 4);
-  const int64_t h = pairs * f * 2, part = pairs * d * (out_dtype == MLA_BF16 ? 2 : 4);
+  const int64_t h = pairs * f * 2, part = pairs * d * 4;
   S->few = n_rows * L->top_k <= mla::kExpertsFewPairs;
   if (S->few) {
     S->off_h = take(h);
@@ -243,7 +243,7 @@ mla_status mla_moe_experts_i8(const mla_moe_layer* layer, int64_t n_rows, const 
   a.h = reinterpret_cast<uint16_t*>(W + S.off_h);
   a.hq = reinterpret_cast<int8_t*>(W + S.off_hq);
   a.hs = reinterpret_cast<float*>(W + S.off_hs);
-  a.part = W + S.off_part;
+  a.part = reinterpret_cast<float*>(W + S.off_part);
   a.tile_rows = S.tile_rows;
   a.few = S.few;
   const hipError_t e = mla::launch_experts(a, reinterpret_cast<hipStream_t>(stream));
