@@ -762,8 +762,8 @@ mla_status mla_shared_wb_i8(int64_t n_rows, int32_t d_in, int32_t d_out, const v
  *                16-byte aligned
  *   out_dtype, y           MLA_BF16 or MLA_F32; device [N, d_model], 16-byte aligned, every
  *                row written
- *   workspace    device, 256-byte aligned, mla_moe_experts_i8_query bytes; overwritten (calls
- *                that may overlap need one each)
+ *   workspace    device, 256-byte aligned, mla_moe_experts_i8_query bytes (which do for fewer
+ *                rows too); overwritten (calls that may overlap need one each)
  * Everything that changes from call to call is read on the device.  Errors: NULL, SHAPE,
  * UNSUPPORTED, WORKSPACE, HIP.  Kernels only: may be captured.
  * ------------------------------------------------------------------------- */

@@ -612,17 +612,6 @@ hipError_t launch_chunk(const ExpertsArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// The pairs of an expert on average, an upper bound where others hold experts too.  Few: 64 rows x
-// 128 columns, two workgroups a unit, whose time is that of the weights (64 tokens, 6 of 256
-// experts: gate and up 343 us, down 170; 32 x 128 the same, 64 x 256 alone on a unit 350 and 175).
-// Enough to fill them: 128 x 256 (2100 tokens, 6 of 64: 106 and 63 us against 123 and 68 in 64 x 128,
-// 131 and 71 in 256 x 256), then 256 x 256 (33,792 tokens, 6 of 256: 2606 and 1450 against 2897 and
-// 1597 in 128 x 256).
-int32_t experts_tile_rows(int64_t n_pairs, int32_t n_experts) {
-  const int64_t avg = n_pairs / n_experts;
-  return avg <= 128 ? 64 : avg <= 384 ? 128 : 256;
-}
-
 hipError_t launch_experts(const ExpertsArgs& all, hipStream_t s) {
   for (int64_t r = 0; r < all.n_rows; r += kExpertsChunk) {
     ExpertsArgs a = all;

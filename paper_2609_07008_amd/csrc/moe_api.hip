@@ -29,7 +29,9 @@ mla_status check_i8(int64_t n_rows, int32_t n_cols, const void* x, int64_t x_str
   return MLA_OK;
 }
 
-// Where the tables and intermediates of mla_moe_experts_i8 lie in its workspace
+// Where the tables and intermediates of mla_moe_experts_i8 lie in its workspace.  `total` never
+// falls as rows are added, though tiles get taller and h and the parts lie apart up to
+// kExpertsFewPairs pairs alone: bytes that do for a batch do for a smaller one.
 struct ExpertsSplit {
   int32_t tile_rows;
   bool few;
@@ -63,19 +65,21 @@ mla_status experts_split(const mla_moe_layer* L, int64_t n_rows, int32_t out_dty
   };
   S->off_hist = take((int64_t)mla::kDispatchBlocks * L->n_experts * 4);
   S->off_head = take(16);
-  S->off_tiles = take(mla::experts_max_tiles(pairs, L->n_experts, S->tile_rows) * (int64_t)sizeof(mla::ExpertTile));
+  S->off_tiles = take(mla::experts_most_tiles(pairs, L->n_experts) * (int64_t)sizeof(mla::ExpertTile));
   S->off_pairs = take(pairs * (int64_t)sizeof(int2));
   S->off_xq = take(rows * d);
   S->off_xs = take(rows * 4);
   S->off_hq = take(pairs * f);
   S->off_hs = take(pairs * 4);
-  const int64_t h = pairs * f * 2, part = pairs * d * 4;
   S->few = n_rows * L->top_k <= mla::kExpertsFewPairs;
-  if (S->few) {
-    S->off_h = take(h);
-    S->off_part = take(part);
-  } else {   // h is read for the last time before the first of the parts is written
-    S->off_h = S->off_part = take(std::max(h, part));
+  const int64_t before = at, few = std::min<int64_t>(rows, mla::kExpertsFewPairs / L->top_k) * L->top_k;
+  S->off_h = take(few * f * 2);
+  S->off_part = take(few * d * 4);
+  if (!S->few) {   // h is read for the last time before the first of the parts is written
+    const int64_t apart = at;
+    at = before;
+    S->off_h = S->off_part = take(pairs * std::max(f * 2, d * 4));
+    at = std::max(at, apart);
   }
   S->total = (size_t)std::max<int64_t>(at, 256);
   return MLA_OK;
