@@ -138,6 +138,17 @@ def _check(status: int):
         raise MlaError(status, LIB.mla_last_error_detail().decode())
 
 
+def _refuse(what: str, status: int = 2):
+    raise MlaError(status, what)
+
+
+def _int32(*values):
+    """Refuses numbers that the C ABI's int32 arguments cannot hold (ctypes would pass their lower
+    32 bits)."""
+    if max(values) > 0x7FFFFFFF or min(values) < -0x80000000:
+        _refuse(f"{max(values, key=abs)} does not fit 32 bits", 3)
+
+
 def make_geom(g) -> Geom:
     """Geometry from any object with the fields of mla_geom."""
     return Geom(int(g.n_heads), int(g.n_groups), int(g.d_latent), int(g.d_rope), int(g.d_model),
@@ -334,6 +345,7 @@ def moe_fanout(router, tau, expert_idx, expert_w, fanout, expert_count=None, top
     float32 into expert_idx [N, top_k] int32, expert_w [N, top_k] float32,
     fanout [N] int32 and, if given, expert_count [E] int32."""
     n, e = (int(router.shape[0]), int(router.shape[1])) if router is not None else (0, 0)
+    _int32(e, int(top_k), int(min_k))
     _check(LIB.mla_moe_fanout(n, e, _ptr(router), int(top_k), int(min_k), float(tau), _ptr(expert_idx),
                               _ptr(expert_w), _ptr(fanout), _ptr(expert_count), _stream(stream)))
 
@@ -343,6 +355,7 @@ def shared_wb(z, w_b, y, stream=None):
     tensors, y [N, d_out] float32 or bfloat16."""
     n, d_in = int(z.shape[0]), int(z.shape[1])
     d_out = int(w_b.shape[0])
+    _int32(d_in, d_out)
     out = MLA_BF16 if y.dtype == torch.bfloat16 else MLA_F32
     _check(LIB.mla_shared_wb(n, d_in, d_out, _ptr(z), _ptr(w_b), out, _ptr(y), _stream(stream)))
 
@@ -351,10 +364,6 @@ def shared_wb(z, w_b, y, stream=None):
 # (types, shapes, strides, the device); a refusal raises MlaError like the library's own.
 WB_MAX_D_IN, WB_MX4_MAX_ROWS, WB_MX4_MAX_D_OUT = 16384, 1024, 1 << 24   # MLA_WB_MAX_D_IN, MLA_WB_MX4_MAX_ROWS, MLA_WB_MX4_MAX_D_OUT
 CACHE_ROW_BYTES = 400   # a row of the paged 4-bit cache: 256 code bytes, 16 scales, 64 bf16
-
-
-def _refuse(what: str, status: int = 2):
-    raise MlaError(status, what)
 
 
 def _device():
@@ -410,6 +419,7 @@ def mx4_quantize(x, codes, scales, stream=None):
     dev = _device()
     _tensor("x", x, dev, torch.bfloat16, rows=True)
     n, c = x.shape
+    _int32(c)
     _tensor("codes", codes, dev, torch.uint8, (n, c // 2))
     _tensor("scales", scales, dev, torch.uint8, (n, c // 32))
     _check(LIB.mla_mx4_quantize(n, c, _addr(x), _row_stride(x), _addr(codes), _addr(scales), _queue(stream, dev)))
@@ -421,6 +431,7 @@ def mx4_dequantize(codes, scales, x, stream=None):
     dev = _device()
     _tensor("x", x, dev, torch.bfloat16, rows=True)
     n, c = x.shape
+    _int32(c)
     _tensor("codes", codes, dev, torch.uint8, (n, c // 2))
     _tensor("scales", scales, dev, torch.uint8, (n, c // 32))
     _check(LIB.mla_mx4_dequantize(n, c, _addr(codes), _addr(scales), _addr(x), _row_stride(x), _queue(stream, dev)))
@@ -437,6 +448,7 @@ def shared_wb_mx4(z, w_codes, w_scales, y, stream=None):
         _refuse(f"z is {tuple(z.shape)}, w_codes {tuple(w_codes.shape)}")
     n, d_in = z.shape
     d_out = w_codes.shape[0]
+    _int32(d_in, d_out)
     _tensor("w_scales", w_scales, dev, torch.uint8, (d_out, d_in // 32))
     bf16 = isinstance(y, torch.Tensor) and y.dtype == torch.bfloat16
     _tensor("y", y, dev, torch.bfloat16 if bf16 else torch.float32, (n, d_out))
@@ -523,12 +535,14 @@ SCORINGS = {"softmax": 0, "sigmoid": 1}   # MLA_SOFTMAX, MLA_SIGMOID
 def _route_cfg(top_k, scoring="softmax", n_groups=1, top_groups=1, group_best=1, renormalize=True, scale=1.0, min_k=1, tau=2.0):
     if scoring not in SCORINGS:
         _refuse(f"scoring {scoring!r}, expected one of {sorted(SCORINGS)}")
+    _int32(top_k, n_groups, top_groups, group_best, min_k)
     return RouteCfg(SCORINGS[scoring], n_groups, top_groups, group_best, top_k, min_k, bool(renormalize), scale, tau)
 
 
 def check_route(n_experts: int, top_k: int, **cfg):
     """Host-only: refuses what mla_moe_route would refuse for these experts and this choice
     (keyword arguments of moe_route)."""
+    _int32(int(n_experts))
     _check(LIB.mla_moe_route(0, int(n_experts), None, MLA_F32, int(n_experts), None, ctypes.byref(_route_cfg(int(top_k), **cfg)), None, None, None,
                              None, None))
 
@@ -543,6 +557,7 @@ def moe_route(logits, expert_idx, expert_w, fanout=None, expert_count=None, bias
     bf16 = isinstance(logits, torch.Tensor) and logits.dtype == torch.bfloat16
     _tensor("logits", logits, dev, torch.bfloat16 if bf16 else torch.float32, rows=True)
     n, e = logits.shape
+    _int32(e)
     _tensor("expert_idx", expert_idx, dev, torch.int32)
     if expert_idx.dim() != 2 or expert_idx.shape[0] != n:
         _refuse(f"expert_idx is {tuple(expert_idx.shape)}, expected [{n}, top_k]")
@@ -566,6 +581,7 @@ def i8_quantize(x, codes, scales, stream=None):
     dev = _device()
     _tensor("x", x, dev, torch.bfloat16, rows=True)
     n, c = x.shape
+    _int32(c)
     _tensor("codes", codes, dev, torch.int8, (n, c))
     _tensor("scales", scales, dev, torch.float32, (n,))
     _check(LIB.mla_i8_quantize(n, c, _addr(x), _row_stride(x), _addr(codes), _addr(scales), _queue(stream, dev)))
@@ -577,6 +593,7 @@ def i8_dequantize(codes, scales, x, stream=None):
     dev = _device()
     _tensor("x", x, dev, torch.bfloat16, rows=True)
     n, c = x.shape
+    _int32(c)
     _tensor("codes", codes, dev, torch.int8, (n, c))
     _tensor("scales", scales, dev, torch.float32, (n,))
     _check(LIB.mla_i8_dequantize(n, c, _addr(codes), _addr(scales), _addr(x), _row_stride(x), _queue(stream, dev)))
@@ -592,6 +609,7 @@ def shared_wb_i8(z_codes, z_scales, w_codes, w_scales, y, stream=None):
         _refuse(f"z_codes is {tuple(z_codes.shape)}, w_codes {tuple(w_codes.shape)}")
     n, d_in = z_codes.shape
     d_out = w_codes.shape[0]
+    _int32(d_in, d_out)
     _tensor("z_scales", z_scales, dev, torch.float32, (n,))
     _tensor("w_scales", w_scales, dev, torch.float32, (d_out,))
     bf16 = isinstance(y, torch.Tensor) and y.dtype == torch.bfloat16
@@ -600,11 +618,18 @@ def shared_wb_i8(z_codes, z_scales, w_codes, w_scales, y, stream=None):
                                 MLA_BF16 if bf16 else MLA_F32, _addr(y), _queue(stream, dev)))
 
 
+def _moe_layer(*values) -> MoeLayer:
+    _int32(*values)
+    return MoeLayer(*values)
+
+
 def moe_experts_i8_query(n_rows: int, d_model: int, d_ffn: int, n_experts: int, top_k: int, y_dtype=torch.bfloat16) -> int:
     """Host-only: workspace bytes of mla_moe_experts_i8."""
     if y_dtype not in (torch.bfloat16, torch.float32):
         _refuse(f"y_dtype {y_dtype}, expected torch.bfloat16 or torch.float32")
-    layer = MoeLayer(int(d_model), int(d_ffn), int(n_experts), 0, int(top_k))
+    if not 0 <= n_rows < 1 << 63:
+        _refuse(f"n_rows = {n_rows}")
+    layer = _moe_layer(int(d_model), int(d_ffn), int(n_experts), 0, int(top_k))
     ws = ctypes.c_size_t()
     _check(LIB.mla_moe_experts_i8_query(ctypes.byref(layer), int(n_rows), MLA_BF16 if y_dtype == torch.bfloat16 else MLA_F32,
                                         ctypes.byref(ws)))
@@ -638,7 +663,7 @@ def moe_experts_i8(x, expert_idx, expert_w, w_gate_up, s_gate_up, w_down, s_down
     bf16 = isinstance(y, torch.Tensor) and y.dtype == torch.bfloat16
     _tensor("y", y, dev, torch.bfloat16 if bf16 else torch.float32, (n, d))
     _tensor("workspace", workspace, dev, torch.uint8)
-    layer = MoeLayer(d, f, e, first_expert, k)
+    layer = _moe_layer(d, f, e, first_expert, k)
     _check(LIB.mla_moe_experts_i8(ctypes.byref(layer), n, _addr(x), _row_stride(x), _addr(expert_idx), _addr(expert_w), _addr(fanout),
                                   _addr(w_gate_up), _addr(s_gate_up), _addr(w_down), _addr(s_down), MLA_BF16 if bf16 else MLA_F32,
                                   _addr(y), _addr(workspace), workspace.numel(), _queue(stream, dev)))
