@@ -660,8 +660,9 @@ mla_status mla_cache_attend(const mla_geom* geom, int32_t n_seqs, int32_t n_q, c
  *      min_k = top_k) keeps all.
  * Choices and fanouts are those of scores in 64 bits, so that neighbours in rank a
  * rounding apart come out in their order; weights are within 2^-19 of their value.
- * A NaN never ranks before a number; a row with a NaN or a +infinity has NaN softmax
- * scores (its order stays that of the logits), a row of -infinity alone has scores 0.
+ * A NaN never ranks before a number.  A row with a NaN or a +infinity has NaN softmax
+ * scores: its groups are the lowest, in them the order is that of the logits without a
+ * bias and that of the indexes with one.  A row of -infinity alone has scores 0.
  * An expert with bias -infinity is chosen only where nothing else is left; a group whose
  * group_best largest c have one among them scores -infinity.
  *
