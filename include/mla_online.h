@@ -750,7 +750,8 @@ mla_status mla_shared_wb_i8(int64_t n_rows, int32_t d_in, int32_t d_out, const v
  * row, y = 0).  An expert may be given twice in a row and counts twice.
  *   layer        host: d_model, d_ffn multiples of 64 up to MLA_I8_MAX_COLS; n_experts
  *                here (1 .. 1024); first_expert >= 0; top_k columns of expert_idx (1 .. 16:
- *                a caller may append experts that every row uses)
+ *                experts that every row uses may come in front of a router's, counted in
+ *                fanout; behind them they would lie past it)
  *   n_rows       N (>= 0); taken 65536 at a time, which bounds the workspace
  *   x            device bf16 [N, d_model], rows x_stride elements apart (a multiple of 8, at
  *                least d_model), 16-byte aligned
