@@ -2,9 +2,8 @@
 // and the experts of a mixture-of-experts layer in them: argument structs and launchers.
 #pragma once
 
-#include <initializer_list>
-
 #include "common.h"
+#include "i8_rules.h"
 
 namespace mla {
 
@@ -84,30 +83,6 @@ struct ExpertsArgs {
   int32_t few;               // the whole call has at most kExpertsFewPairs pairs: h and part lie apart
 };
 
-// Rows of a tile, by the pairs of an expert on average, an upper bound where others hold experts too.  Few: 64 rows x
-// 128 columns, two workgroups a unit, whose time is that of the weights (64 tokens, 6 of 256
-// experts: gate and up 343 us, down 170; 32 x 128 the same, 64 x 256 alone on a unit 350 and 175).
-// Enough to fill them: 128 x 256 (2100 tokens, 6 of 64: 106 and 63 us against 123 and 68 in 64 x 128,
-// 131 and 71 in 256 x 256), then 256 x 256 (33,792 tokens, 6 of 256: 2606 and 1450 against 2897 and
-// 1597 in 128 x 256).
-constexpr int64_t kExpertsAvg64 = 128, kExpertsAvg128 = 384;   // the most for 64 and for 128 rows
-inline int32_t experts_tile_rows(int64_t n_pairs, int32_t n_experts) {
-  const int64_t avg = n_pairs / n_experts;
-  return avg <= kExpertsAvg64 ? 64 : avg <= kExpertsAvg128 ? 128 : 256;
-}
-inline int64_t experts_max_tiles(int64_t n_pairs, int32_t n_experts, int32_t tile_rows) {
-  return n_pairs / tile_rows + (n_experts < n_pairs ? n_experts : n_pairs);
-}
-// the most tiles that any number of pairs up to n_pairs has in the height taken for it
-inline int64_t experts_most_tiles(int64_t n_pairs, int32_t n_experts) {
-  const int64_t upto64 = (kExpertsAvg64 + 1) * n_experts - 1, upto128 = (kExpertsAvg128 + 1) * n_experts - 1;
-  int64_t most = 0;
-  for (const int64_t n : {upto64, upto128, n_pairs}) {
-    const int64_t met = n < n_pairs ? n : n_pairs, tiles = experts_max_tiles(met, n_experts, experts_tile_rows(met, n_experts));
-    most = tiles > most ? tiles : most;
-  }
-  return most;
-}
 hipError_t launch_experts(const ExpertsArgs& a, hipStream_t s);
 
 }  // namespace mla

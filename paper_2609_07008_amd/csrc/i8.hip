@@ -38,7 +38,6 @@ __global__ __launch_bounds__(256) void i8_dequantize_kernel(I8Args a, int segs) 
 }
 
 constexpr int kWbGroup = 8;                              // row panels per column panel in the tile walk
-constexpr int64_t kI8FewRows = 32, kI8FewBlocks = 256;   // largest requests of the few-row kernel
 
 // y = W_b z in tiles (i8_tiles.h).  Workgroups go to the 8 XCDs round-robin, so XCD x takes a
 // contiguous range of tiles, and inside it tiles walk 8 row panels per column panel.  The output
@@ -210,61 +209,44 @@ __global__ __launch_bounds__(I8_WAVES * 64) void wb_i8_rows_kernel(WbI8Args a) {
   }
 }
 
-template <bool OUT_BF16, int MI, int BN, int NST>
+template <bool OUT_BF16, int MI, int BN>
 hipError_t launch_tiles(const WbI8Args& a, hipStream_t s) {
   const int m_tiles = (int)((a.n_rows + 32 * MI - 1) / (32 * MI));
   const int n_tiles = (a.d_out + BN - 1) / BN;
   const int total = m_tiles * n_tiles;
   // an output beyond the L2s' 32 MB cannot stay there: stored past them, it leaves them to the panels
   const bool stream_out = a.n_rows * a.d_out * (OUT_BF16 ? 2 : 4) > (int64_t)32 << 20;
-  wb_i8_tile_kernel<OUT_BF16, MI, BN, NST><<<dim3((unsigned)(8 * ((total + 7) / 8))), dim3(I8_WAVES * 64), 0, s>>>(a, m_tiles, n_tiles, stream_out);
+  wb_i8_tile_kernel<OUT_BF16, MI, BN, wb_i8_slices(32 * MI, BN)><<<dim3((unsigned)(8 * ((total + 7) / 8))), dim3(I8_WAVES * 64), 0, s>>>(a, m_tiles, n_tiles, stream_out);
+  return hipGetLastError();
+}
+
+template <bool OUT_BF16, int MB>
+hipError_t launch_few(const WbI8Args& a, hipStream_t s) {
+  wb_i8_rows_kernel<OUT_BF16, MB, wb_i8_slices(16 * MB, 16)><<<dim3((unsigned)((a.d_out + 15) / 16)), dim3(I8_WAVES * 64), 0, s>>>(a);
   return hipGetLastError();
 }
 
 template <bool OUT_BF16>
 hipError_t launch_out(const WbI8Args& a, hipStream_t s) {
-  // Up to 32 rows and a workgroup of 16 channels a compute unit, the few-row kernel: 4096 -> 4096
-  // at 16 rows 8.2 us, in tiles of 32 x 64 9.4.
-  const int64_t few_blocks = ((int64_t)a.d_out + 15) / 16;
-  if (a.n_rows <= kI8FewRows && few_blocks <= kI8FewBlocks) {
-    if (a.n_rows <= 16) wb_i8_rows_kernel<OUT_BF16, 1, 4><<<dim3((unsigned)few_blocks), dim3(I8_WAVES * 64), 0, s>>>(a);
-    else wb_i8_rows_kernel<OUT_BF16, 2, 3><<<dim3((unsigned)few_blocks), dim3(I8_WAVES * 64), 0, s>>>(a);
-    return hipGetLastError();
-  }
-  // The tile whose rounds over the 256 compute units cost least: a round of 32 mi rows x 256
-  // channels taken as 6 (mi + 3), x 128 as 2 (mi + 7), x 64 as 9 and 10 (mi = 1, 2; two fit a unit,
-  // and a second round comes in under the first).  At 4096 channels, weights from memory: 64 rows
-  // 9.9 us at 32 x 64 against 14.8 at 32 x 128, 300 rows 16.6 at 64 x 128 against 21 at 32 x 64, 1000 rows 23.8 at 128 x 128 against 26.4 at 64 x 256, 2100 rows 41.6 at 160 x 256
-  // against 46.7 at 256 x 256, 4096 rows 58 at 256 x 256 against 71 at 128 x 256; 33 rows of 7168 ->
-  // 16384 23.7 at 64 x 64 against 27.5 at 32 x 128.
-  int best = 8;
-  int64_t cost = INT64_MAX;
-  auto tile = [&](int id, int mi, int bn, int w, int first) {
-    const int64_t tiles = (a.n_rows + 32 * mi - 1) / (32 * mi) * ((a.d_out + bn - 1) / bn);
-    const int64_t c = (tiles + 255) / 256 * w + first;
-    if (c < cost) {
-      cost = c;
-      best = id;
+  const I8TileShape t = wb_i8_tile(a.n_rows, a.d_out);
+  if (t.channels == 16) return t.rows == 16 ? launch_few<OUT_BF16, 1>(a, s) : launch_few<OUT_BF16, 2>(a, s);
+  if (t.channels == 64) return t.rows == 32 ? launch_tiles<OUT_BF16, 1, 64>(a, s) : launch_tiles<OUT_BF16, 2, 64>(a, s);
+  if (t.channels == 128) {
+    switch (t.rows) {
+      case 32: return launch_tiles<OUT_BF16, 1, 128>(a, s);
+      case 64: return launch_tiles<OUT_BF16, 2, 128>(a, s);
+      case 96: return launch_tiles<OUT_BF16, 3, 128>(a, s);
+      default: return launch_tiles<OUT_BF16, 4, 128>(a, s);
     }
-  };
-  for (int mi = 8; mi >= 2; --mi) tile(mi, mi, 256, 6 * (mi + 3), 0);
-  for (int mi = 4; mi >= 1; --mi) tile(10 + mi, mi, 128, 2 * (mi + 7), 0);
-  tile(22, 2, 64, 10, 1);
-  tile(21, 1, 64, 9, 1);
-  switch (best) {
-    case 2: return launch_tiles<OUT_BF16, 2, 256, 3>(a, s);
-    case 3: return launch_tiles<OUT_BF16, 3, 256, 3>(a, s);
-    case 4: return launch_tiles<OUT_BF16, 4, 256, 3>(a, s);
-    case 5: return launch_tiles<OUT_BF16, 5, 256, 3>(a, s);
-    case 6: return launch_tiles<OUT_BF16, 6, 256, 2>(a, s);
-    case 7: return launch_tiles<OUT_BF16, 7, 256, 2>(a, s);
-    case 11: return launch_tiles<OUT_BF16, 1, 128, 7>(a, s);
-    case 12: return launch_tiles<OUT_BF16, 2, 128, 6>(a, s);
-    case 13: return launch_tiles<OUT_BF16, 3, 128, 5>(a, s);
-    case 14: return launch_tiles<OUT_BF16, 4, 128, 4>(a, s);
-    case 21: return launch_tiles<OUT_BF16, 1, 64, 6>(a, s);
-    case 22: return launch_tiles<OUT_BF16, 2, 64, 5>(a, s);
-    default: return launch_tiles<OUT_BF16, 8, 256, 2>(a, s);
+  }
+  switch (t.rows) {
+    case 64: return launch_tiles<OUT_BF16, 2, 256>(a, s);
+    case 96: return launch_tiles<OUT_BF16, 3, 256>(a, s);
+    case 128: return launch_tiles<OUT_BF16, 4, 256>(a, s);
+    case 160: return launch_tiles<OUT_BF16, 5, 256>(a, s);
+    case 192: return launch_tiles<OUT_BF16, 6, 256>(a, s);
+    case 224: return launch_tiles<OUT_BF16, 7, 256>(a, s);
+    default: return launch_tiles<OUT_BF16, 8, 256>(a, s);
   }
 }
 
