@@ -144,9 +144,10 @@ def _refuse(what: str, status: int = 2):
 
 def _int32(*values):
     """Refuses numbers that the C ABI's int32 arguments cannot hold (ctypes would pass their lower
-    32 bits)."""
-    if max(values) > 0x7FFFFFFF or min(values) < -0x80000000:
-        _refuse(f"{max(values, key=abs)} does not fit 32 bits", 3)
+    32 bits).  Calls that are made often ask it only of what has a bit past the 31st."""
+    for v in values:
+        if not -0x80000000 <= v <= 0x7FFFFFFF:
+            _refuse(f"{v} does not fit 32 bits", 3)
 
 
 def make_geom(g) -> Geom:
@@ -355,7 +356,8 @@ def shared_wb(z, w_b, y, stream=None):
     tensors, y [N, d_out] float32 or bfloat16."""
     n, d_in = int(z.shape[0]), int(z.shape[1])
     d_out = int(w_b.shape[0])
-    _int32(d_in, d_out)
+    if (d_in | d_out) >> 31:
+        _int32(d_in, d_out)
     out = MLA_BF16 if y.dtype == torch.bfloat16 else MLA_F32
     _check(LIB.mla_shared_wb(n, d_in, d_out, _ptr(z), _ptr(w_b), out, _ptr(y), _stream(stream)))
 
@@ -419,7 +421,8 @@ def mx4_quantize(x, codes, scales, stream=None):
     dev = _device()
     _tensor("x", x, dev, torch.bfloat16, rows=True)
     n, c = x.shape
-    _int32(c)
+    if c >> 31:
+        _int32(c)
     _tensor("codes", codes, dev, torch.uint8, (n, c // 2))
     _tensor("scales", scales, dev, torch.uint8, (n, c // 32))
     _check(LIB.mla_mx4_quantize(n, c, _addr(x), _row_stride(x), _addr(codes), _addr(scales), _queue(stream, dev)))
@@ -431,7 +434,8 @@ def mx4_dequantize(codes, scales, x, stream=None):
     dev = _device()
     _tensor("x", x, dev, torch.bfloat16, rows=True)
     n, c = x.shape
-    _int32(c)
+    if c >> 31:
+        _int32(c)
     _tensor("codes", codes, dev, torch.uint8, (n, c // 2))
     _tensor("scales", scales, dev, torch.uint8, (n, c // 32))
     _check(LIB.mla_mx4_dequantize(n, c, _addr(codes), _addr(scales), _addr(x), _row_stride(x), _queue(stream, dev)))
@@ -448,7 +452,8 @@ def shared_wb_mx4(z, w_codes, w_scales, y, stream=None):
         _refuse(f"z is {tuple(z.shape)}, w_codes {tuple(w_codes.shape)}")
     n, d_in = z.shape
     d_out = w_codes.shape[0]
-    _int32(d_in, d_out)
+    if (d_in | d_out) >> 31:
+        _int32(d_in, d_out)
     _tensor("w_scales", w_scales, dev, torch.uint8, (d_out, d_in // 32))
     bf16 = isinstance(y, torch.Tensor) and y.dtype == torch.bfloat16
     _tensor("y", y, dev, torch.bfloat16 if bf16 else torch.float32, (n, d_out))
@@ -535,7 +540,8 @@ SCORINGS = {"softmax": 0, "sigmoid": 1}   # MLA_SOFTMAX, MLA_SIGMOID
 def _route_cfg(top_k, scoring="softmax", n_groups=1, top_groups=1, group_best=1, renormalize=True, scale=1.0, min_k=1, tau=2.0):
     if scoring not in SCORINGS:
         _refuse(f"scoring {scoring!r}, expected one of {sorted(SCORINGS)}")
-    _int32(top_k, n_groups, top_groups, group_best, min_k)
+    if (top_k | n_groups | top_groups | group_best | min_k) >> 31:
+        _int32(top_k, n_groups, top_groups, group_best, min_k)
     return RouteCfg(SCORINGS[scoring], n_groups, top_groups, group_best, top_k, min_k, bool(renormalize), scale, tau)
 
 
@@ -557,7 +563,8 @@ def moe_route(logits, expert_idx, expert_w, fanout=None, expert_count=None, bias
     bf16 = isinstance(logits, torch.Tensor) and logits.dtype == torch.bfloat16
     _tensor("logits", logits, dev, torch.bfloat16 if bf16 else torch.float32, rows=True)
     n, e = logits.shape
-    _int32(e)
+    if e >> 31:
+        _int32(e)
     _tensor("expert_idx", expert_idx, dev, torch.int32)
     if expert_idx.dim() != 2 or expert_idx.shape[0] != n:
         _refuse(f"expert_idx is {tuple(expert_idx.shape)}, expected [{n}, top_k]")
@@ -581,7 +588,8 @@ def i8_quantize(x, codes, scales, stream=None):
     dev = _device()
     _tensor("x", x, dev, torch.bfloat16, rows=True)
     n, c = x.shape
-    _int32(c)
+    if c >> 31:
+        _int32(c)
     _tensor("codes", codes, dev, torch.int8, (n, c))
     _tensor("scales", scales, dev, torch.float32, (n,))
     _check(LIB.mla_i8_quantize(n, c, _addr(x), _row_stride(x), _addr(codes), _addr(scales), _queue(stream, dev)))
@@ -593,7 +601,8 @@ def i8_dequantize(codes, scales, x, stream=None):
     dev = _device()
     _tensor("x", x, dev, torch.bfloat16, rows=True)
     n, c = x.shape
-    _int32(c)
+    if c >> 31:
+        _int32(c)
     _tensor("codes", codes, dev, torch.int8, (n, c))
     _tensor("scales", scales, dev, torch.float32, (n,))
     _check(LIB.mla_i8_dequantize(n, c, _addr(codes), _addr(scales), _addr(x), _row_stride(x), _queue(stream, dev)))
@@ -609,7 +618,8 @@ def shared_wb_i8(z_codes, z_scales, w_codes, w_scales, y, stream=None):
         _refuse(f"z_codes is {tuple(z_codes.shape)}, w_codes {tuple(w_codes.shape)}")
     n, d_in = z_codes.shape
     d_out = w_codes.shape[0]
-    _int32(d_in, d_out)
+    if (d_in | d_out) >> 31:
+        _int32(d_in, d_out)
     _tensor("z_scales", z_scales, dev, torch.float32, (n,))
     _tensor("w_scales", w_scales, dev, torch.float32, (d_out,))
     bf16 = isinstance(y, torch.Tensor) and y.dtype == torch.bfloat16
@@ -618,9 +628,10 @@ def shared_wb_i8(z_codes, z_scales, w_codes, w_scales, y, stream=None):
                                 MLA_BF16 if bf16 else MLA_F32, _addr(y), _queue(stream, dev)))
 
 
-def _moe_layer(*values) -> MoeLayer:
-    _int32(*values)
-    return MoeLayer(*values)
+def _moe_layer(d_model: int, d_ffn: int, n_experts: int, first_expert: int, top_k: int) -> MoeLayer:
+    if (d_model | d_ffn | n_experts | first_expert | top_k) >> 31:
+        _int32(d_model, d_ffn, n_experts, first_expert, top_k)
+    return MoeLayer(d_model, d_ffn, n_experts, first_expert, top_k)
 
 
 def moe_experts_i8_query(n_rows: int, d_model: int, d_ffn: int, n_experts: int, top_k: int, y_dtype=torch.bfloat16) -> int:
