@@ -7,8 +7,12 @@
 // (route_row_kernel, by 16 lanes up to 256 experts, else by a wave): c becomes a fixed-point code of
 // 24 or 22 bits over its whole range, above the inverted index in a 32-bit key, and whatever hangs
 // on two codes that the errors could have swapped sends its row to route_exact: one in some
-// hundreds of rows of random logits.  Where groups do not fit the lanes every row takes the
-// 64-bit path.
+// hundreds to thousands of rows of random logits, and more where the biases share an offset, which widens
+// the range (264,192 rows of 256: 109 us, with an offset of 5 133, of 50 181).  A lane keeps its 5 or 6
+// largest keys, so rows also go there where the groups kept lie on few lanes: all of them where one
+// group of one lane gives 6 or more (66,048 rows of 256 in 16 groups, top 8: 335 us, of two groups 125, of
+// five 52; in 8 groups, one kept, 170, four 54; one row of the first 20, of the last 8).  Where groups
+// do not fit the lanes every row does.
 #include "rank.h"
 #include "route.h"
 
@@ -38,9 +42,9 @@ __device__ __forceinline__ double from_order_bits(uint64_t k) {
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup"); }
 
 // A row by a whole wave in 64 bits; lane holds experts lane, lane + 64, ...; `score` and `key` are
-// LDS of the wave, [E].  Lane j returns
-// the expert of rank j if the row executes it, else -1.  Loops stay rolled: where this runs for one row in hundreds its time is
-// that of fetching its instructions (unrolled by four, some 150 rows of 264,192 cost 30 us).
+// LDS of the wave, [E].  Lane j returns the expert of rank j if the row executes it, else -1.
+// Loops stay rolled: where this runs for one row in hundreds its time is that of fetching its
+// instructions (unrolled by four, some 150 rows of 264,192 cost 30 us).
 __device__ int route_exact(const RouteArgs& a, int64_t r, int lane, double* score, uint64_t* key) {
   const int E = a.n_experts;
   double m = -INFINITY, sum = 0.0;
@@ -267,10 +271,11 @@ __device__ __forceinline__ void load_logits(const RouteArgs& a, int wide, int64_
 // the sigmoid's exponential is off by (1.5 |l| + 2) 2^-24 of itself, of which s (1 - s) <= 1/4 and
 // s (1 - s) |l| < 0.23 reach s; 1 + e and its reciprocal add 3 s: below 4.  The bias in code units
 // is off by 2, the fma by 1/2, the conversion by 1: a code by less than 8, and the order of two
-// that are 17 apart is certain.  A softmax score takes the sum's error besides (its terms' 1.5 d + 2
-// weighted by e^-d, and 20 additions), relative, below 50, and its factor's 2: with the bias's 2 and
-// the last two below 56 of its range, the row's largest score + 2 B: 113 apart.  Codes of 22 bits,
-// under indexes of 10, are off by a quarter of that and by the last two: less than 4 and 16.  A group's score is the
+// that are 17 apart is certain.  A softmax score takes the sum's error besides (its terms' 2.3 d + 2
+// at a distance d from the largest logit, whose mean weighted by e^-d is at most 4.5 with 1024
+// experts, and 11 additions), relative, below 50, and its factor's 2: with the bias's 2 and the last
+// two below 56 of its range, the row's largest score + 2 B: 113 apart.  Codes of 22 bits, under
+// indexes of 10, are off by a quarter of that and by the last two: less than 4 and 16.  A group's score is the
 // sum of two codes: twice that.  Without a bias codes are the upper bits of the logit's order: exact
 // for bf16, else equal codes are not certain.  What is no number, or -infinity, has a code at the
 // bottom of its kind, as have the places past the end: a row that comes down to it is not certain
@@ -391,7 +396,7 @@ __global__ __launch_bounds__(256, 4) void route_row_kernel(RouteArgs a, int lg, 
       uint32_t lo = 0, hi = 0;   // kByPair: the order of a sum less and plus its error
       if constexpr (BY == kByPair) {
         // The scores (a softmax's without its sum) of the middles of the two codes: the logit is off by
-        // |x| 2^(IB - 24), the exponential by (1.5 * 70 + 2) 2^-24 of itself and what follows by 6.  Taken
+        // |x| 2^(IB - 24), the exponential by (2.3 * 70 + 2) 2^-24 of itself and what follows by 6.  Taken
         // twice and more, in relative terms.  Sigmoids that add up to more than 1 are ordered by what
         // lacks to 2, sigmoid(-x) each, which has its bits where they have none.
         float sum = 0.f, err = 0.f, lack = 0.f, lack_err = 0.f;
