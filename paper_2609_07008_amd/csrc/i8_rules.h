@@ -31,9 +31,10 @@ inline I8TileShape wb_i8_tile(int64_t n_rows, int32_t d_out) {
   // The tile whose rounds over the 256 compute units cost least: a round of 32 mi rows x 256
   // channels taken as 6 (mi + 3), x 128 as 2 (mi + 7), x 64 as 9 and 10 (mi = 1, 2; two fit a unit,
   // and a second round comes in under the first).  At 4096 channels, weights from memory: 64 rows
-  // 9.9 us at 32 x 64 against 14.8 at 32 x 128, 300 rows 16.6 at 64 x 128 against 21 at 32 x 64, 1000 rows 23.8 at 128 x 128 against 26.4 at 64 x 256, 2100 rows 41.6 at 160 x 256
-  // against 46.7 at 256 x 256, 4096 rows 58 at 256 x 256 against 71 at 128 x 256; 33 rows of 7168 ->
-  // 16384 23.7 at 64 x 64 against 27.5 at 32 x 128.
+  // 9.9 us at 32 x 64 against 14.8 at 32 x 128, 300 rows 16.6 at 64 x 128 against 21 at 32 x 64,
+  // 1000 rows 23.8 at 128 x 128 against 26.4 at 64 x 256, 2100 rows 41.6 at 160 x 256 against 46.7
+  // at 256 x 256, 4096 rows 58 at 256 x 256 against 71 at 128 x 256; 33 rows of 7168 -> 16384 23.7
+  // at 64 x 64 against 27.5 at 32 x 128.
   I8TileShape best{256, 256};
   int64_t cost = INT64_MAX;
   auto tile = [&](int mi, int bn, int w, int first) {
@@ -52,11 +53,11 @@ inline I8TileShape wb_i8_tile(int64_t n_rows, int32_t d_out) {
 }
 
 // Rows of a tile of the experts' products, by the pairs of an expert on average, an upper bound
-// where others hold experts too.  Few: 64 rows x 128 columns, two workgroups a unit, whose time is that of the weights (64 tokens, 6 of 256
-// experts: gate and up 343 us, down 170; 32 x 128 the same, 64 x 256 alone on a unit 350 and 175).
-// Enough to fill them: 128 x 256 (2100 tokens, 6 of 64: 106 and 63 us against 123 and 68 in 64 x 128,
-// 131 and 71 in 256 x 256), then 256 x 256 (33,792 tokens, 6 of 256: 2606 and 1450 against 2897 and
-// 1597 in 128 x 256).
+// where others hold experts too.  Few: 64 rows x 128 columns, two workgroups a unit, whose time is
+// that of the weights (64 tokens, 6 of 256 experts: gate and up 345 us, down 175; 32 x 128 the same,
+// 128 x 256 356 and 180).  Enough to fill them: 128 x 256 (2100 tokens, 6 of 64: 109 and 72 us against
+// 124 and 76 in 64 x 128, 123 and 81 in 256 x 256), then 256 x 256 (33,792 tokens, 6 of 256: 2.63 and
+// 1.73 ms against 2.96 and 1.99 in 128 x 256).
 constexpr int64_t kExpertsAvg64 = 128, kExpertsAvg128 = 384;   // the most for 64 and for 128 rows
 inline int32_t experts_tile_rows(int64_t n_pairs, int32_t n_experts) {
   const int64_t avg = n_pairs / n_experts;
